@@ -313,6 +313,50 @@ ew_status_t ew_last_device_error(ew_pool_t *pool, int32_t *code);
  * touched outside the pool's error word. */
 ew_status_t ew_selftest_bounded_wait(ew_pool_t *pool, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Stand-alone operators: the pieces of an expert outside a forward, for callers that tune an adapter's experts (the
+ * products' gradients, which ew_load_adapter's weights come from) or serve them in four bits.  They take no pool.
+ *   device       CUDA device ordinal that all pointers and the stream belong to; -1 gives EW_ERR_NO_DEVICE
+ *   dtype        type of the operands; out_dtype of the results (ew_dtype_t)
+ *   ld*          elements between the rows of a row-major matrix; the innermost dimension is contiguous
+ * All pointers are DEVICE memory; results may not overlap operands; calls are asynchronous on cuda_stream, allocate
+ * nothing, keep nothing and may come from several threads.  They may be captured into a CUDA graph after one call on
+ * that device outside a capture.  An index in device memory that lies outside its range cannot fail the call: it is
+ * clamped or skipped as said below and reported by ew_last_operator_error.
+ * ------------------------------------------------------------------------------------------------------------ */
+typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2 } ew_dtype_t;
+
+/* Matrix product grouped by expert (Section 2.1's grouped matrix multiplication, on its own): for every group g and
+ * its rows offsets[g] <= r < offsets[g+1]
+ *     y[r, :] = x[r, :] w[g]^T        x [rows, k], w [groups, n, k] (group_stride elements between groups), y [rows, n]
+ * accumulated in fp32 and rounded once.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
+ * they need not start at 0 nor end at `rows`, and rows outside them are left as they were.  An offset below the one
+ * before it or outside [0, rows] is clamped and reported as EW_ERR_INVALID_ARG.
+ * dtype: EW_BF16 or EW_FP16; out_dtype: the same or EW_FP32.  x and w are 16-byte aligned with ldx, ldw and
+ * group_stride multiples of 8 (n and k may be anything up to them); y needs its element's alignment only.
+ * groups <= 2048.  rows = 0 is a no-op.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
+ew_status_t ew_grouped_mm(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *w,
+                          int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows, int32_t groups,
+                          int32_t n, int32_t k, void *y, int64_t ldy, void *cuda_stream);
+
+/* Its gradient with respect to x:  dx[r, :] = dy[r, :] w[g]    dy [rows, n], dx [rows, k]; all else as above. */
+ew_status_t ew_grouped_mm_dx(int32_t device, int32_t dtype, int32_t out_dtype, const void *dy, int64_t lddy,
+                             const void *w, int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows,
+                             int32_t groups, int32_t n, int32_t k, void *dx, int64_t lddx, void *cuda_stream);
+
+/* Its gradient with respect to w:  dw[g] = dy_g^T x_g over the rows of group g, or dw[g] += with accumulate != 0
+ * (added in fp32 and rounded to out_dtype).  dw [groups, n, k]; the gradient of a group without rows is zero (with
+ * accumulate: stays as it is).  To take the gradient of some groups only, pass their part of offsets and dw.
+ * lddw and group_stride may be any strides that keep rows apart; all else as above. */
+ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, const void *dy, int64_t lddy,
+                             const void *x, int64_t ldx, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n,
+                             int32_t k, int32_t accumulate, void *dw, int64_t lddw, int64_t group_stride,
+                             void *cuda_stream);
+
+/* Read and clear the operators' error word of a device (waits for all work on it).  *code receives EW_OK,
+ * EW_ERR_INVALID_ARG (an index in device memory was outside its range) or EW_ERR_TIMEOUT (a bounded wait expired). */
+ew_status_t ew_last_operator_error(int32_t device, int32_t *code);
+
 /* Device address of slot `slot` of a layer's fused gate|up tensor (which = 0) or down tensor
  * (which = 1); slots M + N*E_max .. +S-1 are the shared experts.  For tests and tools: reading an
  * unmapped slot faults, so callers must only touch slots of loaded experts. */

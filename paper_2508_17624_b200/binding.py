@@ -23,7 +23,8 @@ STATUS_NAMES = ["EW_OK", "EW_ERR_INVALID_ARG", "EW_ERR_OOM", "EW_ERR_SLOT_IN_USE
 EXPORTS = ["ew_pool_create", "ew_pool_destroy", "ew_load_base", "ew_load_adapter", "ew_unload_adapter",
            "ew_pool_trim", "ew_moe_forward", "ew_moe_forward_debug", "ew_moe_forward_host", "ew_profile_enable",
            "ew_profile_read", "ew_reroute", "ew_reroute_unfused", "ew_route_logits", "ew_route_noalloc", "ew_selftest_bounded_wait", "ew_get_expert_map",
-           "ew_moe_forward_partial", "ew_ep_finish", "ew_moe_forward_scatter", "ew_ep_finish_gathered", "ew_pool_stats", "ew_last_device_error", "ew_slot_address", "ew_status_str", "ew_last_error_string"]
+           "ew_moe_forward_partial", "ew_ep_finish", "ew_moe_forward_scatter", "ew_ep_finish_gathered", "ew_pool_stats", "ew_last_device_error", "ew_slot_address", "ew_grouped_mm", "ew_grouped_mm_dx", "ew_grouped_mm_dw",
+           "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
 
 
 class EwConfig(C.Structure):
@@ -67,6 +68,11 @@ def lib():
         _lib.ew_last_error_string.restype = C.c_char_p
         for name in EXPORTS:
             getattr(_lib, name)
+        # the stand-alone operators are called with plain integers (addresses among them)
+        i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
+        for name in ("ew_grouped_mm", "ew_grouped_mm_dx"):
+            getattr(_lib, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, i64, ptr, i32, i32, i32, i32, ptr, i64, ptr]
+        _lib.ew_grouped_mm_dw.argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, i64, i64, ptr]
     return _lib
 
 
@@ -287,6 +293,115 @@ class Pool:
         p = C.c_void_p()
         _check(lib().ew_slot_address(self._h, layer, which, slot, C.byref(p)), "ew_slot_address")
         return p.value or 0
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Stand-alone operators (no pool): argument checks, output allocation, one library call on the current stream.
+_DTYPE = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+
+
+def _dtype(t) -> int:
+    code = _DTYPE.get(str(t))
+    if code is None:
+        raise ValueError(f"dtype {t} is not supported: bfloat16, float16 (results also float32)")
+    return code
+
+
+def _on(t, like=None, ndim=2, name="operand", dtype=None):
+    """Checks a device tensor: dimensions, type, contiguous innermost dimension, the same device as `like`."""
+    if not t.is_cuda or t.dim() != ndim:
+        raise ValueError(f"{name}: a {ndim}-dimensional CUDA tensor is wanted, got {tuple(t.shape)} on {t.device}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, the other operands on {like.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, {dtype} is wanted")
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the innermost dimension is not contiguous")
+    return t
+
+
+def _stride(t, dim) -> int:
+    """Elements between the rows (or matrices) of `t`; a dimension of length one has no stride of its own."""
+    if t.shape[dim] > 1:
+        return t.stride(dim)
+    n = t.shape[-1] if dim in (-2, t.dim() - 2) else t.shape[-2] * _stride(t, -2)
+    return (n + 7) // 8 * 8
+
+
+def _offsets(offsets, like):
+    _on(offsets, like, 1, "offsets")
+    if str(offsets.dtype) != "torch.int32" or offsets.shape[0] < 2 or offsets.stride(0) != 1:
+        raise ValueError("offsets: a contiguous int32 tensor with one more entry than groups is wanted")
+    return offsets.shape[0] - 1
+
+
+def _stream_of(device):
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _result(out, shape, dtype, like, name="out"):
+    import torch
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _on(out, like, len(shape), name)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
+        raise ValueError(f"{name}: {tuple(shape)} of {dtype} is wanted, got {tuple(out.shape)} of {out.dtype}")
+    return out
+
+
+def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
+    _on(a, name="the rows' operand")
+    _on(w, a, 3, "w", a.dtype)
+    groups, n, k = w.shape
+    if _offsets(offsets, a) != groups:
+        raise ValueError(f"offsets has {offsets.shape[0]} entries for {groups} groups")
+    if a.shape[1] != (n if grad else k):
+        raise ValueError(f"rows of {a.shape[1]} do not match w of {tuple(w.shape)}")
+    rows = a.shape[0]
+    out = _result(out, (rows, k if grad else n), out_dtype or (a.dtype if out is None else out.dtype), a)
+    dev = a.device
+    _check(fn(dev.index, _dtype(a.dtype), _dtype(out.dtype), a.data_ptr(), _stride(a, 0), w.data_ptr(), _stride(w, 1),
+              _stride(w, 0), offsets.data_ptr(), rows, groups, n, k, out.data_ptr(), _stride(out, 0), _stream_of(dev)), where)
+    return out
+
+
+def grouped_mm(x, w, offsets, out=None, out_dtype=None):
+    """y[r] = x[r] w[g]^T for the rows offsets[g] <= r < offsets[g+1] of each group: x [rows, k], w [groups, n, k], offsets
+    int32 [groups + 1] (all on one device).  Rows outside the offsets are left as they were in `out`.  out_dtype: x's type
+    or float32.  See the header for alignment."""
+    return _rows_product(lib().ew_grouped_mm, "ew_grouped_mm", x, w, offsets, out, out_dtype, False)
+
+
+def grouped_mm_dx(dy, w, offsets, out=None, out_dtype=None):
+    """The gradient of `grouped_mm` with respect to x: dx[r] = dy[r] w[g]; dy [rows, n] -> [rows, k]."""
+    return _rows_product(lib().ew_grouped_mm_dx, "ew_grouped_mm_dx", dy, w, offsets, out, out_dtype, True)
+
+
+def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
+    """The gradient of `grouped_mm` with respect to w: dw[g] = dy_g^T x_g -> [groups, n, k]; a group without rows gets zeros.
+    accumulate: adds to `out` instead (required then), as over the steps of a large batch."""
+    _on(dy, name="dy")
+    _on(x, dy, 2, "x", dy.dtype)
+    groups = _offsets(offsets, dy)
+    (rows, n), k = dy.shape, x.shape[1]
+    if x.shape[0] != rows:
+        raise ValueError(f"dy has {rows} rows, x {x.shape[0]}")
+    if accumulate and out is None:
+        raise ValueError("accumulate adds to `out`: pass it")
+    out = _result(out, (groups, n, k), out_dtype or (dy.dtype if out is None else out.dtype), dy)
+    dev = dy.device
+    _check(lib().ew_grouped_mm_dw(dev.index, _dtype(dy.dtype), _dtype(out.dtype), dy.data_ptr(), _stride(dy, 0), x.data_ptr(),
+                                  _stride(x, 0), offsets.data_ptr(), rows, groups, n, k, int(accumulate), out.data_ptr(),
+                                  _stride(out, 1), _stride(out, 0), _stream_of(dev)), "ew_grouped_mm_dw")
+    return out
+
+
+def last_operator_error(device: int = 0) -> int:
+    """Read and clear the stand-alone operators' error word of a device (a status code; waits for the device)."""
+    code = C.c_int32(0)
+    _check(lib().ew_last_operator_error(int(device), C.byref(code)), "ew_last_operator_error")
+    return code.value
 
 
 def load_model(pool: Pool, cfg, bank=None, layers=None, adapters=None, tuned=None):

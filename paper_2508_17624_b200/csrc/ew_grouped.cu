@@ -1,0 +1,615 @@
+// Matrix products grouped by expert, with ragged groups of rows, and their two gradients (tcgen05 + TMEM + TMA).
+//
+//   EW product     y [r, n] = sum_k x[r, k] w[g, n, k]          for the rows r of group g: offsets[g] <= r < offsets[g+1]
+//   input gradient dx[r, k] = sum_n dy[r, n] w[g, n, k]
+//   weight gradient dw[g, n, k] (+)= sum_{r in g} dy[r, n] x[r, k]
+//
+// One kernel for the three.  In all of them the output is row-major with a contiguous axis f (n, k, k), and
+//   D[f, c] = sum_t A[f, t] B[c, t],   out[row(c), f] = D[f, c]:
+//
+//               f   c            t (summed)   A                              B
+//   product     n   rows of x    k            w[g]  (t contiguous)           x  (t contiguous)
+//   dx          k   rows of dy   n            w[g]  (f contiguous)           dy (t contiguous)
+//   dw          k   n            rows of g    x     (f contiguous)           dy (c contiguous)
+//
+// f is the MMA's M axis (TMEM lanes), so a warp of the epilogue holds 32 neighbouring f of one output row and its store
+// instructions write whole sectors, whatever the group's length; c is the MMA's N axis, which an instruction can choose
+// in steps of 16: a group of few rows costs few tensor-core cycles and the kernel is then a stream of its weights.  The
+// operand whose summed axis is contiguous is staged K-major, the other MN-major: the tensor core transposes, nothing is
+// moved for it.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ew_ops.h"
+#include "ew_tc.cuh"
+
+namespace ew {
+namespace ops {
+namespace {
+using namespace tc;
+
+enum Way { kProduct = 0, kInputGrad = 1, kWeightGrad = 2 };
+
+constexpr int kThreads = 224;                          // TMA, MMA, four epilogue warps, relay (weight gradient)
+constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one stage
+constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
+constexpr int kSmemLimit = 227 * 1024;
+constexpr int kMaxStages = 12;
+
+struct Args {
+    const int32_t *offsets;
+    void *out;
+    int *err;
+    long long ldo;          // elements between output rows
+    long long group_out;    // dw: elements between groups
+    int rows, groups;
+    int f_size;             // length of the output's contiguous axis
+    int c_size;             // dw: n
+    int t_size;             // product, dx: length of the summed axis
+    int f_tiles, c_tiles;
+    int out_kind;           // ew_dtype_t
+    int accumulate;
+    int fp16;               // operand type
+    int stages;
+    int table_bytes;
+};
+
+// CG: CTAs that share one MMA tile (1, or 2 = a pair with 256 f); NT: columns of an accumulator set
+template <int CG, int NT>
+struct Cfg {
+    static constexpr int kBRows = NT / CG;                                   // c staged by each CTA
+    static constexpr int kStageBytes = kATile + kBRows * kBlockK * 2;
+    static constexpr int kTile = 128 * CG;                                   // f of an item
+    static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+    static constexpr int kStep = 16 * CG;                                    // granularity of an MMA's N
+};
+
+struct Item {
+    int g, f0, row0, cols, kb, tail;      // cols: output rows (c) of this item; kb: k-blocks; tail: live rows of the last one (dw)
+};
+
+__device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) { return smem_desc_sw128(addr); }
+// MN-major operand, 128-byte swizzle: blocks of 64 MN-elements x 64 summed rows of 128 bytes (one TMA box, 8 KiB); the
+// next 64 MN-elements lie 8 KiB further on (leading offset), the next eight summed rows 1 KiB (stride offset).
+__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3FFFF) >> 4);
+    d |= (uint64_t)(8192 >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+__device__ __forceinline__ bool try_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// bounded wait on a barrier that may receive arrivals from the peer CTA
+template <int CG>
+__device__ __forceinline__ bool wait_any(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    if constexpr (CG == 1) return mbar_wait(bar, parity, abort_flag, err);
+    if (try_cluster(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t it = 1;; ++it) {
+        if (try_cluster(bar, parity)) return true;
+        if ((it & 63u) == 0) {
+            if (*abort_flag) return false;
+            if (clock64() - t0 > kWaitLimitCycles) {
+                *abort_flag = 1;
+                atomicOr(err, 2);
+                return false;
+            }
+        }
+    }
+}
+
+template <int CG>
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1) tma_load_2d(dst, m, x, y, bar);
+    else tma2_load_2d(dst, m, x, y, bar);
+}
+template <int CG>
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, uint32_t bar) {
+    if constexpr (CG == 1) tma_load_3d(dst, m, x, y, z, bar);
+    else tma2_load_3d(dst, m, x, y, z, bar);
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    if constexpr (CG == 1) tc_mma(d, a, b, idesc, acc);
+    else tc2_mma(d, a, b, idesc, acc);
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (CG == 1) tc_commit(bar);
+    else tc2_commit_both(bar);
+}
+template <int CG>
+__device__ __forceinline__ void arrive_leader(uint32_t bar) {
+    if constexpr (CG == 1) mbar_arrive(bar);
+    else mbar_arrive_leader(bar);
+}
+
+// One column of the accumulator (32 neighbouring f of one output row, one per lane) into the output row.
+__device__ __forceinline__ void put(void *out, size_t at, float v, int kind, int accumulate) {
+    if (kind == EW_FP32) {
+        float *p = reinterpret_cast<float *>(out) + at;
+        *p = accumulate ? *p + v : v;
+    } else if (kind == EW_BF16) {
+        __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(out) + at;
+        *p = __float2bfloat16_rn(accumulate ? __bfloat162float(*p) + v : v);
+    } else {
+        __half *p = reinterpret_cast<__half *>(out) + at;
+        *p = __float2half_rn(accumulate ? __half2float(*p) + v : v);
+    }
+}
+
+template <int CG, int NT, int WAY>
+__global__ void __launch_bounds__(kThreads, 1)
+grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                       const __grid_constant__ CUtensorMap map_b_big, const __grid_constant__ Args a) {
+    using C = Cfg<CG, NT>;
+    constexpr bool DW = WAY == kWeightGrad;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
+    // after the ring: barriers full, ready, empty [kMaxStages] each, tmem full [2], tmem empty [2], TMEM base, abort
+    // flag; then the group table: first block of each group, first row, rows
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem_al + a.stages * C::kStageBytes);
+    const uint32_t bar_full = smem_u32(bars), bar_ready = bar_full + 8 * kMaxStages, bar_empty = bar_ready + 8 * kMaxStages;
+    const uint32_t bar_tfull = bar_empty + 8 * kMaxStages, bar_tempty = bar_tfull + 16;
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 3 * kMaxStages + 4);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    int *t_pre = reinterpret_cast<int *>(bars + 3 * kMaxStages + 6), *t_lo = t_pre + a.groups + 1, *t_cnt = t_lo + a.groups;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
+    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_ready + 8 * s, CG);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_tfull + 8 * i, 1);
+            mbar_init(bar_tempty + 8 * i, 4 * CG);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 1) {
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                         "r"((uint32_t)C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                         "r"((uint32_t)C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    pdl_launch_dependents();
+    pdl_wait();                                        // the operands and the offsets may come from the kernel before
+    if (warp == 0) {
+        // group table: first row and rows of each group, and the number of row blocks before it.  Offsets are clamped to
+        // the matrix and to the largest one before them, so that whatever the call was given the groups lie inside the
+        // matrix and apart from one another.
+        int before = 0, raw = *(const volatile int32_t *)a.offsets, end = min(max(raw, 0), a.rows);
+        bool bad = raw != end;
+        for (int g0 = 0; g0 < a.groups; g0 += 32) {
+            const int g = g0 + lane;
+            int hi = end;
+            if (g < a.groups) {
+                raw = *(const volatile int32_t *)(a.offsets + g + 1);
+                hi = min(max(raw, 0), a.rows);
+            }
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, hi, d);
+                if (lane >= d) hi = max(hi, v);
+            }
+            hi = max(hi, end);
+            int lo = __shfl_up_sync(0xffffffffu, hi, 1);
+            if (lane == 0) lo = end;
+            const int nb = g >= a.groups ? 0 : DW ? a.c_tiles : (hi - lo + NT - 1) / NT;
+            int inc = nb;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, inc, d);
+                if (lane >= d) inc += v;
+            }
+            if (g < a.groups) {
+                bad |= raw != hi;
+                t_lo[g] = lo;
+                t_cnt[g] = hi - lo;
+                t_pre[g] = before + inc - nb;
+            }
+            before += __shfl_sync(0xffffffffu, inc, 31);
+            end = __shfl_sync(0xffffffffu, hi, 31);
+        }
+        if (lane == 0) t_pre[a.groups] = before;
+        if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadIndex);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+    const int n_items = t_pre[a.groups] * a.f_tiles;
+    const int t_blocks = (a.t_size + kBlockK - 1) / kBlockK;
+
+    auto item_at = [&](int i) -> Item {
+        Item it;
+        const int block = i / a.f_tiles;
+        it.f0 = (i - block * a.f_tiles) * C::kTile;
+        int lo = 0, hi = a.groups;                     // the last group whose first block is <= block
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (t_pre[mid] <= block) lo = mid; else hi = mid;
+        }
+        it.g = lo;
+        const int b = block - t_pre[lo], cnt = t_cnt[lo];
+        if (DW) {
+            it.row0 = b * NT;                          // first n of the tile
+            it.cols = min(NT, a.c_size - it.row0);
+            it.kb = (cnt + kBlockK - 1) / kBlockK;
+            it.tail = cnt - (it.kb - 1) * kBlockK;
+        } else {
+            // the group's rows in equal blocks (multiples of the MMA's step): 257 rows make 144 + 113, not 256 + 1
+            const int nb = t_pre[lo + 1] - t_pre[lo];
+            const int size = ((cnt + nb - 1) / nb + C::kStep - 1) / C::kStep * C::kStep;
+            it.row0 = t_lo[lo] + b * size;
+            it.cols = min(size, cnt - b * size);
+            it.kb = t_blocks;
+            it.tail = kBlockK;
+        }
+        return it;
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            for (int i = unit; i < n_items && ok; i += units) {
+                const Item it = item_at(i);
+                const int n = (it.cols + C::kStep - 1) / C::kStep * C::kStep;
+                const int n_cta = n / CG;                                    // c of this item that each CTA stages
+                const int f = it.f0 + (int)rank * 128;
+                const int c = it.row0 + (DW ? (int)rank * (NT / CG) : (int)rank * n_cta);
+                const bool big = !DW && n_cta > 64 && C::kBRows >= 128;
+                const int boxes = DW ? (NT / CG) / 64 : (n_cta + kChunkRows - 1) / kChunkRows;
+                const uint32_t b_bytes = DW ? (uint32_t)(NT / CG) * kBlockK * 2 : big ? 128 * kBlockK * 2 : boxes * kChunkBytes;
+                const int first = DW ? t_lo[it.g] : 0;
+                for (int kb = 0; kb < it.kb; ++kb) {
+                    if (!(ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1, abort_flag, a.err))) break;
+                    const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
+                    // the weight gradient's copies are counted on each CTA's own barrier (its relay warp reads them), the
+                    // others' on the leader's
+                    const uint32_t bar = (CG == 2 && !DW) ? leader_addr(bar_full + 8 * stage) : bar_full + 8 * stage;
+                    if (DW || rank == 0) mbar_expect_tx(bar_full + 8 * stage, DW ? kATile + b_bytes : CG * (kATile + b_bytes));
+                    const int t = first + kb * kBlockK;
+                    if (WAY == kProduct) {
+                        load_3d<CG>(sa, &map_a, t, f, it.g, bar);
+                    } else if (WAY == kInputGrad) {
+                        load_3d<CG>(sa, &map_a, f, t, it.g, bar);
+                        load_3d<CG>(sa + 8192, &map_a, f + 64, t, it.g, bar);
+                    } else {
+                        tma_load_2d(sa, &map_a, f, t, bar);
+                        tma_load_2d(sa + 8192, &map_a, f + 64, t, bar);
+                    }
+                    if (DW) {
+                        for (int j = 0; j < boxes; ++j) tma_load_2d(sb + j * 8192, &map_b, c + j * 64, t, bar);
+                    } else if (big) {
+                        load_2d<CG>(sb, &map_b_big, t, c, bar);
+                    } else {
+                        for (int j = 0; j < boxes; ++j) load_2d<CG>(sb + j * kChunkBytes, &map_b, t, c + j * kChunkRows, bar);
+                    }
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (the leader CTA's)
+        if (lane == 0 && rank == 0) {
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            const uint32_t type = a.fp16 ? 0u : (1u << 7) | (1u << 10);
+            const uint32_t base = (1u << 4) | type | (WAY != kProduct ? 1u << 15 : 0u) | (DW ? 1u << 16 : 0u) |
+                                  ((uint32_t)(C::kTile >> 4) << 24);
+            const uint32_t bar_in = DW ? bar_ready : bar_full;
+            bool ok = true;
+            for (int i = unit; i < n_items && ok; i += units) {
+                const Item it = item_at(i);
+                if (DW && it.kb == 0) continue;                              // an empty group: the epilogue writes its zeros
+                const int n = DW ? NT : (it.cols + C::kStep - 1) / C::kStep * C::kStep;
+                const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
+                if (!(ok = wait_any<CG>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
+                tc_fence_after();
+                const uint32_t d = tmem_base + acc * NT;
+                for (int kb = 0; kb < it.kb; ++kb) {
+                    if (!(ok = wait_any<CG>(bar_in + 8 * stage, phase, abort_flag, a.err))) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
+                    const uint64_t da = WAY == kProduct ? desc_kmajor(sa) : desc_mnmajor(sa);
+                    const uint64_t db = DW ? desc_mnmajor(sb) : desc_kmajor(sb);
+                    // 16 summed elements a step: 32 bytes further along a K-major row, two groups of eight 128-byte rows
+                    // (2 KiB) further in an MN-major tile; descriptors count 16 bytes
+                    constexpr int kStepA = WAY == kProduct ? 2 : 128, kStepB = DW ? 128 : 2;
+                    const int steps = DW && kb == it.kb - 1 ? (it.tail + 15) >> 4 : kBlockK / 16;
+#pragma unroll
+                    for (int ki = 0; ki < kBlockK / 16; ++ki)
+                        if (!DW || ki < steps) mma<CG>(d, da + kStepA * ki, db + kStepB * ki, idesc, (kb | ki) ? 1u : 0u);
+                    commit<CG>(bar_empty + 8 * stage);
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                }
+                if (!ok) break;
+                commit<CG>(bar_tfull + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            }
+        }
+    } else if (warp == 6) {
+        // ------------------------------------------------------------------ relay (weight gradient, both CTAs)
+        // The last k-block of a group ends inside a tile, and the rows behind it are the next group's: up to the end of
+        // the MMA step both operands are set to zero (both: a NaN there would survive a zero on the other side).
+        if (DW) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            for (int i = unit; i < n_items && ok; i += units) {
+                const Item it = item_at(i);
+                for (int kb = 0; kb < it.kb; ++kb) {
+                    if (!(ok = mbar_wait_warp(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
+                    if (kb == it.kb - 1 && (it.tail & 15)) {
+                        const int from = it.tail * 128, to = ((it.tail + 15) & ~15) * 128;
+                        uint8_t *tile = smem_al + stage * C::kStageBytes;
+                        for (int box = 0; box < C::kStageBytes / 8192; ++box)
+                            for (int o = from + lane * 16; o < to; o += 512)
+                                *reinterpret_cast<uint4 *>(tile + box * 8192 + o) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (lane == 0) arrive_leader<CG>(bar_ready + 8 * stage);
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue (warps 2..5 of each CTA)
+        const int lg = warp & 3;                                             // the TMEM lanes this warp may read
+        uint32_t acc = 0, acc_phase = 0;
+        bool ok = true;
+        for (int i = unit; i < n_items && ok; i += units) {
+            const Item it = item_at(i);
+            const int f = it.f0 + (int)rank * 128 + lg * 32 + lane;
+            const bool f_ok = f < a.f_size;
+            const size_t at = (DW ? (size_t)it.g * a.group_out : 0) + (size_t)it.row0 * a.ldo + f;
+            if (DW && it.kb == 0) {
+                if (f_ok && !a.accumulate)
+                    for (int j = 0; j < it.cols; ++j) put(a.out, at + (size_t)j * a.ldo, 0.f, a.out_kind, 0);
+                continue;
+            }
+            if (!(ok = mbar_wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
+            tc_fence_after();
+            const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
+#pragma unroll 1
+            for (int c0 = 0; c0 < it.cols; c0 += 32) {
+                uint32_t v[32];
+                tc_ld32(t0 + c0, v);                   // columns behind the item's last are in the accumulator set, not stored
+                tc_wait_ld();
+                const int lim = min(32, it.cols - c0);
+                if (f_ok) {
+                    if (a.out_kind == EW_FP32 && !a.accumulate) {
+                        float *p = reinterpret_cast<float *>(a.out) + at + (size_t)c0 * a.ldo;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < lim) p[(size_t)j * a.ldo] = __uint_as_float(v[j]);
+                    } else if (a.out_kind == EW_BF16 && !a.accumulate) {
+                        __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(a.out) + at + (size_t)c0 * a.ldo;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < lim) p[(size_t)j * a.ldo] = __float2bfloat16_rn(__uint_as_float(v[j]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < lim) put(a.out, at + (size_t)(c0 + j) * a.ldo, __uint_as_float(v[j]), a.out_kind, a.accumulate);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_leader<CG>(bar_tempty + 8 * acc);
+            if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+        }
+    }
+
+    // ---------------------------------------------------------------------- teardown
+    if (*abort_flag) {                                 // let copies in flight land before the CTA's memory is reused
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000ll) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();
+    tc_fence_after();
+    if (warp == 1) {
+        if constexpr (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+    }
+}
+
+constexpr int kBarBytes = (3 * kMaxStages + 6) * 8;
+
+template <int CG, int NT, int WAY>
+ew_status_t launch(const Device &d, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mbb, Args a, long long max_items,
+                   cudaStream_t st) {
+    using C = Cfg<CG, NT>;
+    if (max_items > 0x7fffffff) return refuse("grouped product: too many output tiles");
+    a.table_bytes = (3 * a.groups + 1) * 4;
+    const int room = kSmemLimit - 1024 - kBarBytes - a.table_bytes;
+    a.stages = room / C::kStageBytes < kMaxStages ? room / C::kStageBytes : kMaxStages;
+    cudaLaunchConfig_t cfg = {};
+    const long long units = d.sm_count / CG;
+    cfg.gridDim = dim3((unsigned)(CG * (max_items < units ? max_items : units)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)a.stages * C::kStageBytes + 1024 + kBarBytes + a.table_bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, WAY>, ma, mb, mbb, a), "grouped product");
+}
+
+template <int CG, int NT, int WAY>
+int setup_one() {
+    return (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+}
+
+// A row-major matrix's row stride: multiples of eight elements keep every TMA copy on a 16-byte boundary.
+bool bad_matrix(const void *p, long long ld, long long width) {
+    return !p || ((uintptr_t)p & 15) || ld < width || (ld & 7) || ld >= (1ll << 38);
+}
+
+ew_status_t check_common(int32_t dtype, int32_t out_dtype, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k,
+                         const void *out) {
+    if (!is_16bit(dtype) || (out_dtype != dtype && out_dtype != EW_FP32)) return refuse("grouped product: operands are bf16 or fp16, results of the same type or fp32");
+    if (rows < 0 || groups < 1 || groups > kMaxGroups || n < 1 || k < 1) return refuse("grouped product: size out of range");
+    if (!offsets || ((uintptr_t)offsets & 3) || !out || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)))
+        return refuse("grouped product: null or misaligned pointer");
+    return EW_OK;
+}
+
+ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *w,
+                         int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k,
+                         void *out, int64_t ldo, void *stream) {
+    const int t = grad ? n : k, f = grad ? k : n;
+    // (a tensor without rows may have no address)
+    ew_status_t s = check_common(dtype, out_dtype, offsets, rows, groups, n, k, rows == 0 ? w : out);
+    if (s != EW_OK) return s;
+    if ((rows > 0 && bad_matrix(x, ldx, t)) || bad_matrix(w, ldw, k) || ldo < f || (groups > 1 && (group_stride < (int64_t)(n - 1) * ldw + k || (group_stride & 7) || group_stride >= (1ll << 38))))
+        return refuse("grouped product: operands need 16-byte aligned rows (strides in multiples of eight elements) that do not overlap");
+    if (device < 0) return EW_ERR_NO_DEVICE;
+    if (rows == 0) return EW_OK;
+    DeviceGuard guard;
+    if ((s = launched((int)guard.enter(device), "cudaSetDevice")) != EW_OK) return s;
+    const Device *d;
+    if ((s = device_state(device, &d)) != EW_OK) return s;
+    CUtensorMap ma, mb, mbb;
+    const uint64_t wd[3] = {(uint64_t)k, (uint64_t)n, (uint64_t)groups};
+    const uint64_t ws[2] = {(uint64_t)ldw * 2, groups > 1 ? (uint64_t)group_stride * 2 : (uint64_t)ldw * 2};
+    const uint32_t wbox[3] = {64, grad ? 64u : 128u, 1};
+    const uint64_t xd[2] = {(uint64_t)t, (uint64_t)rows}, xs[1] = {(uint64_t)ldx * 2};
+    const uint32_t xbox[2] = {64, kChunkRows}, xbig[2] = {64, 128};
+    if ((s = encode_map(*d, &ma, map_type(dtype), w, 3, wd, ws, wbox, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    if ((s = encode_map(*d, &mb, map_type(dtype), x, 2, xd, xs, xbox, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    if ((s = encode_map(*d, &mbb, map_type(dtype), x, 2, xd, xs, xbig, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    Args a = {};
+    a.offsets = offsets;
+    a.out = out;
+    a.err = d->err;
+    a.ldo = ldo;
+    a.rows = rows;
+    a.groups = groups;
+    a.f_size = f;
+    a.t_size = t;
+    a.out_kind = out_dtype;
+    a.fp16 = dtype == EW_FP16;
+    cudaStream_t st = (cudaStream_t)stream;
+    const long long live = groups < rows ? groups : rows;                    // groups that can have rows
+#define EW_LAUNCH(CG, NT)                                                                                                     \
+    do {                                                                                                                      \
+        a.f_tiles = (f + 128 * CG - 1) / (128 * CG);                                                                          \
+        const long long items = (live + rows / NT) * a.f_tiles;                                                               \
+        return grad ? launch<CG, NT, kInputGrad>(*d, ma, mb, mbb, a, items, st) : launch<CG, NT, kProduct>(*d, ma, mb, mbb, a, items, st); \
+    } while (0)
+    if (rows <= 32ll * groups) EW_LAUNCH(1, 64);
+    if (rows <= 96ll * groups) EW_LAUNCH(1, 128);
+    EW_LAUNCH(2, 256);
+#undef EW_LAUNCH
+}
+
+}  // namespace
+
+int grouped_setup() {
+    return setup_one<1, 64, kProduct>() | setup_one<1, 64, kInputGrad>() | setup_one<1, 128, kProduct>() | setup_one<1, 128, kInputGrad>() |
+           setup_one<2, 256, kProduct>() | setup_one<2, 256, kInputGrad>() | setup_one<2, 256, kWeightGrad>();
+}
+
+}  // namespace ops
+}  // namespace ew
+
+using namespace ew;
+using namespace ew::ops;
+
+extern "C" ew_status_t ew_grouped_mm(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *w,
+                                     int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n,
+                                     int32_t k, void *y, int64_t ldy, void *cuda_stream) {
+    return rows_product(false, device, dtype, out_dtype, x, ldx, w, ldw, group_stride, offsets, rows, groups, n, k, y, ldy, cuda_stream);
+}
+
+extern "C" ew_status_t ew_grouped_mm_dx(int32_t device, int32_t dtype, int32_t out_dtype, const void *dy, int64_t lddy, const void *w,
+                                        int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n,
+                                        int32_t k, void *dx, int64_t lddx, void *cuda_stream) {
+    return rows_product(true, device, dtype, out_dtype, dy, lddy, w, ldw, group_stride, offsets, rows, groups, n, k, dx, lddx, cuda_stream);
+}
+
+extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, const void *dy, int64_t lddy, const void *x,
+                                        int64_t ldx, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k,
+                                        int32_t accumulate, void *dw, int64_t lddw, int64_t group_stride, void *cuda_stream) {
+    ew_status_t s = check_common(dtype, out_dtype, offsets, rows, groups, n, k, dw);
+    if (s != EW_OK) return s;
+    if (lddw < k || (groups > 1 && group_stride < (int64_t)(n - 1) * lddw + k))
+        return refuse("grouped product: the weight gradient's rows overlap");
+    if (rows > 0 && (bad_matrix(dy, lddy, n) || bad_matrix(x, ldx, k)))
+        return refuse("grouped product: operands need 16-byte aligned rows (strides in multiples of eight elements) that do not overlap");
+    if (device < 0) return EW_ERR_NO_DEVICE;
+    DeviceGuard guard;
+    if ((s = launched((int)guard.enter(device), "cudaSetDevice")) != EW_OK) return s;
+    const Device *d;
+    if ((s = device_state(device, &d)) != EW_OK) return s;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (rows == 0) {                                                         // no row: every group's gradient is zero
+        if (accumulate) return EW_OK;
+        const size_t e = elem_bytes(out_dtype);
+        for (int g = 0; g < groups; ++g)
+            if ((s = launched((int)cudaMemset2DAsync((uint8_t *)dw + (size_t)g * group_stride * e, lddw * e, 0, k * e, n, st), "cudaMemset2DAsync")) != EW_OK)
+                return s;
+        return EW_OK;
+    }
+    CUtensorMap ma, mb;
+    const uint64_t xd[2] = {(uint64_t)k, (uint64_t)rows}, xs[1] = {(uint64_t)ldx * 2};
+    const uint64_t yd[2] = {(uint64_t)n, (uint64_t)rows}, ys[1] = {(uint64_t)lddy * 2};
+    const uint32_t box[2] = {64, 64};
+    if ((s = encode_map(*d, &ma, map_type(dtype), x, 2, xd, xs, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    if ((s = encode_map(*d, &mb, map_type(dtype), dy, 2, yd, ys, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    Args a = {};
+    a.offsets = offsets;
+    a.out = dw;
+    a.err = d->err;
+    a.ldo = lddw;
+    a.group_out = group_stride;
+    a.rows = rows;
+    a.groups = groups;
+    a.f_size = k;
+    a.c_size = n;
+    a.f_tiles = (k + 255) / 256;
+    a.c_tiles = (n + 255) / 256;
+    a.out_kind = out_dtype;
+    a.accumulate = accumulate != 0;
+    a.fp16 = dtype == EW_FP16;
+    return launch<2, 256, kWeightGrad>(*d, ma, mb, mb, a, (long long)groups * a.c_tiles * a.f_tiles, st);
+}

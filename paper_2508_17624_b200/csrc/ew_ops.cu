@@ -1,0 +1,62 @@
+// What the stand-alone operators keep per device: its size, the tensor-map encoder and one error word.
+#include "ew_ops.h"
+
+#include <mutex>
+
+namespace ew {
+namespace ops {
+namespace {
+
+constexpr int kMaxDevices = 64;
+__device__ int g_operator_error;
+
+std::mutex g_mutex;
+Device g_devices[kMaxDevices];
+bool g_ready[kMaxDevices];
+
+ew_status_t resolve(Device *d, int device) {
+    void *fn = nullptr, *err = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+    if (e == cudaSuccess && !fn) e = cudaErrorUnknown;
+    if (e == cudaSuccess) e = cudaGetSymbolAddress(&err, g_operator_error);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d->sm_count, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return launched((int)e, "operator set-up");
+    d->encode = reinterpret_cast<EncodeTiled>(fn);
+    d->err = static_cast<int *>(err);
+    return launched(grouped_setup(), "operator set-up (grouped products)");
+}
+
+}  // namespace
+
+ew_status_t device_state(int device, const Device **out) {
+    if (device >= kMaxDevices) return refuse("device ordinal out of range");
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (!g_ready[device]) {
+        const ew_status_t s = resolve(&g_devices[device], device);
+        if (s != EW_OK) return s;
+        g_ready[device] = true;
+    }
+    *out = &g_devices[device];
+    return EW_OK;
+}
+
+}  // namespace ops
+}  // namespace ew
+
+using namespace ew;
+
+extern "C" ew_status_t ew_last_operator_error(int32_t device, int32_t *code) {
+    if (!code) return EW_ERR_INVALID_ARG;
+    if (device < 0) return EW_ERR_NO_DEVICE;
+    DeviceGuard guard;
+    ew_status_t s = ops::launched((int)guard.enter(device), "cudaSetDevice");
+    const ops::Device *d = nullptr;
+    if (s == EW_OK) s = ops::device_state(device, &d);
+    if (s == EW_OK) s = ops::launched((int)cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+    int32_t v = 0;
+    if (s == EW_OK) s = ops::launched((int)cudaMemcpy(&v, d->err, 4, cudaMemcpyDeviceToHost), "cudaMemcpy");
+    if (s == EW_OK && v) s = ops::launched((int)cudaMemset(d->err, 0, 4), "cudaMemset");
+    if (s == EW_OK) *code = (v & 2) ? EW_ERR_TIMEOUT : (v & ops::kErrBadIndex) ? EW_ERR_INVALID_ARG : EW_OK;
+    return s;
+}
