@@ -353,6 +353,42 @@ ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, c
                              int32_t k, int32_t accumulate, void *dw, int64_t lddw, int64_t group_stride,
                              void *cuda_stream);
 
+/* Products of a batch's (token, expert) pairs with 4-bit expert weights (decode: the layer is a stream of weights, and
+ * these are a quarter of the bytes):
+ *     y[p, :] = x[p / pairs_per_row, :] W[slots[p]]^T,    W[s, n, k] = (q[s, n, k] - 8) scales[s, k / group, n]
+ * accumulated in fp32 and rounded once.  slots: int32 [pairs], as ew_reroute, ew_route_logits and ew_route_noalloc write
+ * them for k pairs a token (pairs_per_row = k for the projections that read the token's row, 1 for the one that reads a
+ * pair's own).  A negative slot has no expert: its row of y is zero.  A slot >= n_slots gives a row of zeros too and is
+ * reported as EW_ERR_INVALID_ARG.  slots = null: one matrix (n_slots = 1) for every pair.
+ *   q       uint8 [n_slots, n, k/2]: every eight weights of a row are one little-endian 32-bit word whose bits 4i..4i+3 hold
+ *           the weight 2i and bits 16+4i..16+4i+3 the weight 2i + 1, i = 0..3
+ *   scales  of x's type [n_slots, k/group, n];  group 32, 64 or 128, a divisor of k;  n a multiple of 8
+ *   x       [pairs / pairs_per_row, k];  x, q and scales 16-byte aligned, ldx a multiple of 8;  y [pairs, n]
+ * Every pair count is taken; beyond some 32 rows a slot the 16-bit weights' ew_grouped_mm is the better call.
+ * n_slots <= 2048.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
+ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *q,
+                        const void *scales, const int32_t *slots, int32_t pairs, int32_t pairs_per_row, int32_t n_slots,
+                        int32_t n, int32_t k, int32_t group, void *y, int64_t ldy, void *cuda_stream);
+
+/* Packs 16-bit weights w [n_slots, n, k] (slot_stride elements between matrices) into q and scales of the form above:
+ * scale = max |w| / 7 of the group, rounded to w's type, and q = 8 + the nearest whole number to w / scale (ties to even).
+ * Weights are finite.  */
+ew_status_t ew_quant_pack(int32_t device, int32_t dtype, const void *w, int64_t ldw, int64_t slot_stride, int32_t n_slots,
+                          int32_t n, int32_t k, int32_t group, void *q, void *scales, void *cuda_stream);
+
+/* SwiGLU between an expert's two linears (Section 2.1's expert FFN), with the routing weight of a row folded in:
+ *     act[r, i] = row_weights[r] * silu(h[r, i]) * h[r, inter + i]     h [rows, 2 inter]: gate block, then up block
+ * computed in fp32, rounded once.  row_weights: fp32 [rows], or null for 1.  h and act: dtype EW_BF16 or EW_FP16; any
+ * alignment is taken, rows on 16-byte boundaries are fastest. */
+ew_status_t ew_swiglu(int32_t device, int32_t dtype, const void *h, int64_t ldh, const float *row_weights, int32_t rows,
+                      int32_t inter, void *act, int64_t ldact, void *cuda_stream);
+
+/* Its gradient: dh [rows, 2 inter] from dact [rows, inter] and h, and drow_weights fp32 [rows] (null: not wanted; needs
+ * row_weights). */
+ew_status_t ew_swiglu_grad(int32_t device, int32_t dtype, const void *dact, int64_t lddact, const void *h, int64_t ldh,
+                           const float *row_weights, int32_t rows, int32_t inter, void *dh, int64_t lddh,
+                           float *drow_weights, void *cuda_stream);
+
 /* Read and clear the operators' error word of a device (waits for all work on it).  *code receives EW_OK,
  * EW_ERR_INVALID_ARG (an index in device memory was outside its range) or EW_ERR_TIMEOUT (a bounded wait expired). */
 ew_status_t ew_last_operator_error(int32_t device, int32_t *code);

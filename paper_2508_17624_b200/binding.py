@@ -24,7 +24,7 @@ EXPORTS = ["ew_pool_create", "ew_pool_destroy", "ew_load_base", "ew_load_adapter
            "ew_pool_trim", "ew_moe_forward", "ew_moe_forward_debug", "ew_moe_forward_host", "ew_profile_enable",
            "ew_profile_read", "ew_reroute", "ew_reroute_unfused", "ew_route_logits", "ew_route_noalloc", "ew_selftest_bounded_wait", "ew_get_expert_map",
            "ew_moe_forward_partial", "ew_ep_finish", "ew_moe_forward_scatter", "ew_ep_finish_gathered", "ew_pool_stats", "ew_last_device_error", "ew_slot_address", "ew_grouped_mm", "ew_grouped_mm_dx", "ew_grouped_mm_dw",
-           "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
+           "ew_quant_mv", "ew_quant_pack", "ew_swiglu", "ew_swiglu_grad", "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
 
 
 class EwConfig(C.Structure):
@@ -73,6 +73,10 @@ def lib():
         for name in ("ew_grouped_mm", "ew_grouped_mm_dx"):
             getattr(_lib, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, i64, ptr, i32, i32, i32, i32, ptr, i64, ptr]
         _lib.ew_grouped_mm_dw.argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, i64, i64, ptr]
+        _lib.ew_quant_mv.argtypes = [i32, i32, i32, ptr, i64, ptr, ptr, ptr, i32, i32, i32, i32, i32, i32, ptr, i64, ptr]
+        _lib.ew_quant_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, i32, ptr, ptr, ptr]
+        _lib.ew_swiglu.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr]
+        _lib.ew_swiglu_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, ptr, i64, ptr, ptr]
     return _lib
 
 
@@ -328,6 +332,11 @@ def _stride(t, dim) -> int:
     return (n + 7) // 8 * 8
 
 
+def _width(t) -> int:
+    """Elements between the rows of a matrix (its width where it has one row only)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 def _offsets(offsets, like):
     _on(offsets, like, 1, "offsets")
     if str(offsets.dtype) != "torch.int32" or offsets.shape[0] < 2 or offsets.stride(0) != 1:
@@ -395,6 +404,92 @@ def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
                                   _stride(x, 0), offsets.data_ptr(), rows, groups, n, k, int(accumulate), out.data_ptr(),
                                   _stride(out, 1), _stride(out, 0), _stream_of(dev)), "ew_grouped_mm_dw")
     return out
+
+
+def quant_pack(w, group, out=None):
+    """4-bit weights and group scales of w [slots, n, k] (bf16 or fp16) for `quant_mv`: (q uint8 [slots, n, k/2], scales
+    [slots, k/group, n] of w's type).  The header has the format."""
+    import torch
+    _on(w, ndim=3, name="w")
+    slots, n, k = w.shape
+    if group not in (32, 64, 128) or k % group:
+        raise ValueError(f"groups of 32, 64 or 128 weights that divide k = {k} are wanted, got {group}")
+    q, scales = out or (None, None)
+    q = _result(q, (slots, n, k // 2), torch.uint8, w, "q")
+    scales = _result(scales, (slots, k // group, n), w.dtype, w, "scales")
+    if not (q.is_contiguous() and scales.is_contiguous()):
+        raise ValueError("q and scales are contiguous")
+    dev = w.device
+    _check(lib().ew_quant_pack(dev.index, _dtype(w.dtype), w.data_ptr(), _stride(w, 1), _stride(w, 0), slots, n, k, group,
+                               q.data_ptr(), scales.data_ptr(), _stream_of(dev)), "ew_quant_pack")
+    return q, scales
+
+
+def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
+    """y[p] = x[p // per_row] W[slots[p]]^T with the 4-bit weights of `quant_pack`.  x [rows, k]; slots int32, one entry a
+    pair in any shape ([tokens, top_k] as the router writes it), per_row = pairs / rows of x; negative: a row of zeros.
+    slots None: one matrix, a pair a row.  -> [pairs, n]; out_dtype: x's type or float32."""
+    import torch
+    _on(x, name="x")
+    _on(q, x, 3, "q", torch.uint8)
+    _on(scales, x, 3, "scales", x.dtype)
+    (n_slots, n, half), (rows, k), groups = q.shape, x.shape, scales.shape[1]
+    if half * 2 != k or groups < 1 or k % groups or tuple(scales.shape) != (n_slots, groups, n) or not (q.is_contiguous() and scales.is_contiguous()):
+        raise ValueError(f"x {tuple(x.shape)}, q {tuple(q.shape)} and scales {tuple(scales.shape)} do not belong together")
+    pairs = rows
+    if slots is not None:
+        if not slots.is_cuda or slots.device != x.device or slots.dtype != torch.int32 or not slots.is_contiguous():
+            raise ValueError("slots: a contiguous int32 tensor on x's device is wanted")
+        pairs = slots.numel()
+        if pairs and (rows == 0 or pairs % rows):
+            raise ValueError(f"{pairs} pairs for {rows} rows of x")
+    out = _result(out, (pairs, n), out_dtype or (x.dtype if out is None else out.dtype), x)
+    dev = x.device
+    _check(lib().ew_quant_mv(dev.index, _dtype(x.dtype), _dtype(out.dtype), x.data_ptr(), _stride(x, 0), q.data_ptr(), scales.data_ptr(),
+                             None if slots is None else slots.data_ptr(), pairs, max(1, pairs // rows if rows else 1), n_slots, n, k,
+                             k // groups, out.data_ptr(), _stride(out, 0), _stream_of(dev)), "ew_quant_mv")
+    return out
+
+
+def _row_weights(p, h):
+    import torch
+    if p is None:
+        return None
+    _on(p, h, 1, "row_weights", torch.float32)
+    if p.shape[0] != h.shape[0]:
+        raise ValueError(f"{p.shape[0]} row weights for {h.shape[0]} rows")
+    return p.data_ptr()
+
+
+def swiglu(h, row_weights=None, out=None):
+    """row_weights[r] * silu(h[r, :inter]) * h[r, inter:] -> [rows, inter]: the activation between an expert's linears, the
+    routing weights (float32, or None) folded in."""
+    _on(h, name="h")
+    rows, two = h.shape
+    if two < 2 or two % 2:
+        raise ValueError(f"h holds a gate and an up block side by side: an even width is wanted, got {two}")
+    p = _row_weights(row_weights, h)
+    out = _result(out, (rows, two // 2), h.dtype, h)
+    dev = h.device
+    _check(lib().ew_swiglu(dev.index, _dtype(h.dtype), h.data_ptr(), _width(h), p, rows, two // 2, out.data_ptr(), _width(out), _stream_of(dev)), "ew_swiglu")
+    return out
+
+
+def swiglu_grad(dact, h, row_weights=None, out=None):
+    """The gradient of `swiglu`: dh [rows, 2 inter], and with row_weights also theirs, float32 [rows] -> dh or (dh, dp)."""
+    import torch
+    _on(h, name="h")
+    _on(dact, h, 2, "dact", h.dtype)
+    rows, two = h.shape
+    if two < 2 or tuple(dact.shape) != (rows, two // 2) or two % 2:
+        raise ValueError(f"dact {tuple(dact.shape)} does not belong to h {tuple(h.shape)}")
+    p = _row_weights(row_weights, h)
+    out = _result(out, (rows, two), h.dtype, h)
+    dev = h.device
+    dp = None if p is None else torch.empty((rows,), dtype=torch.float32, device=dev)
+    _check(lib().ew_swiglu_grad(dev.index, _dtype(h.dtype), dact.data_ptr(), _width(dact), h.data_ptr(), _width(h), p, rows, two // 2, out.data_ptr(),
+                                _width(out), None if dp is None else dp.data_ptr(), _stream_of(dev)), "ew_swiglu_grad")
+    return out if dp is None else (out, dp)
 
 
 def last_operator_error(device: int = 0) -> int:

@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libexpertweave.so")
-SOURCES = ["ew_vmm.cpp", "ew_pool.cu", "ew_route.cu", "ew_router.cu", "ew_gemm.cu", "ew_ablate.cu", "ew_ops.cu", "ew_grouped.cu"]
+SOURCES = ["ew_vmm.cpp", "ew_pool.cu", "ew_route.cu", "ew_router.cu", "ew_gemm.cu", "ew_ablate.cu", "ew_ops.cu", "ew_grouped.cu", "ew_quant.cu",
+           "ew_swiglu.cu"]
 
 
 def _nvcc() -> str:

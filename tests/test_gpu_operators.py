@@ -109,3 +109,166 @@ def test_no_rows():
     assert not binding.grouped_mm_dw(dy, x, offsets).any()
     kept = torch.ones((3, 16, 24), dtype=FP32, device="cuda")
     assert (binding.grouped_mm_dw(dy, x, offsets, out=kept, accumulate=True) == 1).all()
+
+
+# ------------------------------------------------------------------------------------------ 4-bit weights
+PLACE = [0, 4, 1, 5, 2, 6, 3, 7]                        # nibble of weight 0..7 in its 32-bit word
+
+
+def unpacked(q, scales):
+    """The weights that (q, scales) stand for, in 64 bits."""
+    s, n, half = q.shape
+    words = q.cpu().numpy().view("<u4").astype(np.int64)
+    levels = np.stack([(words >> (4 * p)) & 15 for p in PLACE], axis=-1).reshape(s, n, 2 * half)
+    group = 2 * half // scales.shape[1]
+    return (torch.from_numpy(levels).cuda() - 8).double() * scales.double().transpose(1, 2).repeat_interleave(group, dim=2)
+
+
+def check_quant(slots, n_slots, n, k, group, dtype=BF16, out_dtype=None, per_row=None, seed=0, pad=0):
+    pairs = slots.numel() if slots is not None else per_row
+    rows = pairs // per_row if slots is not None else pairs
+    x = randn((rows, k), dtype, seed + 1, 1.0, pad)
+    q, scales = binding.quant_pack(randn((n_slots, n, k), dtype, seed, 0.05), group)
+    y = binding.quant_mv(x, q, scales, slots, out_dtype=out_dtype)
+    torch.cuda.synchronize()
+    assert y.shape == (pairs, n) and y.dtype == (out_dtype or dtype)
+    w, flat = unpacked(q, scales), [0] * pairs if slots is None else slots.reshape(-1).tolist()
+    step = 1 if slots is None else per_row
+    for s in sorted(set(flat)):
+        at = [i for i, v in enumerate(flat) if v == s]
+        if not 0 <= s < n_slots:
+            assert not y[at].any()
+            continue
+        xd = x[[i // step for i in at]].double()
+        near(y[at], xd @ w[s].t(), xd.abs() @ w[s].abs().t(), 2 * k, ("slot", s))
+
+
+def some_slots(tokens, per, n_slots, seed=0):
+    r = np.random.RandomState(seed)
+    return torch.from_numpy(np.stack([r.choice(n_slots, per, replace=False) for _ in range(tokens)]).astype(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
+@pytest.mark.parametrize("group,k", [(32, 32), (32, 96), (64, 192), (128, 128), (128, 1408), (64, 2048)])
+@pytest.mark.parametrize("n", [8, 24, 264])
+def test_quant_sizes(dtype, group, k, n):
+    check_quant(some_slots(5, 2, 7), 7, n, k, group, dtype, per_row=2)
+    check_quant(None, 1, n, k, group, dtype, FP32, per_row=3, seed=4, pad=8)
+
+
+@pytest.mark.parametrize("tokens,per,n_slots", [(1, 1, 1), (1, 6, 64), (7, 3, 3), (40, 1, 1), (33, 2, 2), (150, 6, 8), (256, 6, 96), (600, 4, 300)])
+@pytest.mark.parametrize("per_row", ["token", "pair"])
+def test_quant_batches(tokens, per, n_slots, per_row):
+    check_quant(some_slots(tokens, per, n_slots, 3), n_slots, 72, 512, 64, BF16, FP32, per_row=per if per_row == "token" else 1, seed=2)
+
+
+def test_quant_pairs_without_a_slot():
+    slots = some_slots(12, 6, 20, 5)
+    slots[3] = -1
+    slots[7, 2:] = -5
+    check_quant(slots, 20, 48, 256, 32, per_row=6)
+    check_quant(torch.full((4, 2), -1, dtype=torch.int32, device="cuda"), 3, 16, 128, 128, per_row=1)
+    assert binding.last_operator_error() == 0
+    slots[0, 0] = 20                                    # beyond the last slot: a row of zeros, reported
+    check_quant(slots, 20, 48, 256, 32, per_row=6)
+    assert binding.last_operator_error() == 1 and binding.last_operator_error() == 0
+
+
+def test_quant_rows_do_not_touch_one_another():
+    slots = torch.tensor([[0, 1], [-1, -1], [1, 0]], dtype=torch.int32, device="cuda")
+    x = randn((3, 256), BF16, 1)
+    q, scales = binding.quant_pack(randn((2, 40, 256), BF16, 2, 0.05), 64)
+    clean = binding.quant_mv(x, q, scales, slots)
+    x[1] = float("nan")
+    out = torch.full((6, 48), 7.0, dtype=BF16, device="cuda")
+    binding.quant_mv(x, q, scales, slots, out=out[:, :40])
+    assert torch.equal(out[:, :40], clean) and (out[:, 40:] == 7).all()
+    x[0] = float("inf")
+    got = binding.quant_mv(x, q, scales, slots)
+    assert not got[:2].isfinite().any() and torch.equal(got[2:], clean[2:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
+@pytest.mark.parametrize("shape,group", [((1, 8, 32), 32), ((3, 40, 192), 64), ((5, 72, 640), 128), ((2, 8, 2048), 32)])
+def test_quant_pack(dtype, shape, group):
+    w = randn(shape, dtype, 8, 0.1, pad=3)
+    w[0, 0, :group] = 0                                 # a group of zeros
+    w[0, 1, 0] = 40.0                                   # a group with an outlier
+    q, scales = binding.quant_pack(w, group)
+    s, n, k = shape
+    most = w.float().view(s, n, k // group, group).abs().amax(-1)
+    assert torch.equal(scales, (most / torch.full_like(most, 7.0)).to(dtype).transpose(1, 2))
+    wide = scales.float().transpose(1, 2).repeat_interleave(group, dim=2)
+    level = torch.where(wide > 0, (w.float() / wide).round().clamp(-8, 7), torch.zeros_like(wide))
+    assert torch.equal(unpacked(q, scales), level.double() * wide.double())
+    assert ((unpacked(q, scales) - w.double()).abs() <= wide.double() * 0.5 + most.double().repeat_interleave(group, 2) * torch.finfo(dtype).eps / 2).all()
+
+
+# ------------------------------------------------------------------------------------------------ SwiGLU
+def swiglu_ref(h, p, da=None):
+    """The formulas in 64 bits: act, or (dh, dp), each with the size of what is summed up in it."""
+    g, u = h.double().chunk(2, dim=1)
+    s, pp = torch.sigmoid(g), 1.0 if p is None else p.double()[:, None]
+    if da is None:
+        return pp * g * s * u, (pp * g * s * u).abs()
+    d = da.double()
+    dg, du, dp = pp * d * u * s * (1 + g * (1 - s)), pp * d * g * s, d * g * s * u
+    return torch.cat((dg, du), 1), torch.cat(((pp * d * u * s).abs() * (1 + g.abs() * (1 - s)), du.abs()), 1), dp.sum(1), dp.abs().sum(1)
+
+
+def close(got, ref, mag, sums=0):
+    """Half a step of the type, and the fast exponential's error: at most 2 + 1.2 |g| steps of 2^-23, two more for the
+    division and a handful of products, 20 for |g| < 8; `sums`: length of a sum in fp32."""
+    tol = torch.finfo(got.dtype).eps / 2 * ref.abs() + (20 + sums) * 2.0 ** -23 * mag + (2.0 ** -25 if got.dtype == FP16 else 2.0 ** -134 if got.dtype == BF16 else 0)
+    assert ((got.double() - ref).abs() <= tol).all(), float(((got.double() - ref).abs() / tol.clamp(min=1e-300)).max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
+@pytest.mark.parametrize("weights", [True, False])
+@pytest.mark.parametrize("rows,inter,pad", [(1, 1, 0), (1, 1408, 0), (3, 7, 5), (70, 264, 8), (6000, 24, 0), (5000, 131, 1), (2, 9000, 0)])
+def test_swiglu(rows, inter, pad, weights, dtype):
+    h, da = randn((rows, 2 * inter), dtype, 1, 1.5, pad).clamp(-7.9, 7.9), randn((rows, inter), dtype, 2, 0.5, pad)
+    h = randn((rows, 2 * inter), dtype, 1, 1.5, pad)
+    h.clamp_(-7.9, 7.9)
+    p = torch.rand(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)) if weights else None
+    out = torch.full((rows, inter + 3), 7.0, dtype=dtype, device="cuda")
+    act = binding.swiglu(h, p, out=out[:, :inter])
+    close(act, *swiglu_ref(h, p))
+    assert (out[:, inter:] == 7).all()
+    got = binding.swiglu_grad(da, h, p)
+    dh, dh_mag, dp, dp_mag = swiglu_ref(h, p, da)
+    close(got[0] if weights else got, dh, dh_mag)
+    if weights:
+        close(got[1], dp, dp_mag, inter)
+
+
+def test_swiglu_extremes():
+    """Saturated gates, infinities and NaN come out as the formula's."""
+    g = torch.tensor([-200.0, -100.0, -88.5, 88.5, 100.0, 200.0, 0.0, float("inf"), float("-inf"), float("nan")], device="cuda")
+    h = torch.cat((g, torch.full_like(g, 2.0))).to(BF16)[None]
+    act = binding.swiglu(h)[0].float()
+    assert torch.equal(act[:3], torch.zeros(3, device="cuda") * act[:3]) and (act[:3].abs() < 1e-30).all()
+    assert torch.equal(act[3:6], (2 * h[0, 3:6].float()).to(BF16).float()) and act[6] == 0
+    assert act[7] == float("inf") and act[8:].isnan().all()
+    da = torch.ones_like(h[:, :10])
+    dh = binding.swiglu_grad(da, h)[0].float()
+    assert (dh[:3].abs() < 1e-30).all() and (dh[3:6] == 2).all() and dh[6] == 1
+
+
+def test_swiglu_gradient_by_differences():
+    """d act / d h along a random direction against (act(h + e v) - act(h - e v)) / 2 e of the formula in 64 bits."""
+    h, da = randn((5, 48), FP16, 4, 1.0), randn((5, 24), FP16, 5, 1.0)
+    p = torch.rand(5, device="cuda")
+    dh, dp = binding.swiglu_grad(da, h, p)
+    v, e = randn((5, 48), FP32, 6).double(), 1e-4
+
+    def act(at, w):
+        g, u = at.chunk(2, 1)
+        return (w[:, None] * g * torch.sigmoid(g) * u * da.double()).sum()
+
+    by_h = (act(h.double() + e * v, p.double()) - act(h.double() - e * v, p.double())) / (2 * e)
+    # dh is rounded to fp16: each term is off by half a step; the differences by e^2 times a third derivative, below 1e-6
+    assert abs(float((dh.double() * v).sum() - by_h)) <= float((dh.double() * v).abs().sum()) * 2.0 ** -11 + 1e-5
+    q = torch.rand(5, device="cuda").double()
+    by_p = (act(h.double(), p.double() + e * q) - act(h.double(), p.double() - e * q)) / (2 * e)
+    assert abs(float((dp.double() * q).sum() - by_p)) <= 1e-4

@@ -49,6 +49,43 @@ def test_grouped_mm_dw_refuses(lib):
         assert dw(lib, **change) == INVALID, change
 
 
+def mv(lib, device=-1, dtype=BF16, out_dtype=BF16, x=X, ldx=64, q=W, sc=0x5000, slots=OFF, pairs=12, per=6, n_slots=4, n=16, k=64, group=32, y=OUT, ldy=16):
+    return lib.ew_quant_mv(device, dtype, out_dtype, x, ldx, q, sc, slots, pairs, per, n_slots, n, k, group, y, ldy, None)
+
+
+def test_quant_mv_refuses(lib):
+    assert mv(lib) == mv(lib, pairs=0, x=None, y=None) == mv(lib, slots=None, n_slots=1, per=1) == NO_DEVICE
+    for change in [dict(dtype=FP32), dict(out_dtype=FP16), dict(x=None), dict(x=X + 8), dict(ldx=63), dict(ldx=68), dict(q=None), dict(q=W + 8), dict(sc=None), dict(sc=X + 2),
+                   dict(slots=None), dict(slots=OFF + 1), dict(pairs=-6), dict(pairs=13), dict(per=0), dict(n_slots=0), dict(n_slots=2049), dict(n=12), dict(n=0), dict(k=48),
+                   dict(k=0), dict(group=16), dict(group=96, k=96, ldx=96), dict(group=128), dict(y=None), dict(y=OUT + 1), dict(ldy=15)]:
+        assert mv(lib, **change) == INVALID, change
+
+
+def test_quant_pack_refuses(lib):
+    def pack(device=-1, dtype=BF16, w=X, ldw=64, stride=1024, n_slots=2, n=16, k=64, group=32, q=W, sc=OUT):
+        return lib.ew_quant_pack(device, dtype, w, ldw, stride, n_slots, n, k, group, q, sc, None)
+
+    assert pack() == pack(n_slots=1, stride=0) == pack(ldw=65, stride=1040) == NO_DEVICE
+    for change in [dict(dtype=FP32), dict(w=None), dict(w=X + 1), dict(ldw=63), dict(stride=1023), dict(n_slots=0), dict(n=4), dict(n=12), dict(k=65), dict(group=48, k=96, ldw=96),
+                   dict(q=None), dict(q=W + 8), dict(sc=None), dict(sc=OUT + 2)]:
+        assert pack(**change) == INVALID, change
+
+
+def test_swiglu_refuses(lib):
+    def act(device=-1, dtype=BF16, h=X, ldh=32, p=W, rows=4, inter=16, out=OUT, ldo=16):
+        return lib.ew_swiglu(device, dtype, h, ldh, p, rows, inter, out, ldo, None)
+
+    def grad(device=-1, dtype=BF16, da=X, ldda=16, h=X, ldh=32, p=W, rows=4, inter=16, out=OUT, ldo=32, dp=OFF):
+        return lib.ew_swiglu_grad(device, dtype, da, ldda, h, ldh, p, rows, inter, out, ldo, dp, None)
+
+    assert act() == act(p=None) == act(rows=0, h=None, out=None, p=None) == grad() == grad(dp=None) == grad(p=None, dp=None) == NO_DEVICE
+    for change in [dict(dtype=FP32), dict(h=None), dict(h=X + 1), dict(ldh=31), dict(p=W + 2), dict(rows=-1), dict(inter=0), dict(out=None), dict(out=OUT + 1), dict(ldo=15)]:
+        assert act(**change) == INVALID, change
+    for change in [dict(dtype=FP32), dict(da=None), dict(da=X + 1), dict(ldda=15), dict(h=None), dict(ldh=31), dict(p=None), dict(rows=-1), dict(inter=-1), dict(out=None),
+                   dict(ldo=31), dict(dp=OFF + 2)]:
+        assert grad(**change) == INVALID, change
+
+
 def test_operator_error_word_refuses(lib):
     assert lib.ew_last_operator_error(0, None) == INVALID
     assert lib.ew_last_operator_error(-1, C.byref(C.c_int32())) == NO_DEVICE
@@ -61,3 +98,7 @@ def test_python_checks_before_the_library():
         binding.grouped_mm(x, w, offsets)
     with pytest.raises(ValueError, match="CUDA tensor"):
         binding.grouped_mm_dw(x, x, offsets)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        binding.swiglu(x)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        binding.quant_pack(w, 32)
