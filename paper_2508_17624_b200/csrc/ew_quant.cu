@@ -5,14 +5,22 @@
 // for a batch's (token, expert) pairs p, whose slots come straight from the router: nothing is sorted or counted before
 // the call, every CTA groups the few hundred pairs itself, so that pairs of one slot share its weights' bytes.
 //
-// Bound by HBM: half a byte a weight and little else.  A stream of 6.5 TB/s is 46 weights a cycle and SM, more than plain
-// fp32 arithmetic keeps up with once an expert has several rows, so the products run on the warp-level tensor-core
-// instruction m16n8k16: 16 weight rows x 8 pairs (the tcgen05 kernels need 128-row tiles staged as 16-bit values in shared
-// memory, i.e. four times the bytes written and read back there).  A warp owns 16 rows and streams them through a ring of
-// its own with TMA (2 KiB a stage: 16 rows x 256 weights), no barrier is shared between warps.  Within a 32-weight step a
-// lane's word holds eight neighbouring k of one row and its 16 bytes of x the same eight k, so the operands meet without
-// any shuffling: the order of k inside an MMA is arbitrary as long as both sides use it.  q - 8 is exact in bf16 and fp16,
-// products are summed per group in fp32 and scaled in fp32: no rounding but the result's.
+// Bound by HBM: half a byte a weight and little else, at 6.5 TB/s 46 weights a cycle and SM.  Turning each into a 16-bit
+// number first (and-or, shift, subtract: 22 warp instructions for 512 weights and as many again around them) keeps the SM's
+// issue slots busy for longer than the bytes take (measured: 37 us where the bytes need 22), so the weights are used as
+// they are: one mask, or a shift and a mask, turns a word into four bytes 0..15, and the 8-bit integer m16n8k32
+// instruction multiplies 512 weights with eight pairs (2.1 cycles of an SM measured, what bf16 takes for 256; the 8-bit
+// floating-point form is made of 16-bit ones on this machine and slower).  x goes in as fixed-point numbers: a group of x,
+// which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 16319 (16 bits,
+// for 16-bit results) or above 4177919 (24 bits, for fp32 results), rounded to whole numbers and cut into signed
+// bytes.  That rounding is below 2^-15 (2^-23) of the group's largest x, and none at all for bf16 values down to a 128th
+// of it (a 2^15th).  The products' sums are exact integers, the offset 8 is their first value (-8 sum x); only then come
+// fp32 numbers: group sum times scale, added up over the groups.
+//
+// A warp owns 32 weight rows and streams them through a ring of its own with TMA, a line of 256 weights of each row (4 KiB)
+// at a time; the products' order within a line is arbitrary as long as both operands agree, so a lane's word of eight
+// weights meets the same eight k of x without any shuffling.  A CTA's tiles are contiguous and its lines are dealt to
+// its warps evenly; a tile that crosses from one warp to the next is added up in shared memory, in order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -24,107 +32,295 @@ namespace ops {
 namespace {
 using namespace tc;
 
-constexpr int kWarps = 16;
-constexpr int kThreads = kWarps * 32;
-constexpr int kStageK = 256;                   // weights of a row in one stage = one 128-byte swizzled line
-constexpr int kStageBytes = 16 * kStageK / 2;  // 2 KiB
-constexpr int kScaleBytes = 256;               // up to eight groups x 16 rows
-constexpr int kStages = 4;
+// warps of a CTA: sixteen, or eight with twice the registers where a warp has three columns of pairs
+constexpr __host__ __device__ int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+constexpr int kRows = 32;                      // weight rows of a tile: two tiles of the MMA
+constexpr int kLineK = 256;                    // weights of a row in one 128-byte swizzled line
+constexpr int kLineBytes = kRows * kLineK / 2; // a stage: 4 KiB
+constexpr int kScaleBytes = 512;               // a stage's scales: up to eight groups x 32 rows
+constexpr int kMaxStages = 4;                  // of a warp
 constexpr int kMaxPairs = 2048;                // of one launch; a larger batch is split
 constexpr int kMaxSlots = 2048;
+constexpr int kMaxK = 16384;
+constexpr int kSmemLimit = 227 * 1024;
 
 struct Args {
-    const uint8_t *x;
+    const uint8_t *x;           // row 0 of this launch
     const int32_t *slots;       // null: every pair uses slot 0
     void *out;
     int *err;
     long long ldx, ldo;         // elements
     int pairs, pair0, share;    // of this launch; its first pair; pairs per row of x
+    int lead;                   // pair0 % share
     int n, k, n_slots;
-    int tiles;                  // 16-row tiles of a slot
-    int split;                  // warps that share a tile, each with every split-th stage of k
-    int out_kind;
+    int tiles;                  // 32-row tiles of a slot
+    int out_fp32;
+    int job_rows;               // most pairs of a job
+    int stages;                 // of a warp's ring
+    // shared memory: the rows of x being worked on (capacity, bytes a row, of that the first two pieces and the third)
+    int x_cap, x_bytes, x_wide, x_third;
+    int at_x, at_bars, at_red, at_jobs, at_start, at_order, at_row;
 };
 
 struct alignas(8) Job { uint16_t slot, first, count, pad; };                // pairs order[first .. first + count) of one slot
 
-__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b, __nv_bfloat16) {
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
+__device__ __forceinline__ void mma8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b, __half) {
-    const __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
+// byte `at` of four numbers, the first one's lowest
+__device__ __forceinline__ uint32_t bytes(const uint32_t (&u)[8], int i0, int i1, int i2, int i3, int at) {
+    const uint32_t sel = (uint32_t)at | (uint32_t)(4 + at) << 4;
+    return __byte_perm(__byte_perm(u[i0], u[i1], sel), __byte_perm(u[i2], u[i3], sel), 0x5410);
+}
+template <class T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+
+template <class T>
+__device__ __forceinline__ void put(void *out, size_t at, float v, bool wide) {
+    if (wide) reinterpret_cast<float *>(out)[at] = v;
+    else reinterpret_cast<T *>(out)[at] = (T)v;
+}
+
+template <class T>
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    } else {
+        const __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
 }
 // Eight 4-bit values to q - 8 in four registers, k ascending: a nibble or-ed into the last mantissa bits of 128 (bf16) or
 // 1024 (fp16) is that number plus q, from which 136 (1032) is subtracted exactly.
 template <class T>
 __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&a)[4]) {
-    constexpr bool kBf = sizeof(T) == 2 && __is_same(T, __nv_bfloat16);
+    constexpr bool kBf = __is_same(T, __nv_bfloat16);
     constexpr uint32_t kMagic = kBf ? 0x43004300u : 0x64006400u, kBias = kBf ? 0x43084308u : 0x64086408u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = sub2(((w >> (4 * i)) & 0x000F000Fu) | kMagic, kBias, T());
+    for (int i = 0; i < 4; ++i) {
+        uint32_t v;
+        asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(v) : "r"(w >> (4 * i)), "r"(kMagic));    // (w & mask) | magic
+        a[i] = sub2<T>(v, kBias);
+    }
 }
 template <class T>
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const float (&c)[4]) {
     if constexpr (__is_same(T, __nv_bfloat16))
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-template <class T> __device__ __forceinline__ float scale_at(const uint8_t *s, int i);
-template <> __device__ __forceinline__ float scale_at<__nv_bfloat16>(const uint8_t *s, int i) { return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(s)[i]); }
-template <> __device__ __forceinline__ float scale_at<__half>(const uint8_t *s, int i) { return __half2float(reinterpret_cast<const __half *>(s)[i]); }
-
-__device__ __forceinline__ void put(void *out, size_t at, float v, int kind) {
-    if (kind == EW_FP32) reinterpret_cast<float *>(out)[at] = v;
-    else if (kind == EW_BF16) reinterpret_cast<__nv_bfloat16 *>(out)[at] = __float2bfloat16_rn(v);
-    else reinterpret_cast<__half *>(out)[at] = __float2half_rn(v);
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-// Shared memory.  The tables from which the pairs are grouped (per warp and slot the pairs before it, per pair its place)
-// lie in the ring, which is not in use yet.
-struct Layout {
-    int scales, bars, red, start, jobs, order, bytes;
-    int place, slot_of;                         // in the ring, behind the counters
-    __host__ __device__ Layout(int nt, int split, int n_slots, int pairs) {
-        int o = kWarps * kStages * kStageBytes;
-        scales = o; o += kWarps * kStages * kScaleBytes;
-        bars = o; o += kWarps * kStages * 8 + 16;
-        red = o; o += split > 1 ? kWarps * 128 * nt * 4 : 0;
-        jobs = o; o += pairs * 8;
-        start = o; o += (n_slots + 1) * 4;
-        order = o; o += pairs * 2;
-        bytes = o + 1024;
-        place = kWarps * (n_slots + 1) * 2;
-        slot_of = place + pairs * 2;
+// A whole number i, |i| < 2^22, plus these bits is the float kFloat + i: the sums start there and become floats by one
+// subtraction (the conversion instruction runs at an eighth of its rate; |a group's sum of q times a byte| < 2^18).
+constexpr int kFloatBits = 0x4B400000;
+constexpr float kFloat = 12582912.f;
+
+// A line of a row of x (a lane: eight k) into P bytes a number, highest first; per group of 32 SPG its scale 2^-e and the
+// sums' first values -8 sum of each byte (the weights' offset).  A group with an infinity or NaN gets the scale NaN.
+template <class T, int P, int SPG>
+__device__ __forceinline__ void convert_line(const uint4 raw, int line, bool there, uint8_t *to, const Args &a) {
+    static_assert(P == 2 || P == 3, "bytes of a number");
+    const int lane = threadIdx.x & 31, at_k = line * kLineK + lane * 8;
+    const T *v = reinterpret_cast<const T *>(&raw);
+    float f[8], most = 0.f;
+    bool odd = false;                                                        // (fmaxf drops a NaN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        f[i] = to_f<T>(v[i]);
+        most = fmaxf(most, fabsf(f[i]));
+        odd |= !(fabsf(f[i]) < __int_as_float(0x7f800000));
     }
-};
-static_assert(kWarps * (kMaxSlots + 1) * 2 + kMaxPairs * 4 <= kWarps * kStages * kStageBytes, "the grouping tables fit the ring");
-static_assert(kWarps * kStages * (kStageBytes + kScaleBytes + 8) + 16 + kWarps * 128 * 4 * 4 + kMaxPairs * 10 + (kMaxSlots + 1) * 4 + 1024 <= 227 * 1024, "shared memory");
+    if (odd) most = __int_as_float(0x7f800000);
+#pragma unroll
+    for (int m = 1; m < 4 * SPG; m <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
+    // signed bytes reach 127 (1 + 256 (+ 65536)): the largest x goes to [2^14, 2^15) ([2^22, 2^23)), or half of that
+    constexpr int kTop = P == 2 ? 14 : 22, kMost = P == 2 ? 32639 : 8355711;
+    const int e = __float_as_int(most) >> 23;                                // biased exponent of the largest
+    int up = min(254 + kTop - e, 253);                                       // biased exponent of the scale
+    if (most * __int_as_float(max(up, 1) << 23) > (float)kMost) --up;
+    up = max(up, 1);
+    const float scale = __int_as_float(up << 23), back = e == 255 ? __int_as_float(0x7fc00000) : __int_as_float((254 - up) << 23);
+    uint32_t u[8], lo[P], hi[P];
+    int sums[P];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        // number = sum of (byte_j - 128) 256^j for the bytes of number + 0x80 (1 + 256 (+ 65536)); the same bytes with their top
+        // bit turned are byte_j - 128
+        u[i] = (uint32_t)(__float2int_rn(e == 255 ? 0.f : f[i] * scale) + (P == 2 ? 0x8080 : 0x808080)) ^ (P == 2 ? 0x8080u : 0x808080u);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {                                            // in the order in which a word's nibbles come out
+        lo[j] = bytes(u, 0, 4, 1, 5, j);
+        hi[j] = bytes(u, 2, 6, 3, 7, j);
+        sums[j] = __dp4a((int)lo[j], 0x01010101, __dp4a((int)hi[j], 0x01010101, 0));
+    }
+    // |a group's sum of a byte| <= 2^14: two of them in one number on their way through the lanes
+    int low = sums[0] + sums[1] * 65536;
+#pragma unroll
+    for (int m = 1; m < 4 * SPG; m <<= 1) {
+        low += __shfl_xor_sync(0xffffffffu, low, m);
+        if (P == 3) sums[P - 1] += __shfl_xor_sync(0xffffffffu, sums[P - 1], m);
+    }
+    sums[0] = (int)(int16_t)low;
+    sums[1] = (low - sums[0]) >> 16;
+    if (!there) return;
+    *reinterpret_cast<uint4 *>(to + line * 512 + lane * 16) = make_uint4(lo[P - 1], hi[P - 1], lo[P - 2], hi[P - 2]);
+    if (P == 3) *reinterpret_cast<uint2 *>(to + a.x_wide + line * 256 + lane * 8) = make_uint2(lo[0], hi[0]);
+    if (lane % (4 * SPG) == 0)
+        *reinterpret_cast<int4 *>(to + a.x_wide + a.x_third + (at_k / (32 * SPG)) * 16) =
+            make_int4(__float_as_int(back), kFloatBits - 8 * sums[P - 1], kFloatBits - 8 * sums[P - 2], P == 3 ? kFloatBits - 8 * sums[0] : 0);
+}
 
-// T: operand type; NT: columns of eight pairs a warp accumulates at a time; SPG: 32-weight steps in a group
-template <class T, int NT, int SPG>
-__global__ void __launch_bounds__(kThreads, 1)
+__device__ __forceinline__ int4 lds4(uint32_t at) {
+    int4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+
+// One line (N columns of pairs): acc += scale 2^-e (sum of q x 2^e - 8 sum of x 2^e).  w_at: this lane's word of the line's
+// first 32-weight step; 16-byte piece i of row r lies at piece i ^ (r mod 8) of its line, one exclusive-or of the address.
+// xb, xc: this lane's operand bytes of the row's first step, fac0, fac1: of its first group, for the columns 2c and 2c + 1.
+template <class T, int P, int N, int NT, int SPG>
+__device__ __forceinline__ void line_products(float (&acc)[2][NT][4], const uint32_t (&xb)[NT], const uint32_t (&xc)[NT], const uint32_t (&fac0)[NT],
+                                              const uint32_t (&fac1)[NT], uint32_t w_at, uint32_t s_at, int line, int left) {
+    // (with one column a group a pass of the loop, not unrolled: small calls run this code cold, and fetching it is what they
+    // wait for)
+#pragma unroll(NT == 1 ? 1 : 8 / SPG)
+    for (int i0 = 0; i0 < 8 && 32 * i0 < left; i0 += SPG) {
+        int sum[P][2][N][4];
+        float f0[N], f1[N];
+        const uint32_t g16 = (uint32_t)(line * (8 / SPG) + i0 / SPG) * 16;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int4 v0 = lds4(fac0[t] + g16), v1 = lds4(fac1[t] + g16);
+            f0[t] = __int_as_float(v0.x);
+            f1[t] = __int_as_float(v1.x);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                sum[0][m][t][0] = sum[0][m][t][2] = v0.y;
+                sum[0][m][t][1] = sum[0][m][t][3] = v1.y;
+                sum[1][m][t][0] = sum[1][m][t][2] = v0.z;
+                sum[1][m][t][1] = sum[1][m][t][3] = v1.z;
+                if (P == 3) {
+                    sum[P - 1][m][t][0] = sum[P - 1][m][t][2] = v0.w;
+                    sum[P - 1][m][t][1] = sum[P - 1][m][t][3] = v1.w;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < SPG; ++j) {
+            const int i = i0 + j;
+            uint32_t w[4];
+            asm volatile("ld.shared.b32 %0, [%4];\n\tld.shared.b32 %1, [%4 + 1024];\n\tld.shared.b32 %2, [%4 + 2048];\n\tld.shared.b32 %3, [%4 + 3072];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(w_at ^ (i << 4)));
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                lo[h] = w[h] & 0x0F0F0F0Fu;
+                hi[h] = (w[h] >> 4) & 0x0F0F0F0Fu;
+            }
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const int4 b = lds4(xb[t] + line * 512 + i * 64);
+                uint32_t d0 = 0, d1 = 0;
+                if (P == 3) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(d0), "=r"(d1) : "r"(xc[t] + line * 256 + i * 32));
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    mma8(sum[0][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.x, b.y);
+                    mma8(sum[1][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.z, b.w);
+                    if (P == 3) mma8(sum[P - 1][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], d0, d1);
+                }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            uint16_t r0, r1;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r0) : "r"(s_at + ((i0 / SPG) * kRows + m * 16) * 2));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r1) : "r"(s_at + ((i0 / SPG) * kRows + m * 16) * 2 + 16));
+            const float s0 = to_f<T>(*reinterpret_cast<T *>(&r0)), s1 = to_f<T>(*reinterpret_cast<T *>(&r1));
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = fmaf(__int_as_float(sum[0][m][t][e]) - kFloat, 256.f, __int_as_float(sum[1][m][t][e]) - kFloat);
+                    if (P == 3) v = fmaf(v, 256.f, __int_as_float(sum[P - 1][m][t][e]) - kFloat);
+                    acc[m][t][e] += ((e < 2 ? s0 : s1) * (e & 1 ? f1[t] : f0[t])) * v;
+                }
+        }
+    }
+}
+
+// The same with 16-bit operands: the weights as q - 8, x as it is.
+template <class T, int N, int NT, int SPG>
+__device__ __forceinline__ void line_products_16(float (&acc)[2][NT][4], const uint32_t (&xb)[NT], uint32_t w_at, uint32_t s_at, int line, int left) {
+#pragma unroll
+    for (int i0 = 0; i0 < 8; i0 += SPG) {
+        if (32 * i0 >= left) break;
+        float sum[2][N][4];
+#pragma unroll
+        for (int j = 0; j < SPG; ++j) {
+            const int i = i0 + j;
+            uint32_t w[4];
+            asm volatile("ld.shared.b32 %0, [%4];\n\tld.shared.b32 %1, [%4 + 1024];\n\tld.shared.b32 %2, [%4 + 2048];\n\tld.shared.b32 %3, [%4 + 3072];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(w_at ^ (i << 4)));
+            int4 b[N];
+#pragma unroll
+            for (int t = 0; t < N; ++t) b[t] = lds4(xb[t] + line * 512 + i * 64);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                uint32_t lo[4], hi[4];
+                unpack<T>(w[2 * m], lo);
+                unpack<T>(w[2 * m + 1], hi);
+                const float none[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < N; ++t) {
+                    if (j == 0) mma16<T>(sum[m][t], lo[0], hi[0], lo[1], hi[1], b[t].x, b[t].y, none);
+                    else mma16<T>(sum[m][t], lo[0], hi[0], lo[1], hi[1], b[t].x, b[t].y, sum[m][t]);
+                }
+#pragma unroll
+                for (int t = 0; t < N; ++t) mma16<T>(sum[m][t], lo[2], hi[2], lo[3], hi[3], b[t].z, b[t].w, sum[m][t]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            uint16_t r0, r1;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r0) : "r"(s_at + ((i0 / SPG) * kRows + m * 16) * 2));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r1) : "r"(s_at + ((i0 / SPG) * kRows + m * 16) * 2 + 16));
+            const float s0 = to_f<T>(*reinterpret_cast<T *>(&r0)), s1 = to_f<T>(*reinterpret_cast<T *>(&r1));
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m][t][e] += (e < 2 ? s0 : s1) * sum[m][t][e];
+        }
+    }
+}
+
+// T: operand type; P: bytes of a number of x, 0: x in its own type; NT: columns of eight pairs a warp accumulates at a time; SPG: 32-weight
+// steps in a group
+template <class T, int P, int NT, int SPG>
+__global__ void __launch_bounds__(warps_of(NT) * 32, 1)
 quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ Args a) {
+    constexpr int kWarps = warps_of(NT), kThreads = kWarps * 32;
+    const bool wide = P == 3 || (P == 0 && a.out_fp32);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem_base - smem_u32(smem_raw));
-    const Layout L(NT, a.split, a.n_slots, a.pairs);
-    int *start = reinterpret_cast<int *>(smem + L.start);
-    uint16_t *order = reinterpret_cast<uint16_t *>(smem + L.order);
-    uint16_t *before = reinterpret_cast<uint16_t *>(smem), *place = reinterpret_cast<uint16_t *>(smem + L.place), *slot_of = reinterpret_cast<uint16_t *>(smem + L.slot_of);
-    Job *jobs = reinterpret_cast<Job *>(smem + L.jobs);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L.bars + kWarps * kStages * 8);
+    int *start = reinterpret_cast<int *>(smem + a.at_start);
+    uint16_t *order = reinterpret_cast<uint16_t *>(smem + a.at_order), *x_row = reinterpret_cast<uint16_t *>(smem + a.at_row);
+    Job *jobs = reinterpret_cast<Job *>(smem + a.at_jobs);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + a.at_bars + kWarps * kMaxStages * 8);
     volatile int *n_jobs_at = abort_flag + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t my_bars = smem_base + L.bars + warp * kStages * 8;
-    const uint32_t my_ring = smem_base + warp * kStages * kStageBytes, my_scales = smem_base + L.scales + warp * kStages * kScaleBytes;
+    const uint32_t my_bars = smem_base + a.at_bars + warp * kMaxStages * 8;
+    const uint32_t my_ring = smem_base + warp * a.stages * kLineBytes, my_scales = smem_base + kWarps * a.stages * kLineBytes + warp * a.stages * kScaleBytes;
 
     if (lane == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(my_bars + 8 * s, 1);
+        for (int s = 0; s < a.stages; ++s) mbar_init(my_bars + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 0) {
@@ -132,216 +328,349 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         prefetch_map(&map_q);
         prefetch_map(&map_s);
     }
+    // (the tables from which the pairs are grouped - per warp and slot the pairs before it, per pair its place - lie where the
+    // ring and the rows of x will be)
+    uint16_t *before = reinterpret_cast<uint16_t *>(smem), *place = before + kWarps * (a.n_slots + 1), *slot_of = place + a.pairs;
     const int kinds = a.n_slots + 1;                                         // the last one: pairs without a slot
-    for (int g = threadIdx.x; g < kWarps * kinds; g += kThreads) before[g] = 0;
+    const bool few = a.pairs <= 32;
+    if (!few)
+        for (int g = threadIdx.x; g < kWarps * kinds; g += kThreads) before[g] = 0;
     pdl_launch_dependents();
     __syncthreads();
     pdl_wait();
 
     // ---------------------------------------------------------------------- pairs by slot
-    // A stable counting sort, the same in every CTA: each warp counts its stretch of the pairs in order, the warps' counts
-    // are added up per slot, and a pair's position is that sum plus its rank in its warp.
     const int32_t *slots = a.slots;
-    const int stretch = ((a.pairs + kThreads - 1) / kThreads) * 32, p_end = min(a.pairs, (warp + 1) * stretch);
-    uint16_t *mine = before + warp * kinds;
-    bool bad = false;
-    for (int p0 = warp * stretch; p0 < p_end; p0 += 32) {
-        const int p = p0 + lane;
-        const bool there = p < p_end;
+    auto slot_at = [&](int p, bool there) {
         const int raw = there && slots ? *(const volatile int32_t *)(slots + p) : 0;
-        const int s = !there ? -1 : raw < 0 || raw >= a.n_slots ? a.n_slots : raw;
-        bad |= raw >= a.n_slots;
-        const uint32_t same = __match_any_sync(0xffffffffu, s);
-        const int rank = __popc(same & ((1u << lane) - 1)), prior = there ? mine[s] : 0;
-        __syncwarp();
-        if (there && rank == 0) mine[s] = (uint16_t)(prior + __popc(same));
-        __syncwarp();
-        if (there) {
-            place[p] = (uint16_t)(prior + rank);
-            slot_of[p] = (uint16_t)s;
-        }
-    }
-    if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadIndex);
-    __syncthreads();
-    for (int g = threadIdx.x; g < kinds; g += kThreads) {
-        int sum = 0;
-        for (int w = 0; w < kWarps; ++w) {
-            const int v = before[w * kinds + g];
-            before[w * kinds + g] = (uint16_t)sum;
-            sum += v;
-        }
-        start[g] = sum;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        int seen = 0, jobs_before = 0;
-        for (int g0 = 0; g0 < kinds; g0 += 32) {
-            const int g = g0 + lane, c = g < kinds ? start[g] : 0, nj = g < a.n_slots ? (c + 8 * NT - 1) / (8 * NT) : 0;
-            int inc = c, jinc = nj;
+        if (raw >= a.n_slots && blockIdx.x == 0) atomicOr(a.err, kErrBadIndex);
+        return !there ? -1 : raw < 0 || raw >= a.n_slots ? a.n_slots : raw;
+    };
+    auto scan = [&](int v) {                                                 // inclusive sum over the lanes
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, inc, d), w = __shfl_up_sync(0xffffffffu, jinc, d);
-                if (lane >= d) { inc += v; jinc += w; }
-            }
-            const int first = seen + inc - c;
-            if (g < kinds) start[g] = first;
-            for (int j = 0; j < nj; ++j)
-                jobs[jobs_before + jinc - nj + j] = Job{(uint16_t)g, (uint16_t)(first + j * 8 * NT), (uint16_t)min(8 * NT, c - j * 8 * NT), 0};
-            seen += __shfl_sync(0xffffffffu, inc, 31);
-            jobs_before += __shfl_sync(0xffffffffu, jinc, 31);
+        for (int d = 1; d < 32; d <<= 1) {
+            const int w = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += w;
         }
-        if (lane == 0) *n_jobs_at = jobs_before;
+        return v;
+    };
+    if (few) {
+        // one warp sees all pairs: slots in the order of their first pair, pairs without a slot last
+        if (warp == 0) {
+            const int s = slot_at(lane, lane < a.pairs);
+            const uint32_t same = __match_any_sync(0xffffffffu, s), below = (1u << lane) - 1;
+            const bool live = s >= 0 && s < a.n_slots, leads = live && !(same & below);
+            const int c = __popc(same), nj = leads ? (c + a.job_rows - 1) / a.job_rows : 0;
+            const int to = scan(leads ? c : 0), job_to = scan(nj), live_all = __shfl_sync(0xffffffffu, to, 31);
+            const int of_leader = __shfl_sync(0xffffffffu, to - c, __ffs(same) - 1), first = live ? of_leader : live_all;
+            if (s >= 0) {
+                order[first + __popc(same & below)] = (uint16_t)lane;
+                x_row[first + __popc(same & below)] = (uint16_t)((lane + a.lead) / a.share);
+            }
+            for (int j = 0; j < nj; ++j) jobs[job_to - nj + j] = Job{(uint16_t)s, (uint16_t)(to - c + j * a.job_rows), (uint16_t)min(a.job_rows, c - j * a.job_rows), 0};
+            if (lane == 31) *n_jobs_at = job_to;
+            if (lane == 0) start[a.n_slots] = live_all;
+        }
+    } else {
+        // a stable counting sort, the same in every CTA: each warp counts its stretch of the pairs in order, the warps'
+        // counts are added up per slot, and a pair's position is that sum plus its rank in its warp
+        const int stretch = ((a.pairs + kThreads - 1) / kThreads) * 32, p_end = min(a.pairs, (warp + 1) * stretch);
+        uint16_t *mine = before + warp * kinds;
+        constexpr int kMost = kMaxPairs / kThreads;
+        int s_of[kMost];
+#pragma unroll
+        for (int j = 0; j < kMost; ++j) s_of[j] = slot_at(warp * stretch + 32 * j + lane, warp * stretch + 32 * j + lane < p_end);
+#pragma unroll
+        for (int j = 0; j < kMost; ++j) {
+            const int p = warp * stretch + 32 * j + lane, s = s_of[j];
+            const bool there = p < p_end;
+            const uint32_t same = __match_any_sync(0xffffffffu, s);
+            const int rank = __popc(same & ((1u << lane) - 1)), prior = there ? mine[s] : 0;
+            __syncwarp();
+            if (there && rank == 0) mine[s] = (uint16_t)(prior + __popc(same));
+            __syncwarp();
+            if (there) {
+                place[p] = (uint16_t)(prior + rank);
+                slot_of[p] = (uint16_t)s;
+            }
+        }
+        __syncthreads();
+        for (int g = threadIdx.x; g < kinds; g += kThreads) {
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const int v = before[w * kinds + g];
+                before[w * kinds + g] = (uint16_t)sum;
+                sum += v;
+            }
+            start[g] = sum;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int seen = 0, jobs_before = 0;
+            for (int g0 = 0; g0 < kinds; g0 += 32) {
+                const int g = g0 + lane, c = g < kinds ? start[g] : 0, nj = g < a.n_slots ? (c + a.job_rows - 1) / a.job_rows : 0;
+                const int both = scan(c | nj << 16);                         // two sums of at most 2048 in one
+                const int first = seen + (both & 0xffff) - c, first_job = jobs_before + (both >> 16) - nj;
+                if (g < kinds) start[g] = first;
+                for (int j = 0; j < nj; ++j) jobs[first_job + j] = Job{(uint16_t)g, (uint16_t)(first + j * a.job_rows), (uint16_t)min(a.job_rows, c - j * a.job_rows), 0};
+                const int all = __shfl_sync(0xffffffffu, both, 31);
+                seen += all & 0xffff;
+                jobs_before += all >> 16;
+            }
+            if (lane == 0) *n_jobs_at = jobs_before;
+        }
+        __syncthreads();
+        for (int p = threadIdx.x; p < a.pairs; p += kThreads) {
+            const int s = slot_of[p], to = start[s] + before[(p / stretch) * kinds + s] + place[p];
+            order[to] = (uint16_t)p;
+            x_row[to] = (uint16_t)((p + a.lead) / a.share);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the ring belongs to the copies from here on
     }
-    __syncthreads();
-    for (int p = threadIdx.x; p < a.pairs; p += kThreads) {
-        const int s = slot_of[p];
-        order[start[s] + before[(p / stretch) * kinds + s] + place[p]] = (uint16_t)p;
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring belongs to the copies from here on
     __syncthreads();
 
     // ---------------------------------------------------------------------- the stream
-    const int n_items = *n_jobs_at * a.tiles;
-    const int team = warp / a.split, part = warp - team * a.split, teams = kWarps / a.split;
-    const int first_item = blockIdx.x * teams + team, step_items = gridDim.x * teams;
-    const int k_stages = (a.k + kStageK - 1) / kStageK;
-    const int my_stages = k_stages > part ? (k_stages - part + a.split - 1) / a.split : 0;       // of every item
-    constexpr uint32_t kTx = kStageBytes + (8 / SPG) * 32;
-    const int groups = a.k / (32 * SPG);
-
-    int i_item = first_item, i_stage = 0;                                    // the next stage to ask for
-    uint32_t issued = 0, used = 0;
-    auto issue = [&]() {
-        if (i_item >= n_items || my_stages == 0) return;
-        const int job = i_item / a.tiles, tile = i_item - job * a.tiles, kb = part + i_stage * a.split;
-        const uint32_t s = issued % kStages, bar = my_bars + 8 * s;
-        const int slot = jobs[job].slot;
-        if (lane == 0) {
-            mbar_expect_tx(bar, kTx);
-            tma_load_2d(my_ring + s * kStageBytes, &map_q, kb * (kStageK / 2), slot * a.n + tile * 16, bar);
-            tma_load_2d(my_scales + s * kScaleBytes, &map_s, tile * 16, slot * groups + kb * (8 / SPG), bar);
-        }
-        ++issued;
-        if (++i_stage == my_stages) { i_stage = 0; i_item += step_items; }
-    };
-    for (int s = 0; s < kStages; ++s) issue();
-
+    // This CTA's tiles (an item: a job's 32-row tile), in batches whose rows of x fit the shared memory.
+    const int n_jobs = *n_jobs_at, n_items = n_jobs * a.tiles, grid = (int)gridDim.x, each = n_items / grid, rest = n_items - each * grid;
+    int left_items = each + ((int)blockIdx.x < rest);
+    const int first_item = each * (int)blockIdx.x + min((int)blockIdx.x, rest);
+    int job0 = first_item / a.tiles, tile0 = first_item - job0 * a.tiles;
+    const int k_lines = (a.k + kLineK - 1) / kLineK, groups = a.k / (32 * SPG);
     const int r = lane >> 2, c = lane & 3;
+    uint32_t ask_stage = 0, stage = 0, phase = 0;                            // of the warp's ring, over all batches
     bool ok = true;
-    for (int item = first_item; item < n_items; item += step_items) {
-        const int job = item / a.tiles, tile = item - job * a.tiles;
-        const Job jb = jobs[job];
-        const int n_tiles = (jb.count + 7) >> 3;
-        const uint8_t *xp[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int m = t * 8 + r;
-            xp[t] = m < jb.count ? a.x + ((size_t)((a.pair0 + order[jb.first + m]) / a.share) * a.ldx + 8 * c) * 2 : nullptr;
+    while (left_items > 0) {
+        int job1 = job0, rows = 0, items = -tile0;
+        while (job1 < n_jobs && items < left_items && rows + jobs[job1].count <= a.x_cap) {
+            rows += jobs[job1++].count;
+            items += a.tiles;
         }
-        float acc[NT][4];
+        items = min(items, left_items);
+        const int lines = items * k_lines, l0 = (int)((long long)lines * warp / kWarps), l1 = (int)((long long)lines * (warp + 1) / kWarps);
+
+        // the next line to ask for, and the one being worked on
+        struct Cursor { int job, tile, line; };
+        Cursor at = {job0, tile0 + l0 / k_lines, l0 % k_lines};
+        while (at.tile >= a.tiles) { at.tile -= a.tiles; ++at.job; }
+        Cursor ask = at;
+        int left_to_ask = l1 - l0;
+        auto advance = [&](Cursor &u) {
+            if (++u.line == k_lines) {
+                u.line = 0;
+                if (++u.tile == a.tiles) { u.tile = 0; ++u.job; }
+            }
+        };
+        auto issue = [&]() {
+            if (left_to_ask <= 0 || !ok) return;
+            if (lane == 0) {
+                const int slot = jobs[ask.job].slot;
+                const uint32_t bar = my_bars + 8 * ask_stage;
+                mbar_expect_tx(bar, kLineBytes + (8 / SPG) * kRows * 2);
+                tma_load_2d(my_ring + ask_stage * kLineBytes, &map_q, ask.line * (kLineK / 2), slot * a.n + ask.tile * kRows, bar);
+                tma_load_2d(my_scales + ask_stage * kScaleBytes, &map_s, ask.tile * kRows, slot * groups + ask.line * (8 / SPG), bar);
+            }
+            if (++ask_stage == (uint32_t)a.stages) ask_stage = 0;
+            --left_to_ask;
+            advance(ask);
+        };
+#pragma unroll 1
+        for (int s = 0; s < a.stages; ++s) issue();
+
+        // the batch's rows of x, a line at a time, while the first weights are on their way (they are contiguous in the
+        // order of the pairs)
+        const int pair_at = jobs[job0].first;
+        // (several lines at a time where there are many: a line is a chain of a load and a dozen shuffles)
+        constexpr int kAtOnce = NT == 1 ? 1 : 8;
+        for (int row = warp / k_lines, line = warp - row * k_lines; row < rows;) {
+            uint4 raw[kAtOnce];
+            int rows_of[kAtOnce], lines_of[kAtOnce];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
-        for (int j = 0; j < my_stages; ++j) {
-            const int k0 = (part + j * a.split) * kStageK, steps = min(kStageK, a.k - k0) >> 5;
-            const uint32_t s = used % kStages;
-            const uint8_t *w_at = smem + (my_ring - smem_base) + s * kStageBytes + r * 128 + c * 4;
-            const uint8_t *s_at = smem + (my_scales - smem_base) + s * kScaleBytes;
-            // (after an expired wait the warp walks on without data: its team's barriers still need it)
-            if (ok) ok = mbar_wait_warp(my_bars + 8 * s, (used / kStages) & 1, abort_flag, a.err);
-            if (!ok) continue;
-            ++used;
+            for (int j = 0; j < kAtOnce; ++j) {
+                rows_of[j] = row;
+                lines_of[j] = line;
+                raw[j] = make_uint4(0, 0, 0, 0);
+                const int at_k = line * kLineK + lane * 8;
+                if (row < rows && at_k < a.k) raw[j] = *reinterpret_cast<const uint4 *>(a.x + ((size_t)x_row[pair_at + row] * a.ldx + at_k) * 2);
+                for (line += kWarps; line >= k_lines; line -= k_lines) ++row;
+            }
 #pragma unroll
-            for (int i0 = 0; i0 < 8; i0 += SPG) {
-                if (i0 < steps) {
-                    float sum[NT][4];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = sum[t][2] = sum[t][3] = 0.f;
-#pragma unroll
-                    for (int i = i0; i < i0 + SPG; ++i) {
-                        uint32_t lo[4], hi[4];
-                        const uint8_t *w = w_at + ((i ^ r) << 4);
-                        unpack<T>(*reinterpret_cast<const uint32_t *>(w), lo);
-                        unpack<T>(*reinterpret_cast<const uint32_t *>(w + 1024), hi);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            if (t < n_tiles) {
-                                uint4 b = make_uint4(0, 0, 0, 0);
-                                if (xp[t]) b = *reinterpret_cast<const uint4 *>(xp[t] + (size_t)(k0 + 32 * i) * 2);
-                                mma<T>(sum[t], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
-                                mma<T>(sum[t], lo[2], hi[2], lo[3], hi[3], b.z, b.w);
-                            }
-                        }
-                    }
-                    const float s0 = scale_at<T>(s_at, (i0 / SPG) * 16 + r), s1 = scale_at<T>(s_at, (i0 / SPG) * 16 + 8 + r);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        acc[t][0] += s0 * sum[t][0];
-                        acc[t][1] += s0 * sum[t][1];
-                        acc[t][2] += s1 * sum[t][2];
-                        acc[t][3] += s1 * sum[t][3];
-                    }
+            for (int j = 0; j < kAtOnce; ++j)
+            {
+                const bool there = rows_of[j] < rows && lines_of[j] * kLineK + lane * 8 < a.k;
+                uint8_t *to = smem + a.at_x + rows_of[j] * a.x_bytes;
+                if constexpr (P == 0) {
+                    if (there) *reinterpret_cast<uint4 *>(to + lines_of[j] * 512 + lane * 16) = raw[j];
+                } else {
+                    convert_line<T, P, SPG>(raw[j], lines_of[j], there, to, a);
                 }
             }
-            __syncwarp();                                                    // all lanes have read the stage
-            issue();
         }
-        if (a.split > 1) {
-            // the team's parts meet in shared memory and are added in order
-            float *red = reinterpret_cast<float *>(smem + L.red) + (size_t)team * a.split * 128 * NT;
+        __syncthreads();
+
+        float acc[2][NT][4];
+        Job jb = {};
+        uint32_t xb[NT], xc[NT], fac0[NT], fac1[NT];
+        bool mine = false;                       // the tile's first line was this warp's
+        int pending = -1;                        // line of a tile that this warp began and others go on with, where it stopped
+        float *red = reinterpret_cast<float *>(smem + a.at_red);
+        // one pass more than lines: after it all partial tiles are in place, and the pending one is finished
+#pragma unroll 1
+        for (int l = l0; l <= l1; ++l) {
+            bool done = false;
+            if (l < l1) {
+                if (l == l0 || at.line == 0) {
+                    jb = jobs[at.job];
+                    mine = at.line == 0;
+                    const uint32_t base = smem_base + a.at_x + (jb.first - pair_at) * a.x_bytes, fac = a.x_wide + a.x_third;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t) {
+                        // a column behind the job's last pair repeats that one: an MMA column depends on its own operand
+                        // only, and it is not stored
+                        const uint32_t own = base + min(t * 8 + r, jb.count - 1) * a.x_bytes;
+                        xb[t] = own + c * 16;
+                        xc[t] = own + a.x_wide + c * 8;
+                        fac0[t] = base + min(t * 8 + 2 * c, jb.count - 1) * a.x_bytes + fac;
+                        fac1[t] = base + min(t * 8 + 2 * c + 1, jb.count - 1) * a.x_bytes + fac;
+                    }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) red[(part * NT * 4 + t * 4 + e) * 32 + lane] = acc[t][e];
-            asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(a.split * 32) : "memory");
-            if (part == 0) {
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) acc[m][t][0] = acc[m][t][1] = acc[m][t][2] = acc[m][t][3] = 0.f;
+                }
+                // (after an expired wait the warp walks on without data: the CTA's barriers still need it)
+                if (ok) ok = mbar_wait_warp(my_bars + 8 * stage, phase, abort_flag, a.err);
+                if (ok) {
+                    const uint32_t w_at = my_ring + stage * kLineBytes + r * 144 + c * 4, s_at = my_scales + stage * kScaleBytes + r * 2;
+                    const int left = a.k - at.line * kLineK;
+                    if constexpr (P != 0) {
+                        line_products<T, P, 1, NT, SPG>(acc, xb, xc, fac0, fac1, w_at, s_at, at.line, left);
+                    } else {
+                        if (jb.count <= 8) line_products_16<T, 1, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
+                        else if (jb.count <= 16) line_products_16<T, 2, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
+                        else line_products_16<T, 3, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
+                    }
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                    __syncwarp();                                            // all lanes have read the stage
+                    issue();
+                }
+                const bool last = at.line == k_lines - 1;
+                if (mine) {
+                    done = last;
+                    if (!last && l == l1 - 1) pending = at.line;
+                } else if (last || l == l1 - 1) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) red[((warp * 2 + m) * NT * 4 + t * 4 + e) * 32 + lane] = acc[m][t][e];
+                }
+            } else {
+                __syncthreads();                                             // partial tiles are in place, and the rows of x free
+                if (pending < 0) break;
+                const int tile_end = l1 - 1 - pending + k_lines;
+#pragma unroll 1
+                for (int w = warp + 1; w < kWarps; ++w) {
+                    const int from = (int)((long long)lines * w / kWarps), to = (int)((long long)lines * (w + 1) / kWarps);
+                    if (from >= tile_end) break;
+                    if (to > from) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[m][t][e] += red[((w * 2 + m) * NT * 4 + t * 4 + e) * 32 + lane];
+                    }
+                }
+                done = true;
+            }
+            if (done) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        for (int q = 1; q < a.split; ++q) acc[t][e] += red[(q * NT * 4 + t * 4 + e) * 32 + lane];
+                    for (int e = 0; e < 2; ++e) {
+                        const int at_pair = t * 8 + 2 * c + e;
+                        if (at_pair < jb.count) {
+                            const size_t to = (size_t)(a.pair0 + order[jb.first + at_pair]) * a.ldo;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const int row = at.tile * kRows + m * 16 + r;
+                                if (row < a.n) put<T>(a.out, to + row, acc[m][t][e], wide);
+                                if (row + 8 < a.n) put<T>(a.out, to + row + 8, acc[m][t][2 + e], wide);
+                            }
+                        }
+                    }
             }
-            asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(a.split * 32) : "memory");
-            if (part) continue;
+            if (l < l1) advance(at);
         }
-        const int row = tile * 16 + r;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int m = t * 8 + 2 * c + e;
-                if (m < jb.count) {
-                    const size_t at = (size_t)(a.pair0 + order[jb.first + m]) * a.ldo + row;
-                    if (row < a.n) put(a.out, at, acc[t][e], a.out_kind);
-                    if (row + 8 < a.n) put(a.out, at + 8, acc[t][2 + e], a.out_kind);
-                }
-            }
+        left_items -= items;
+        job0 = job1;
+        tile0 = 0;
     }
     // pairs without a slot: rows of zeros
     for (int i = start[a.n_slots] + blockIdx.x * kWarps + warp; i < a.pairs; i += gridDim.x * kWarps)
-        for (int n = lane; n < a.n; n += 32) put(a.out, (size_t)(a.pair0 + order[i]) * a.ldo + n, 0.f, a.out_kind);
+        for (int n = lane; n < a.n; n += 32) put<T>(a.out, (size_t)(a.pair0 + order[i]) * a.ldo + n, 0.f, wide);
     if (*abort_flag) {                                                       // let copies in flight land
         const long long t0 = clock64();
         while (clock64() - t0 < 2000000ll) {}
     }
 }
 
-template <class T, int NT, int SPG>
-ew_status_t launch(const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int ctas, cudaStream_t st) {
-    const Layout L(NT, a.split, a.n_slots, a.pairs);
-    return launched(launch_pdl(quant_mv_kernel<T, NT, SPG>, dim3(ctas), dim3(kThreads), (size_t)L.bytes, st, mq, ms, a), "4-bit product");
+template <class T, int P, int NT, int SPG>
+ew_status_t launch(const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
+    return launched(launch_pdl(quant_mv_kernel<T, P, NT, SPG>, dim3(ctas), dim3(warps_of(NT) * 32), (size_t)smem, st, mq, ms, a), "4-bit product");
 }
-template <class T, int NT>
-ew_status_t launch_group(int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int ctas, cudaStream_t st) {
-    if (group == 32) return launch<T, NT, 1>(mq, ms, a, ctas, st);
-    if (group == 64) return launch<T, NT, 2>(mq, ms, a, ctas, st);
-    return launch<T, NT, 4>(mq, ms, a, ctas, st);
+template <class T, int P, int NT>
+ew_status_t launch_group(int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
+    if (group == 32) return launch<T, P, NT, 1>(mq, ms, a, smem, ctas, st);
+    if (group == 64) return launch<T, P, NT, 2>(mq, ms, a, smem, ctas, st);
+    return launch<T, P, NT, 4>(mq, ms, a, smem, ctas, st);
 }
-template <class T, int NT>
+template <class T>
+ew_status_t launch_type(int pieces, int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
+    if (pieces == 0) return launch_group<T, 0, 3>(group, mq, ms, a, smem, ctas, st);
+    if (pieces == 2) return launch_group<T, 2, 1>(group, mq, ms, a, smem, ctas, st);
+    return launch_group<T, 3, 1>(group, mq, ms, a, smem, ctas, st);
+}
+template <class T, int P, int NT>
 int setup_one() {
-    const int most = 227 * 1024;
-    return (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) |
-           (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) |
-           (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+}
+template <class T>
+int setup_type() { return setup_one<T, 0, 3>() | setup_one<T, 2, 1>() | setup_one<T, 3, 1>(); }
+
+// Shared memory of a launch: ring and scales, rows of x, barriers, partial tiles, job and pair tables.  As many
+// stages a warp as leave room for the rows of x of a whole job.  Returns the bytes, 0 if not even one row fits.
+int lay_out(Args &a, int nt, int group, int pieces) {
+    const int groups = a.k / group;
+    // rows of x start 64 bytes apart modulo 128: the two rows that a quarter of a warp reads lie in different banks
+    a.x_wide = (a.k * 2 + 127) / 128 * 128 + 64;
+    a.x_third = pieces == 3 ? (a.k + 127) / 128 * 128 : 0;
+    a.x_bytes = (a.x_wide + a.x_third + (pieces ? groups * 16 : 0) + 127) / 128 * 128 + 64;
+    const int warps = warps_of(nt);
+    for (a.stages = nt == 1 ? 2 : 4; a.stages >= 1; --a.stages) {
+        const int ring = warps * a.stages * (kLineBytes + kScaleBytes), bars = warps * kMaxStages * 8 + 16, red = warps * 1024 * nt;
+        const int fixed = 1024 + ring + 16 + bars + red + (a.n_slots + 1) * 4 + a.pairs * 12;
+        a.x_cap = (kSmemLimit - fixed) / a.x_bytes;
+        if (a.x_cap > a.pairs) a.x_cap = a.pairs;
+        if (a.stages > 1 && a.x_cap < 8 * nt && a.x_cap < a.pairs) continue;
+        if (a.x_cap < 1) return 0;
+        a.job_rows = a.x_cap < 8 * nt ? a.x_cap : 8 * nt;
+        int o = ring;
+        a.at_x = o; o += a.x_cap * a.x_bytes;
+        a.at_bars = o = (o + 15) / 16 * 16; o += bars;
+        a.at_red = o; o += red;
+        a.at_jobs = o; o += a.pairs * 8;
+        a.at_start = o; o += (a.n_slots + 1) * 4;
+        a.at_order = o; o += a.pairs * 2;
+        a.at_row = o; o += a.pairs * 2;
+        // the grouping tables lie where ring and rows of x will be
+        if (warps * (a.n_slots + 1) * 2 + a.pairs * 4 <= a.at_bars) return o + 1024;
+    }
+    return 0;
 }
 
 // Packing: eight weights (one 32-bit word) a thread, a group in group / 8 neighbouring lanes.
@@ -383,7 +712,7 @@ __global__ void __launch_bounds__(256) quant_pack_kernel(const T *w, long long l
 }  // namespace
 
 int quant_setup() {
-    return setup_one<__nv_bfloat16, 1>() | setup_one<__nv_bfloat16, 4>() | setup_one<__half, 1>() | setup_one<__half, 4>();
+    return setup_type<__nv_bfloat16>() | setup_type<__half>();
 }
 
 }  // namespace ops
@@ -398,9 +727,8 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
                                    const int32_t *slots, int32_t pairs, int32_t pairs_per_row, int32_t n_slots, int32_t n, int32_t k, int32_t group, void *y,
                                    int64_t ldy, void *cuda_stream) {
     if (!is_16bit(dtype) || (out_dtype != dtype && out_dtype != EW_FP32)) return refuse("4-bit product: x is bf16 or fp16, results of the same type or fp32");
-    if (bad_group(group, k)) return refuse("4-bit product: groups of 32, 64 or 128 weights that divide k");
-    if (pairs < 0 || pairs_per_row < 1 || pairs % pairs_per_row || n_slots < 1 || n_slots > kMaxSlots || n < 8 || n % 8 || (int64_t)n_slots * n > 0x7fffffff ||
-        (int64_t)n_slots * (k / group) > 0x7fffffff)
+    if (bad_group(group, k) || k > kMaxK) return refuse("4-bit product: groups of 32, 64 or 128 weights that divide k, k at most 16384");
+    if (pairs < 0 || pairs_per_row < 1 || pairs % pairs_per_row || n_slots < 1 || n_slots > kMaxSlots || n < 8 || n % 8 || (int64_t)n_slots * n > 0x7fffffff || (int64_t)kMaxPairs * ((n + kRows - 1) / kRows) > 0x7fffffff)
         return refuse("4-bit product: size out of range (n in multiples of 8, at most 2048 slots)");
     if (!slots && n_slots != 1) return refuse("4-bit product: without slot ids there is one matrix");
     if (ldx < k || (ldx & 7) || ldy < n || !q || !scales || (((uintptr_t)q | (uintptr_t)scales) & 15) || ((uintptr_t)slots & 3) ||
@@ -415,39 +743,35 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
     CUtensorMap mq, ms;
     const uint64_t qd[2] = {(uint64_t)k / 2, (uint64_t)n_slots * n}, qs[1] = {(uint64_t)k / 2};
     const uint64_t sd[2] = {(uint64_t)n, (uint64_t)n_slots * (k / group)}, ss[1] = {(uint64_t)n * 2};
-    const uint32_t qbox[2] = {128, 16}, sbox[2] = {16, (uint32_t)(kStageK / group)};
+    const uint32_t qbox[2] = {128, kRows}, sbox[2] = {kRows, (uint32_t)(kLineK / group)};
     if ((s = encode_map(*d, &mq, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, 2, qd, qs, qbox, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
     if ((s = encode_map(*d, &ms, CU_TENSOR_MAP_DATA_TYPE_UINT16, scales, 2, sd, ss, sbox, CU_TENSOR_MAP_SWIZZLE_NONE)) != EW_OK) return s;
     Args a = {};
-    a.x = (const uint8_t *)x;
-    a.out = y;
     a.err = d->err;
+    a.out = y;
     a.ldx = ldx;
     a.ldo = ldy;
     a.share = pairs_per_row;
     a.n = n;
     a.k = k;
     a.n_slots = n_slots;
-    a.tiles = (n + 15) / 16;
-    a.out_kind = out_dtype;
-    const int k_stages = (k + kStageK - 1) / kStageK;
+    a.out_fp32 = out_dtype == EW_FP32;
+    a.tiles = (n + kRows - 1) / kRows;
     for (int32_t p0 = 0; p0 < pairs; p0 += kMaxPairs) {
         a.pair0 = p0;
         a.pairs = pairs - p0 < kMaxPairs ? pairs - p0 : kMaxPairs;
+        a.x = (const uint8_t *)x + (size_t)(p0 / pairs_per_row) * ldx * 2;
+        a.lead = p0 % pairs_per_row;
         a.slots = slots ? slots + p0 : nullptr;
-        // A slot of few pairs needs one column of the MMA, a busy one up to four at a time.
-        const bool narrow = a.pairs <= 8 || a.pairs <= 2 * n_slots;
-        const long long live = a.pairs < n_slots ? a.pairs : n_slots, items = live * a.tiles;
-        // Too few tiles for all warps: several warps share one, each with a part of k.
-        a.split = 1;
-        while (a.split < kWarps && a.split < k_stages && items * a.split * 2 <= (long long)d->sm_count * kWarps) a.split *= 2;
-        const long long most_jobs = a.pairs / (narrow ? 8 : 32) + live, ctas = (most_jobs * a.tiles * a.split + kWarps - 1) / kWarps;
-        const int grid = (int)(ctas < d->sm_count ? ctas : d->sm_count);
+        // One column of eight pairs where a slot has four pairs or fewer on average, up to three otherwise: what a slot has
+        // more is another job, which reads its weights again.
+        const int nt = a.pairs <= 8 || a.pairs <= 4 * n_slots ? 1 : 3;
+        const int pieces = nt > 1 ? 0 : out_dtype == EW_FP32 ? 3 : 2, smem = lay_out(a, nt, group, pieces);
+        if (!smem) return refuse("4-bit product: k is too large for a row of x in shared memory");
+        const long long most = ((long long)a.pairs / a.job_rows + (a.pairs < n_slots ? a.pairs : n_slots)) * a.tiles;
+        const int grid = (int)(most < d->sm_count ? most : d->sm_count);
         cudaStream_t st = (cudaStream_t)cuda_stream;
-        if (dtype == EW_BF16)
-            s = narrow ? launch_group<__nv_bfloat16, 1>(group, mq, ms, a, grid, st) : launch_group<__nv_bfloat16, 4>(group, mq, ms, a, grid, st);
-        else
-            s = narrow ? launch_group<__half, 1>(group, mq, ms, a, grid, st) : launch_group<__half, 4>(group, mq, ms, a, grid, st);
+        s = dtype == EW_BF16 ? launch_type<__nv_bfloat16>(pieces, group, mq, ms, a, smem, grid, st) : launch_type<__half>(pieces, group, mq, ms, a, smem, grid, st);
         if (s != EW_OK) return s;
     }
     return EW_OK;

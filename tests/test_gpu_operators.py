@@ -15,9 +15,9 @@ pytestmark = pytest.mark.gpu
 BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
 
 
-def near(got, ref, mag, terms, what=""):
-    """Elementwise: half a step of the result's type plus the sum's own error (`mag` = sum of |products|)."""
-    tol = torch.finfo(got.dtype).eps / 2 * ref.abs() + (terms / 16 + 1) * 17 * 2.0 ** -23 * mag
+def near(got, ref, mag, terms, what="", more=0.0):
+    """Elementwise: half a step of the result's type plus the sum's own error (`mag` = sum of |products|) plus `more`."""
+    tol = torch.finfo(got.dtype).eps / 2 * ref.abs() + (terms / 16 + 1) * 17 * 2.0 ** -23 * mag + more
     if got.dtype == FP16:
         tol = tol + 2.0 ** -25                          # half a step of the subnormals
     off = (got.double() - ref).abs()
@@ -140,7 +140,10 @@ def check_quant(slots, n_slots, n, k, group, dtype=BF16, out_dtype=None, per_row
             assert not y[at].any()
             continue
         xd = x[[i // step for i in at]].double()
-        near(y[at], xd @ w[s].t(), xd.abs() @ w[s].abs().t(), 2 * k, ("slot", s))
+        # x enters as fixed-point numbers whose largest in a group is above 16319 (16-bit results) or 4177919 (fp32): rounding
+        # them costs at most 1/2, i.e. 2^-15 (2^-23) of the group's largest x, a weight
+        most = xd.view(len(at), k // group, group).abs().amax(2, keepdim=True).expand(-1, -1, group).reshape(len(at), k)
+        near(y[at], xd @ w[s].t(), xd.abs() @ w[s].abs().t(), 2 * k, ("slot", s), 2.0 ** (-23 if y.dtype == FP32 else -15) * (most @ w[s].abs().t()))
 
 
 def some_slots(tokens, per, n_slots, seed=0):
