@@ -300,15 +300,25 @@ class Pool:
 
 
 # ---------------------------------------------------------------------------------------------------------------------
-# Stand-alone operators (no pool): argument checks, output allocation, one library call on the current stream.
-_DTYPE = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+# Stand-alone operators (no pool): argument checks, output allocation, one library call on the current stream.  A small
+# call takes the GPU less time than the host, so the checks of a good call are a handful of comparisons; only when one of
+# them fails does `_on` find out which and say so.
+class _Torch:
+    """What the operators need of torch, resolved on first use (the package imports without it)."""
+    ready = False
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+        cls.int32, cls.float32, cls.uint8 = torch.int32, torch.float32, torch.uint8
+        cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        cls.ready = True
+        return cls
 
 
-def _dtype(t) -> int:
-    code = _DTYPE.get(str(t))
-    if code is None:
-        raise ValueError(f"dtype {t} is not supported: bfloat16, float16 (results also float32)")
-    return code
+def _torch():
+    return _Torch if _Torch.ready else _Torch.load()
 
 
 def _on(t, like=None, ndim=2, name="operand", dtype=None):
@@ -324,35 +334,49 @@ def _on(t, like=None, ndim=2, name="operand", dtype=None):
     return t
 
 
-def _stride(t, dim) -> int:
-    """Elements between the rows (or matrices) of `t`; a dimension of length one has no stride of its own."""
-    if t.shape[dim] > 1:
-        return t.stride(dim)
-    n = t.shape[-1] if dim in (-2, t.dim() - 2) else t.shape[-2] * _stride(t, -2)
-    return (n + 7) // 8 * 8
+def _code(T, dtype) -> int:
+    code = T.codes.get(dtype)
+    if code is None:
+        raise ValueError(f"dtype {dtype} is not supported: bfloat16, float16 (results also float32)")
+    return code
 
 
-def _width(t) -> int:
-    """Elements between the rows of a matrix (its width where it has one row only)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _good(t, dev, dtype, ndim) -> bool:
+    """Whether `t` is what `_on` wants (contiguity of the last dimension apart)."""
+    return t.get_device() == dev and t.dtype is dtype and t.dim() == ndim
 
 
-def _offsets(offsets, like):
-    _on(offsets, like, 1, "offsets")
-    if str(offsets.dtype) != "torch.int32" or offsets.shape[0] < 2 or offsets.stride(0) != 1:
+def _matrix(t, dev, dtype, name, like):
+    """(rows, width, elements between rows) of a matrix; one row alone has no stride of its own."""
+    if not _good(t, dev, dtype, 2) or dev < 0:
+        _on(t, like, 2, name, dtype)
+    (rows, width), (ld, one) = t.shape, t.stride()
+    if one != 1 and width > 1 and rows:
+        _on(t, like, 2, name, dtype)
+    return rows, width, ld if rows > 1 else (width + 7) // 8 * 8
+
+
+def _matrices(t, dev, dtype, name, like):
+    """(matrices, rows, width, elements between rows, between matrices)."""
+    if not _good(t, dev, dtype, 3) or dev < 0:
+        _on(t, like, 3, name, dtype)
+    (g, n, k), (stride, ld, one) = t.shape, t.stride()
+    if one != 1 and k > 1:
+        _on(t, like, 3, name, dtype)
+    ld = ld if n > 1 else (k + 7) // 8 * 8
+    return g, n, k, ld, stride if g > 1 else n * ld
+
+
+def _offsets(offsets, dev, T, like):
+    if offsets.get_device() != dev or offsets.dtype is not T.int32 or offsets.dim() != 1 or offsets.shape[0] < 2 or offsets.stride(0) != 1:
+        _on(offsets, like, 1, "offsets")
         raise ValueError("offsets: a contiguous int32 tensor with one more entry than groups is wanted")
     return offsets.shape[0] - 1
 
 
-def _stream_of(device):
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream
-
-
 def _result(out, shape, dtype, like, name="out"):
-    import torch
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     _on(out, like, len(shape), name)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise ValueError(f"{name}: {tuple(shape)} of {dtype} is wanted, got {tuple(out.shape)} of {out.dtype}")
@@ -360,18 +384,26 @@ def _result(out, shape, dtype, like, name="out"):
 
 
 def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
-    _on(a, name="the rows' operand")
-    _on(w, a, 3, "w", a.dtype)
-    groups, n, k = w.shape
-    if _offsets(offsets, a) != groups:
+    T, dev, dtype = _torch(), a.get_device(), a.dtype
+    code = _code(T, dtype)
+    rows, width, lda = _matrix(a, dev, dtype, "the rows' operand", None)
+    groups, n, k, ldw, stride = _matrices(w, dev, dtype, "w", a)
+    if _offsets(offsets, dev, T, a) != groups:
         raise ValueError(f"offsets has {offsets.shape[0]} entries for {groups} groups")
-    if a.shape[1] != (n if grad else k):
-        raise ValueError(f"rows of {a.shape[1]} do not match w of {tuple(w.shape)}")
-    rows = a.shape[0]
-    out = _result(out, (rows, k if grad else n), out_dtype or (a.dtype if out is None else out.dtype), a)
-    dev = a.device
-    _check(fn(dev.index, _dtype(a.dtype), _dtype(out.dtype), a.data_ptr(), _stride(a, 0), w.data_ptr(), _stride(w, 1),
-              _stride(w, 0), offsets.data_ptr(), rows, groups, n, k, out.data_ptr(), _stride(out, 0), _stream_of(dev)), where)
+    if width != (n if grad else k):
+        raise ValueError(f"rows of {width} do not match w of {tuple(w.shape)}")
+    if out_dtype is None:
+        out_dtype = dtype if out is None else out.dtype
+    wide = k if grad else n
+    if out is None:
+        out, ldo = a.new_empty((rows, wide), dtype=out_dtype), wide
+    else:
+        out = _result(out, (rows, wide), out_dtype, a)
+        ldo = out.stride(0) if rows > 1 else wide
+    rc = fn(dev, code, _code(T, out_dtype), a.data_ptr(), lda, w.data_ptr(), ldw, stride, offsets.data_ptr(), rows, groups, n, k,
+            out.data_ptr(), ldo, T.stream(dev))
+    if rc:
+        _check(rc, where)
     return out
 
 
@@ -390,38 +422,44 @@ def grouped_mm_dx(dy, w, offsets, out=None, out_dtype=None):
 def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
     """The gradient of `grouped_mm` with respect to w: dw[g] = dy_g^T x_g -> [groups, n, k]; a group without rows gets zeros.
     accumulate: adds to `out` instead (required then), as over the steps of a large batch."""
-    _on(dy, name="dy")
-    _on(x, dy, 2, "x", dy.dtype)
-    groups = _offsets(offsets, dy)
-    (rows, n), k = dy.shape, x.shape[1]
-    if x.shape[0] != rows:
-        raise ValueError(f"dy has {rows} rows, x {x.shape[0]}")
+    T, dev, dtype = _torch(), dy.get_device(), dy.dtype
+    code = _code(T, dtype)
+    rows, n, lddy = _matrix(dy, dev, dtype, "dy", None)
+    x_rows, k, ldx = _matrix(x, dev, dtype, "x", dy)
+    groups = _offsets(offsets, dev, T, dy)
+    if x_rows != rows:
+        raise ValueError(f"dy has {rows} rows, x {x_rows}")
     if accumulate and out is None:
         raise ValueError("accumulate adds to `out`: pass it")
-    out = _result(out, (groups, n, k), out_dtype or (dy.dtype if out is None else out.dtype), dy)
-    dev = dy.device
-    _check(lib().ew_grouped_mm_dw(dev.index, _dtype(dy.dtype), _dtype(out.dtype), dy.data_ptr(), _stride(dy, 0), x.data_ptr(),
-                                  _stride(x, 0), offsets.data_ptr(), rows, groups, n, k, int(accumulate), out.data_ptr(),
-                                  _stride(out, 1), _stride(out, 0), _stream_of(dev)), "ew_grouped_mm_dw")
+    if out_dtype is None:
+        out_dtype = dtype if out is None else out.dtype
+    if out is None:
+        out, ldo, stride = dy.new_empty((groups, n, k), dtype=out_dtype), k, n * k
+    else:
+        out = _result(out, (groups, n, k), out_dtype, dy)
+        ldo = out.stride(1) if n > 1 else k
+        stride = out.stride(0) if groups > 1 else n * ldo
+    rc = lib().ew_grouped_mm_dw(dev, code, _code(T, out_dtype), dy.data_ptr(), lddy, x.data_ptr(), ldx, offsets.data_ptr(), rows, groups, n, k,
+                                1 if accumulate else 0, out.data_ptr(), ldo, stride, T.stream(dev))
+    if rc:
+        _check(rc, "ew_grouped_mm_dw")
     return out
 
 
 def quant_pack(w, group, out=None):
     """4-bit weights and group scales of w [slots, n, k] (bf16 or fp16) for `quant_mv`: (q uint8 [slots, n, k/2], scales
     [slots, k/group, n] of w's type).  The header has the format."""
-    import torch
-    _on(w, ndim=3, name="w")
-    slots, n, k = w.shape
+    T, dev, dtype = _torch(), w.get_device(), w.dtype
+    code = _code(T, dtype)
+    slots, n, k, ld, stride = _matrices(w, dev, dtype, "w", None)
     if group not in (32, 64, 128) or k % group:
         raise ValueError(f"groups of 32, 64 or 128 weights that divide k = {k} are wanted, got {group}")
     q, scales = out or (None, None)
-    q = _result(q, (slots, n, k // 2), torch.uint8, w, "q")
-    scales = _result(scales, (slots, k // group, n), w.dtype, w, "scales")
+    q = _result(q, (slots, n, k // 2), T.uint8, w, "q")
+    scales = _result(scales, (slots, k // group, n), dtype, w, "scales")
     if not (q.is_contiguous() and scales.is_contiguous()):
         raise ValueError("q and scales are contiguous")
-    dev = w.device
-    _check(lib().ew_quant_pack(dev.index, _dtype(w.dtype), w.data_ptr(), _stride(w, 1), _stride(w, 0), slots, n, k, group,
-                               q.data_ptr(), scales.data_ptr(), _stream_of(dev)), "ew_quant_pack")
+    _check(lib().ew_quant_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, group, q.data_ptr(), scales.data_ptr(), T.stream(dev)), "ew_quant_pack")
     return q, scales
 
 
@@ -429,66 +467,88 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     """y[p] = x[p // per_row] W[slots[p]]^T with the 4-bit weights of `quant_pack`.  x [rows, k]; slots int32, one entry a
     pair in any shape ([tokens, top_k] as the router writes it), per_row = pairs / rows of x; negative: a row of zeros.
     slots None: one matrix, a pair a row.  -> [pairs, n]; out_dtype: x's type or float32."""
-    import torch
-    _on(x, name="x")
-    _on(q, x, 3, "q", torch.uint8)
-    _on(scales, x, 3, "scales", x.dtype)
-    (n_slots, n, half), (rows, k), groups = q.shape, x.shape, scales.shape[1]
-    if half * 2 != k or groups < 1 or k % groups or tuple(scales.shape) != (n_slots, groups, n) or not (q.is_contiguous() and scales.is_contiguous()):
+    T, dev, dtype = _torch(), x.get_device(), x.dtype
+    code = _code(T, dtype)
+    rows, k, ldx = _matrix(x, dev, dtype, "x", None)
+    if not _good(q, dev, T.uint8, 3):
+        _on(q, x, 3, "q", T.uint8)
+    if not _good(scales, dev, dtype, 3):
+        _on(scales, x, 3, "scales", dtype)
+    (n_slots, n, half), (s_slots, groups, s_n) = q.shape, scales.shape
+    if half * 2 != k or groups < 1 or k % groups or s_slots != n_slots or s_n != n or not (q.is_contiguous() and scales.is_contiguous()):
         raise ValueError(f"x {tuple(x.shape)}, q {tuple(q.shape)} and scales {tuple(scales.shape)} do not belong together")
-    pairs = rows
+    pairs, slots_at, per_row = rows, None, 1
     if slots is not None:
-        if not slots.is_cuda or slots.device != x.device or slots.dtype != torch.int32 or not slots.is_contiguous():
+        if slots.get_device() != dev or slots.dtype is not T.int32 or not slots.is_contiguous():
             raise ValueError("slots: a contiguous int32 tensor on x's device is wanted")
-        pairs = slots.numel()
+        pairs, slots_at = slots.numel(), slots.data_ptr()
         if pairs and (rows == 0 or pairs % rows):
             raise ValueError(f"{pairs} pairs for {rows} rows of x")
-    out = _result(out, (pairs, n), out_dtype or (x.dtype if out is None else out.dtype), x)
-    dev = x.device
-    _check(lib().ew_quant_mv(dev.index, _dtype(x.dtype), _dtype(out.dtype), x.data_ptr(), _stride(x, 0), q.data_ptr(), scales.data_ptr(),
-                             None if slots is None else slots.data_ptr(), pairs, max(1, pairs // rows if rows else 1), n_slots, n, k,
-                             k // groups, out.data_ptr(), _stride(out, 0), _stream_of(dev)), "ew_quant_mv")
+        per_row = pairs // rows if pairs else 1
+    if out_dtype is None:
+        out_dtype = dtype if out is None else out.dtype
+    if out is None:
+        out, ldo = x.new_empty((pairs, n), dtype=out_dtype), n
+    else:
+        out = _result(out, (pairs, n), out_dtype, x)
+        ldo = out.stride(0) if pairs > 1 else n
+    rc = lib().ew_quant_mv(dev, code, _code(T, out_dtype), x.data_ptr(), ldx, q.data_ptr(), scales.data_ptr(), slots_at, pairs, per_row, n_slots, n, k,
+                           k // groups, out.data_ptr(), ldo, T.stream(dev))
+    if rc:
+        _check(rc, "ew_quant_mv")
     return out
 
 
-def _row_weights(p, h):
-    import torch
+def _row_weights(p, dev, T, rows, like):
     if p is None:
         return None
-    _on(p, h, 1, "row_weights", torch.float32)
-    if p.shape[0] != h.shape[0]:
-        raise ValueError(f"{p.shape[0]} row weights for {h.shape[0]} rows")
+    if not _good(p, dev, T.float32, 1) or not p.is_contiguous():
+        _on(p, like, 1, "row_weights", T.float32)
+    if p.shape[0] != rows:
+        raise ValueError(f"{p.shape[0]} row weights for {rows} rows")
     return p.data_ptr()
 
 
 def swiglu(h, row_weights=None, out=None):
     """row_weights[r] * silu(h[r, :inter]) * h[r, inter:] -> [rows, inter]: the activation between an expert's linears, the
     routing weights (float32, or None) folded in."""
-    _on(h, name="h")
-    rows, two = h.shape
+    T, dev, dtype = _torch(), h.get_device(), h.dtype
+    code = _code(T, dtype)
+    rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     if two < 2 or two % 2:
         raise ValueError(f"h holds a gate and an up block side by side: an even width is wanted, got {two}")
-    p = _row_weights(row_weights, h)
-    out = _result(out, (rows, two // 2), h.dtype, h)
-    dev = h.device
-    _check(lib().ew_swiglu(dev.index, _dtype(h.dtype), h.data_ptr(), _width(h), p, rows, two // 2, out.data_ptr(), _width(out), _stream_of(dev)), "ew_swiglu")
+    inter = two // 2
+    p = _row_weights(row_weights, dev, T, rows, h)
+    if out is None:
+        out, ldo = h.new_empty((rows, inter)), inter
+    else:
+        out = _result(out, (rows, inter), dtype, h)
+        ldo = out.stride(0) if rows > 1 else inter
+    rc = lib().ew_swiglu(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, inter, out.data_ptr(), ldo, T.stream(dev))
+    if rc:
+        _check(rc, "ew_swiglu")
     return out
 
 
 def swiglu_grad(dact, h, row_weights=None, out=None):
     """The gradient of `swiglu`: dh [rows, 2 inter], and with row_weights also theirs, float32 [rows] -> dh or (dh, dp)."""
-    import torch
-    _on(h, name="h")
-    _on(dact, h, 2, "dact", h.dtype)
-    rows, two = h.shape
-    if two < 2 or tuple(dact.shape) != (rows, two // 2) or two % 2:
+    T, dev, dtype = _torch(), h.get_device(), h.dtype
+    code = _code(T, dtype)
+    rows, two, ldh = _matrix(h, dev, dtype, "h", None)
+    d_rows, inter, ldd = _matrix(dact, dev, dtype, "dact", h)
+    if two < 2 or d_rows != rows or inter * 2 != two:
         raise ValueError(f"dact {tuple(dact.shape)} does not belong to h {tuple(h.shape)}")
-    p = _row_weights(row_weights, h)
-    out = _result(out, (rows, two), h.dtype, h)
-    dev = h.device
-    dp = None if p is None else torch.empty((rows,), dtype=torch.float32, device=dev)
-    _check(lib().ew_swiglu_grad(dev.index, _dtype(h.dtype), dact.data_ptr(), _width(dact), h.data_ptr(), _width(h), p, rows, two // 2, out.data_ptr(),
-                                _width(out), None if dp is None else dp.data_ptr(), _stream_of(dev)), "ew_swiglu_grad")
+    p = _row_weights(row_weights, dev, T, rows, h)
+    if out is None:
+        out, ldo = h.new_empty((rows, two)), two
+    else:
+        out = _result(out, (rows, two), dtype, h)
+        ldo = out.stride(0) if rows > 1 else two
+    dp = None if p is None else h.new_empty((rows,), dtype=T.float32)
+    rc = lib().ew_swiglu_grad(dev, code, dact.data_ptr(), ldd if rows > 1 else inter, h.data_ptr(), ldh if rows > 1 else two, p, rows, inter, out.data_ptr(),
+                              ldo, None if dp is None else dp.data_ptr(), T.stream(dev))
+    if rc:
+        _check(rc, "ew_swiglu_grad")
     return out if dp is None else (out, dp)
 
 

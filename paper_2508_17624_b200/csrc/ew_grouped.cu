@@ -28,7 +28,7 @@ namespace ops {
 namespace {
 using namespace tc;
 
-enum Way { kProduct = 0, kInputGrad = 1, kWeightGrad = 2 };
+enum Way { kProduct = 0, kInputGrad = 1, kWeightGrad = 2, kWeightAdd = 3 };      // the last: added to what is there
 
 constexpr int kThreads = 224;                          // TMA, MMA, four epilogue warps, relay (weight gradient)
 constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one stage
@@ -48,7 +48,6 @@ struct Args {
     int t_size;             // product, dx: length of the summed axis
     int f_tiles, c_tiles;
     int out_kind;           // ew_dtype_t
-    int accumulate;
     int fp16;               // operand type
     int stages;
     int table_bytes;
@@ -135,18 +134,41 @@ __device__ __forceinline__ void arrive_leader(uint32_t bar) {
     else mbar_arrive_leader(bar);
 }
 
-// One column of the accumulator (32 neighbouring f of one output row, one per lane) into the output row.
-__device__ __forceinline__ void put(void *out, size_t at, float v, int kind, int accumulate) {
-    if (kind == EW_FP32) {
-        float *p = reinterpret_cast<float *>(out) + at;
-        *p = accumulate ? *p + v : v;
-    } else if (kind == EW_BF16) {
-        __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(out) + at;
-        *p = __float2bfloat16_rn(accumulate ? __bfloat162float(*p) + v : v);
+// Columns of the accumulator into `lim` output rows: a warp writes 32 neighbouring f of a row at a time.
+template <class T>
+__device__ __forceinline__ void store_columns(T *p, long long ldo, const uint32_t (&v)[32], int lim) {
+    if (lim == 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j, p += ldo) *p = (T)__uint_as_float(v[j]);
     } else {
-        __half *p = reinterpret_cast<__half *>(out) + at;
-        *p = __float2half_rn(accumulate ? __half2float(*p) + v : v);
+#pragma unroll
+        for (int j = 0; j < 32; ++j, p += ldo)
+            if (j < lim) *p = (T)__uint_as_float(v[j]);
     }
+}
+// The same added to what is there, eight rows at a time (their old values are asked for together).
+template <class T>
+__device__ __forceinline__ void add_columns(T *p, long long ldo, const uint32_t (&v)[32], int lim) {
+#pragma unroll
+    for (int j0 = 0; j0 < 32; j0 += 8) {
+        float old[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j0 + j < lim) old[j] = (float)p[j * ldo];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j0 + j < lim) p[j * ldo] = (T)(old[j] + __uint_as_float(v[j0 + j]));
+        p += 8 * ldo;
+    }
+}
+template <class T, bool ADD>
+__device__ __forceinline__ void put_columns(void *out, size_t at, long long ldo, const uint32_t (&v)[32], int lim) {
+    if (ADD) add_columns(reinterpret_cast<T *>(out) + at, ldo, v, lim);
+    else store_columns(reinterpret_cast<T *>(out) + at, ldo, v, lim);
+}
+__device__ __forceinline__ void store_zero(void *out, size_t at, int kind) {
+    if (kind == EW_FP32) reinterpret_cast<float *>(out)[at] = 0.f;
+    else reinterpret_cast<uint16_t *>(out)[at] = 0;
 }
 
 template <int CG, int NT, int WAY>
@@ -154,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                        const __grid_constant__ CUtensorMap map_b_big, const __grid_constant__ Args a) {
     using C = Cfg<CG, NT>;
-    constexpr bool DW = WAY == kWeightGrad;
+    constexpr bool DW = WAY == kWeightGrad || WAY == kWeightAdd;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -392,8 +414,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             const bool f_ok = f < a.f_size;
             const size_t at = (DW ? (size_t)it.g * a.group_out : 0) + (size_t)it.row0 * a.ldo + f;
             if (DW && it.kb == 0) {
-                if (f_ok && !a.accumulate)
-                    for (int j = 0; j < it.cols; ++j) put(a.out, at + (size_t)j * a.ldo, 0.f, a.out_kind, 0);
+                if (f_ok && WAY == kWeightGrad)
+                    for (int j = 0; j < it.cols; ++j) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
                 continue;
             }
             if (!(ok = mbar_wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
@@ -406,21 +428,10 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 tc_wait_ld();
                 const int lim = min(32, it.cols - c0);
                 if (f_ok) {
-                    if (a.out_kind == EW_FP32 && !a.accumulate) {
-                        float *p = reinterpret_cast<float *>(a.out) + at + (size_t)c0 * a.ldo;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j < lim) p[(size_t)j * a.ldo] = __uint_as_float(v[j]);
-                    } else if (a.out_kind == EW_BF16 && !a.accumulate) {
-                        __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(a.out) + at + (size_t)c0 * a.ldo;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j < lim) p[(size_t)j * a.ldo] = __float2bfloat16_rn(__uint_as_float(v[j]));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j < lim) put(a.out, at + (size_t)(c0 + j) * a.ldo, __uint_as_float(v[j]), a.out_kind, a.accumulate);
-                    }
+                    const size_t to = at + (size_t)c0 * a.ldo;
+                    if (a.out_kind == EW_FP32) put_columns<float, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
+                    else if (a.out_kind == EW_BF16) put_columns<__nv_bfloat16, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
+                    else put_columns<__half, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
                 }
             }
             tc_fence_before();
@@ -546,7 +557,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
 
 int grouped_setup() {
     return setup_one<1, 64, kProduct>() | setup_one<1, 64, kInputGrad>() | setup_one<1, 128, kProduct>() | setup_one<1, 128, kInputGrad>() |
-           setup_one<2, 256, kProduct>() | setup_one<2, 256, kInputGrad>() | setup_one<2, 256, kWeightGrad>();
+           setup_one<2, 256, kProduct>() | setup_one<2, 256, kInputGrad>() | setup_one<2, 256, kWeightGrad>() | setup_one<2, 256, kWeightAdd>();
 }
 
 }  // namespace ops
@@ -609,7 +620,7 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
     a.f_tiles = (k + 255) / 256;
     a.c_tiles = (n + 255) / 256;
     a.out_kind = out_dtype;
-    a.accumulate = accumulate != 0;
     a.fp16 = dtype == EW_FP16;
-    return launch<2, 256, kWeightGrad>(*d, ma, mb, mb, a, (long long)groups * a.c_tiles * a.f_tiles, st);
+    const long long items = (long long)groups * a.c_tiles * a.f_tiles;
+    return accumulate ? launch<2, 256, kWeightAdd>(*d, ma, mb, mb, a, items, st) : launch<2, 256, kWeightGrad>(*d, ma, mb, mb, a, items, st);
 }
