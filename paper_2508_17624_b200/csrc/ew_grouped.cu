@@ -30,7 +30,9 @@ using namespace tc;
 
 enum Way { kProduct = 0, kInputGrad = 1, kWeightGrad = 2, kWeightAdd = 3 };      // the last: added to what is there
 
-constexpr int kThreads = 224;                          // TMA, MMA, four epilogue warps, relay (weight gradient)
+constexpr int kEpilogueWarps = 8;                      // two to each quarter of the TMEM lanes, taking turns at the columns
+constexpr int kRelayWarp = 2 + kEpilogueWarps;
+constexpr int kThreads = (kRelayWarp + 1) * 32;        // TMA, MMA, epilogue, relay (weight gradient)
 constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one stage
 constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
 constexpr int kSmemLimit = 227 * 1024;
@@ -48,6 +50,7 @@ struct Args {
     int t_size;             // product, dx: length of the summed axis
     int f_tiles, c_tiles;
     int out_kind;           // ew_dtype_t
+    int a_pairs, b_pairs;   // operands with a contiguous f (c): 1 = two 64-wide boxes come in one copy
     int fp16;               // operand type
     int stages;
     int table_bytes;
@@ -62,6 +65,11 @@ struct Cfg {
     static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
     static constexpr int kStep = 16 * CG;                                    // granularity of an MMA's N
 };
+
+// The row operand's tensor maps: boxes of 32, 64, 96 and 128 rows (weight gradient: one map).  A stage's rows come in one
+// copy of about their number: several small copies a stage cost up to a fifth of the time of a large product, and a 128-row
+// box for 96 rows a third more bytes.
+struct RowMaps { CUtensorMap m[4]; };
 
 struct Item {
     int g, f0, row0, cols, kb, tail;      // cols: output rows (c) of this item; kb: k-blocks; tail: live rows of the last one (dw)
@@ -80,32 +88,39 @@ __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr) {
     return d;
 }
 
-__device__ __forceinline__ bool try_cluster(uint32_t bar, uint32_t parity) {
+// Bounded waits.  The thread sleeps in the barrier's hardware wait for up to kNap at a time: the products run at the GPU's
+// power limit, where warps that poll cost clock.
+constexpr uint32_t kNapNs = 4000;
+template <bool PEER>
+__device__ __forceinline__ bool try_nap(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if constexpr (PEER)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
     return ok != 0;
 }
-// bounded wait on a barrier that may receive arrivals from the peer CTA
-template <int CG>
-__device__ __forceinline__ bool wait_any(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
-    if constexpr (CG == 1) return mbar_wait(bar, parity, abort_flag, err);
-    if (try_cluster(bar, parity)) return true;
+// PEER: on a barrier that receives arrivals from the peer CTA
+template <bool PEER>
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    if (try_nap<PEER>(bar, parity)) return true;
     const long long t0 = clock64();
-    for (uint32_t it = 1;; ++it) {
-        if (try_cluster(bar, parity)) return true;
-        if ((it & 63u) == 0) {
-            if (*abort_flag) return false;
-            if (clock64() - t0 > kWaitLimitCycles) {
-                *abort_flag = 1;
-                atomicOr(err, 2);
-                return false;
-            }
+    for (;;) {
+        if (try_nap<PEER>(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (clock64() - t0 > kWaitLimitCycles) {
+            *abort_flag = 1;
+            atomicOr(err, 2);
+            return false;
         }
     }
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    int ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = wait_on<false>(bar, parity, abort_flag, err) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
 template <int CG>
@@ -117,6 +132,15 @@ template <int CG>
 __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, uint32_t bar) {
     if constexpr (CG == 1) tma_load_3d(dst, m, x, y, z, bar);
     else tma2_load_3d(dst, m, x, y, z, bar);
+}
+template <int CG>
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, int w, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -137,13 +161,23 @@ __device__ __forceinline__ void arrive_leader(uint32_t bar) {
 // Columns of the accumulator into `lim` output rows: a warp writes 32 neighbouring f of a row at a time.
 template <class T>
 __device__ __forceinline__ void store_columns(T *p, long long ldo, const uint32_t (&v)[32], int lim) {
+    // eight addresses that do not wait for one another
+    T *q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = p + j * ldo;
+    const long long step = 8 * ldo;
     if (lim == 32) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j, p += ldo) *p = (T)__uint_as_float(v[j]);
+        for (int j = 0; j < 32; ++j) {
+            *q[j & 7] = (T)__uint_as_float(v[j]);
+            q[j & 7] += step;
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j, p += ldo)
-            if (j < lim) *p = (T)__uint_as_float(v[j]);
+        for (int j = 0; j < 32; ++j) {
+            if (j < lim) *q[j & 7] = (T)__uint_as_float(v[j]);
+            q[j & 7] += step;
+        }
     }
 }
 // The same added to what is there, eight rows at a time (their old values are asked for together).
@@ -173,8 +207,7 @@ __device__ __forceinline__ void store_zero(void *out, size_t at, int kind) {
 
 template <int CG, int NT, int WAY>
 __global__ void __launch_bounds__(kThreads, 1)
-grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                       const __grid_constant__ CUtensorMap map_b_big, const __grid_constant__ Args a) {
+grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ Args a) {
     using C = Cfg<CG, NT>;
     constexpr bool DW = WAY == kWeightGrad || WAY == kWeightAdd;
     extern __shared__ uint8_t smem_raw[];
@@ -201,12 +234,12 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_tfull + 8 * i, 1);
-            mbar_init(bar_tempty + 8 * i, 4 * CG);
+            mbar_init(bar_tempty + 8 * i, kEpilogueWarps * CG);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_map(&map_a);
-        prefetch_map(&map_b);
+        prefetch_map(&map_b.m[DW ? 0 : C::kBRows / 32 - 1]);
     }
     if (warp == 1) {
         if constexpr (CG == 1) {
@@ -308,12 +341,12 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 const int n_cta = n / CG;                                    // c of this item that each CTA stages
                 const int f = it.f0 + (int)rank * 128;
                 const int c = it.row0 + (DW ? (int)rank * (NT / CG) : (int)rank * n_cta);
-                const bool big = !DW && n_cta > 64 && C::kBRows >= 128;
-                const int boxes = DW ? (NT / CG) / 64 : (n_cta + kChunkRows - 1) / kChunkRows;
-                const uint32_t b_bytes = DW ? (uint32_t)(NT / CG) * kBlockK * 2 : big ? 128 * kBlockK * 2 : boxes * kChunkBytes;
+                const int boxes = DW ? 0 : (n_cta + 31) / 32;                // of 32 rows
+                const CUtensorMap *mb = &map_b.m[DW ? 0 : boxes - 1];
+                const uint32_t b_bytes = DW ? (uint32_t)(NT / CG) * kBlockK * 2 : boxes * kChunkBytes;
                 const int first = DW ? t_lo[it.g] : 0;
                 for (int kb = 0; kb < it.kb; ++kb) {
-                    if (!(ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1, abort_flag, a.err))) break;
+                    if (!(ok = wait_on<false>(bar_empty + 8 * stage, phase ^ 1, abort_flag, a.err))) break;
                     const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
                     // the weight gradient's copies are counted on each CTA's own barrier (its relay warp reads them), the
                     // others' on the leader's
@@ -323,18 +356,25 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     if (WAY == kProduct) {
                         load_3d<CG>(sa, &map_a, t, f, it.g, bar);
                     } else if (WAY == kInputGrad) {
-                        load_3d<CG>(sa, &map_a, f, t, it.g, bar);
-                        load_3d<CG>(sa + 8192, &map_a, f + 64, t, it.g, bar);
+                        if (a.a_pairs) {
+                            load_4d<CG>(sa, &map_a, 0, t, f >> 6, it.g, bar);
+                        } else {
+                            load_3d<CG>(sa, &map_a, f, t, it.g, bar);
+                            load_3d<CG>(sa + 8192, &map_a, f + 64, t, it.g, bar);
+                        }
+                    } else if (a.a_pairs) {
+                        tma_load_3d(sa, &map_a, 0, t, f >> 6, bar);
                     } else {
                         tma_load_2d(sa, &map_a, f, t, bar);
                         tma_load_2d(sa + 8192, &map_a, f + 64, t, bar);
                     }
-                    if (DW) {
-                        for (int j = 0; j < boxes; ++j) tma_load_2d(sb + j * 8192, &map_b, c + j * 64, t, bar);
-                    } else if (big) {
-                        load_2d<CG>(sb, &map_b_big, t, c, bar);
+                    if (!DW) {
+                        load_2d<CG>(sb, mb, t, c, bar);
+                    } else if (a.b_pairs) {
+                        tma_load_3d(sb, mb, 0, t, c >> 6, bar);
                     } else {
-                        for (int j = 0; j < boxes; ++j) load_2d<CG>(sb + j * kChunkBytes, &map_b, t, c + j * kChunkRows, bar);
+                        tma_load_2d(sb, mb, c, t, bar);
+                        tma_load_2d(sb + 8192, mb, c + 64, t, bar);
                     }
                     if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
                 }
@@ -354,11 +394,11 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 if (DW && it.kb == 0) continue;                              // an empty group: the epilogue writes its zeros
                 const int n = DW ? NT : (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
-                if (!(ok = wait_any<CG>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
+                if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
                 tc_fence_after();
                 const uint32_t d = tmem_base + acc * NT;
                 for (int kb = 0; kb < it.kb; ++kb) {
-                    if (!(ok = wait_any<CG>(bar_in + 8 * stage, phase, abort_flag, a.err))) break;
+                    if (!(ok = wait_on<CG == 2>(bar_in + 8 * stage, phase, abort_flag, a.err))) break;
                     tc_fence_after();
                     const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
                     const uint64_t da = WAY == kProduct ? desc_kmajor(sa) : desc_mnmajor(sa);
@@ -378,7 +418,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 if (++acc == 2) { acc = 0; acc_phase ^= 1; }
             }
         }
-    } else if (warp == 6) {
+    } else if (warp == kRelayWarp) {
         // ------------------------------------------------------------------ relay (weight gradient, both CTAs)
         // The last k-block of a group ends inside a tile, and the rows behind it are the next group's: up to the end of
         // the MMA step both operands are set to zero (both: a NaN there would survive a zero on the other side).
@@ -388,7 +428,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             for (int i = unit; i < n_items && ok; i += units) {
                 const Item it = item_at(i);
                 for (int kb = 0; kb < it.kb; ++kb) {
-                    if (!(ok = mbar_wait_warp(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
+                    if (!(ok = wait_warp(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
                     if (kb == it.kb - 1 && (it.tail & 15)) {
                         const int from = it.tail * 128, to = ((it.tail + 15) & ~15) * 128;
                         uint8_t *tile = smem_al + stage * C::kStageBytes;
@@ -404,8 +444,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..5 of each CTA)
-        const int lg = warp & 3;                                             // the TMEM lanes this warp may read
+        // ------------------------------------------------------------------ epilogue (warps 2..9 of each CTA)
+        const int lg = warp & 3, turn = (warp - 2) >> 2;                     // the TMEM lanes this warp may read; its columns
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
         for (int i = unit; i < n_items && ok; i += units) {
@@ -415,14 +455,14 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             const size_t at = (DW ? (size_t)it.g * a.group_out : 0) + (size_t)it.row0 * a.ldo + f;
             if (DW && it.kb == 0) {
                 if (f_ok && WAY == kWeightGrad)
-                    for (int j = 0; j < it.cols; ++j) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
+                    for (int j = turn; j < it.cols; j += 2) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
                 continue;
             }
-            if (!(ok = mbar_wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
+            if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
             tc_fence_after();
             const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
 #pragma unroll 1
-            for (int c0 = 0; c0 < it.cols; c0 += 32) {
+            for (int c0 = 32 * turn; c0 < it.cols; c0 += 64) {
                 uint32_t v[32];
                 tc_ld32(t0 + c0, v);                   // columns behind the item's last are in the accumulator set, not stored
                 tc_wait_ld();
@@ -461,7 +501,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
 constexpr int kBarBytes = (3 * kMaxStages + 6) * 8;
 
 template <int CG, int NT, int WAY>
-ew_status_t launch(const Device &d, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mbb, Args a, long long max_items,
+ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, long long max_items,
                    cudaStream_t st) {
     using C = Cfg<CG, NT>;
     if (max_items > 0x7fffffff) return refuse("grouped product: too many output tiles");
@@ -482,7 +522,7 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const CUtensorMap &mb
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, WAY>, ma, mb, mbb, a), "grouped product");
+    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, WAY>, ma, mb, a), "grouped product");
 }
 
 template <int CG, int NT, int WAY>
@@ -519,15 +559,26 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     if ((s = launched((int)guard.enter(device), "cudaSetDevice")) != EW_OK) return s;
     const Device *d;
     if ((s = device_state(device, &d)) != EW_OK) return s;
-    CUtensorMap ma, mb, mbb;
-    const uint64_t wd[3] = {(uint64_t)k, (uint64_t)n, (uint64_t)groups};
-    const uint64_t ws[2] = {(uint64_t)ldw * 2, groups > 1 ? (uint64_t)group_stride * 2 : (uint64_t)ldw * 2};
-    const uint32_t wbox[3] = {64, grad ? 64u : 128u, 1};
+    CUtensorMap ma;
+    RowMaps mb;
+    const uint64_t between = groups > 1 ? (uint64_t)group_stride * 2 : (uint64_t)ldw * 2;
+    const bool pairs = grad && k % 64 == 0;            // (otherwise a 64-wide block could end behind the last row)
+    if (pairs) {
+        const uint64_t wd[4] = {64, (uint64_t)n, (uint64_t)k / 64, (uint64_t)groups}, ws[3] = {(uint64_t)ldw * 2, 128, between};
+        const uint32_t box[4] = {64, 64, 2, 1};
+        s = encode_map(*d, &ma, map_type(dtype), w, 4, wd, ws, box, CU_TENSOR_MAP_SWIZZLE_128B);
+    } else {
+        const uint64_t wd[3] = {(uint64_t)k, (uint64_t)n, (uint64_t)groups}, ws[2] = {(uint64_t)ldw * 2, between};
+        const uint32_t box[3] = {64, grad ? 64u : 128u, 1};
+        s = encode_map(*d, &ma, map_type(dtype), w, 3, wd, ws, box, CU_TENSOR_MAP_SWIZZLE_128B);
+    }
+    if (s != EW_OK) return s;
     const uint64_t xd[2] = {(uint64_t)t, (uint64_t)rows}, xs[1] = {(uint64_t)ldx * 2};
-    const uint32_t xbox[2] = {64, kChunkRows}, xbig[2] = {64, 128};
-    if ((s = encode_map(*d, &ma, map_type(dtype), w, 3, wd, ws, wbox, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
-    if ((s = encode_map(*d, &mb, map_type(dtype), x, 2, xd, xs, xbox, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
-    if ((s = encode_map(*d, &mbb, map_type(dtype), x, 2, xd, xs, xbig, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    const int most_boxes = rows <= 32ll * groups ? 2 : 4;                    // (the narrowest form stages up to 64 rows)
+    for (int i = 0; i < most_boxes; ++i) {
+        const uint32_t box[2] = {64, 32u * (i + 1)};
+        if ((s = encode_map(*d, &mb.m[i], map_type(dtype), x, 2, xd, xs, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    }
     Args a = {};
     a.offsets = offsets;
     a.out = out;
@@ -539,13 +590,14 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     a.t_size = t;
     a.out_kind = out_dtype;
     a.fp16 = dtype == EW_FP16;
+    a.a_pairs = pairs;
     cudaStream_t st = (cudaStream_t)stream;
     const long long live = groups < rows ? groups : rows;                    // groups that can have rows
 #define EW_LAUNCH(CG, NT)                                                                                                     \
     do {                                                                                                                      \
         a.f_tiles = (f + 128 * CG - 1) / (128 * CG);                                                                          \
         const long long items = (live + rows / NT) * a.f_tiles;                                                               \
-        return grad ? launch<CG, NT, kInputGrad>(*d, ma, mb, mbb, a, items, st) : launch<CG, NT, kProduct>(*d, ma, mb, mbb, a, items, st); \
+        return grad ? launch<CG, NT, kInputGrad>(*d, ma, mb, a, items, st) : launch<CG, NT, kProduct>(*d, ma, mb, a, items, st); \
     } while (0)
     if (rows <= 32ll * groups) EW_LAUNCH(1, 64);
     if (rows <= 96ll * groups) EW_LAUNCH(1, 128);
@@ -601,12 +653,20 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
                 return s;
         return EW_OK;
     }
-    CUtensorMap ma, mb;
-    const uint64_t xd[2] = {(uint64_t)k, (uint64_t)rows}, xs[1] = {(uint64_t)ldx * 2};
-    const uint64_t yd[2] = {(uint64_t)n, (uint64_t)rows}, ys[1] = {(uint64_t)lddy * 2};
-    const uint32_t box[2] = {64, 64};
-    if ((s = encode_map(*d, &ma, map_type(dtype), x, 2, xd, xs, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
-    if ((s = encode_map(*d, &mb, map_type(dtype), dy, 2, yd, ys, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    CUtensorMap ma;
+    RowMaps mb;
+    // 64 columns x 64 rows, two such blocks side by side in one copy where the row is made of whole ones
+    auto columns = [&](CUtensorMap *m, const void *at, int64_t ld, int width) {
+        if (width % 64) {
+            const uint64_t dim[2] = {(uint64_t)width, (uint64_t)rows}, stride[1] = {(uint64_t)ld * 2};
+            const uint32_t box[2] = {64, 64};
+            return encode_map(*d, m, map_type(dtype), at, 2, dim, stride, box, CU_TENSOR_MAP_SWIZZLE_128B);
+        }
+        const uint64_t dim[3] = {64, (uint64_t)rows, (uint64_t)width / 64}, stride[2] = {(uint64_t)ld * 2, 128};
+        const uint32_t box[3] = {64, 64, 2};
+        return encode_map(*d, m, map_type(dtype), at, 3, dim, stride, box, CU_TENSOR_MAP_SWIZZLE_128B);
+    };
+    if ((s = columns(&ma, x, ldx, k)) != EW_OK || (s = columns(&mb.m[0], dy, lddy, n)) != EW_OK) return s;
     Args a = {};
     a.offsets = offsets;
     a.out = dw;
@@ -616,11 +676,13 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
     a.rows = rows;
     a.groups = groups;
     a.f_size = k;
+    a.a_pairs = k % 64 == 0;
+    a.b_pairs = n % 64 == 0;
     a.c_size = n;
     a.f_tiles = (k + 255) / 256;
     a.c_tiles = (n + 255) / 256;
     a.out_kind = out_dtype;
     a.fp16 = dtype == EW_FP16;
     const long long items = (long long)groups * a.c_tiles * a.f_tiles;
-    return accumulate ? launch<2, 256, kWeightAdd>(*d, ma, mb, mb, a, items, st) : launch<2, 256, kWeightGrad>(*d, ma, mb, mb, a, items, st);
+    return accumulate ? launch<2, 256, kWeightAdd>(*d, ma, mb, a, items, st) : launch<2, 256, kWeightGrad>(*d, ma, mb, a, items, st);
 }
