@@ -30,9 +30,7 @@ using namespace tc;
 
 enum Way { kProduct = 0, kInputGrad = 1, kWeightGrad = 2, kWeightAdd = 3 };      // the last: added to what is there
 
-constexpr int kEpilogueWarps = 8;                      // two to each quarter of the TMEM lanes, taking turns at the columns
-constexpr int kRelayWarp = 2 + kEpilogueWarps;
-constexpr int kThreads = (kRelayWarp + 1) * 32;        // TMA, MMA, epilogue, relay (weight gradient)
+constexpr int threads_of(int epilogue_warps) { return (3 + epilogue_warps) * 32; }       // TMA, MMA, epilogue, relay (weight gradient)
 constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one stage
 constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
 constexpr int kSmemLimit = 227 * 1024;
@@ -56,7 +54,8 @@ struct Args {
     int table_bytes;
 };
 
-// CG: CTAs that share one MMA tile (1, or 2 = a pair with 256 f); NT: columns of an accumulator set
+// CG: CTAs that share one MMA tile (1, or 2 = a pair with 256 f); NT: columns of an accumulator set; EW: epilogue warps, four or
+// eight (two to each quarter of the TMEM lanes, taking turns at the columns)
 template <int CG, int NT>
 struct Cfg {
     static constexpr int kBRows = NT / CG;                                   // c staged by each CTA
@@ -205,10 +204,11 @@ __device__ __forceinline__ void store_zero(void *out, size_t at, int kind) {
     else reinterpret_cast<uint16_t *>(out)[at] = 0;
 }
 
-template <int CG, int NT, int WAY>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int CG, int NT, int EW, int WAY>
+__global__ void __launch_bounds__(threads_of(EW), 1)
 grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ Args a) {
     using C = Cfg<CG, NT>;
+    constexpr int kRelayWarp = 2 + EW;
     constexpr bool DW = WAY == kWeightGrad || WAY == kWeightAdd;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -234,7 +234,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_tfull + 8 * i, 1);
-            mbar_init(bar_tempty + 8 * i, kEpilogueWarps * CG);
+            mbar_init(bar_tempty + 8 * i, EW * CG);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -444,7 +444,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..9 of each CTA)
+        // ------------------------------------------------------------------ epilogue (EW warps of each CTA)
         const int lg = warp & 3, turn = (warp - 2) >> 2;                     // the TMEM lanes this warp may read; its columns
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
@@ -455,20 +455,20 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             const size_t at = (DW ? (size_t)it.g * a.group_out : 0) + (size_t)it.row0 * a.ldo + f;
             if (DW && it.kb == 0) {
                 if (f_ok && WAY == kWeightGrad)
-                    for (int j = turn; j < it.cols; j += 2) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
+                    for (int j = turn; j < it.cols; j += EW / 4) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
                 continue;
             }
             if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
             tc_fence_after();
             const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
 #pragma unroll 1
-            for (int c0 = 32 * turn; c0 < it.cols; c0 += 64) {
+            for (int c0 = 32 * turn; c0 < it.cols; c0 += 8 * EW) {
                 uint32_t v[32];
                 tc_ld32(t0 + c0, v);                   // columns behind the item's last are in the accumulator set, not stored
                 tc_wait_ld();
                 const int lim = min(32, it.cols - c0);
+                const size_t to = at + (size_t)c0 * a.ldo;
                 if (f_ok) {
-                    const size_t to = at + (size_t)c0 * a.ldo;
                     if (a.out_kind == EW_FP32) put_columns<float, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
                     else if (a.out_kind == EW_BF16) put_columns<__nv_bfloat16, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
                     else put_columns<__half, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
@@ -500,7 +500,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
 
 constexpr int kBarBytes = (3 * kMaxStages + 6) * 8;
 
-template <int CG, int NT, int WAY>
+template <int CG, int NT, int EW, int WAY>
 ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, long long max_items,
                    cudaStream_t st) {
     using C = Cfg<CG, NT>;
@@ -511,7 +511,7 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     cudaLaunchConfig_t cfg = {};
     const long long units = d.sm_count / CG;
     cfg.gridDim = dim3((unsigned)(CG * (max_items < units ? max_items : units)));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads_of(EW));
     cfg.dynamicSmemBytes = (size_t)a.stages * C::kStageBytes + 1024 + kBarBytes + a.table_bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -522,12 +522,12 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, WAY>, ma, mb, a), "grouped product");
+    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, EW, WAY>, ma, mb, a), "grouped product");
 }
 
-template <int CG, int NT, int WAY>
+template <int CG, int NT, int EW, int WAY>
 int setup_one() {
-    return (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    return (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, EW, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
 }
 
 // A row-major matrix's row stride: multiples of eight elements keep every TMA copy on a 16-byte boundary.
@@ -597,7 +597,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     do {                                                                                                                      \
         a.f_tiles = (f + 128 * CG - 1) / (128 * CG);                                                                          \
         const long long items = (live + rows / NT) * a.f_tiles;                                                               \
-        return grad ? launch<CG, NT, kInputGrad>(*d, ma, mb, a, items, st) : launch<CG, NT, kProduct>(*d, ma, mb, a, items, st); \
+        return grad ? launch<CG, NT, 4, kInputGrad>(*d, ma, mb, a, items, st) : launch<CG, NT, 4, kProduct>(*d, ma, mb, a, items, st); \
     } while (0)
     if (rows <= 32ll * groups) EW_LAUNCH(1, 64);
     if (rows <= 96ll * groups) EW_LAUNCH(1, 128);
@@ -608,8 +608,9 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
 }  // namespace
 
 int grouped_setup() {
-    return setup_one<1, 64, kProduct>() | setup_one<1, 64, kInputGrad>() | setup_one<1, 128, kProduct>() | setup_one<1, 128, kInputGrad>() |
-           setup_one<2, 256, kProduct>() | setup_one<2, 256, kInputGrad>() | setup_one<2, 256, kWeightGrad>() | setup_one<2, 256, kWeightAdd>();
+    return setup_one<1, 64, 4, kProduct>() | setup_one<1, 64, 4, kInputGrad>() | setup_one<1, 128, 4, kProduct>() | setup_one<1, 128, 4, kInputGrad>() |
+           setup_one<2, 256, 4, kProduct>() | setup_one<2, 256, 4, kInputGrad>() | setup_one<2, 256, 4, kWeightGrad>() | setup_one<2, 256, 8, kWeightGrad>() |
+           setup_one<2, 256, 8, kWeightAdd>();
 }
 
 }  // namespace ops
@@ -684,5 +685,8 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
     a.out_kind = out_dtype;
     a.fp16 = dtype == EW_FP16;
     const long long items = (long long)groups * a.c_tiles * a.f_tiles;
-    return accumulate ? launch<2, 256, kWeightAdd>(*d, ma, mb, a, items, st) : launch<2, 256, kWeightGrad>(*d, ma, mb, a, items, st);
+    if (accumulate) return launch<2, 256, 8, kWeightAdd>(*d, ma, mb, a, items, st);
+    // Few rows a group: the results' way out is what counts, and eight warps walk it (192 rows: 80 us against 95); many: the
+    // arithmetic does, at the power limit, where four cost less (768 rows: 259 against 270).
+    return rows <= 256ll * groups ? launch<2, 256, 8, kWeightGrad>(*d, ma, mb, a, items, st) : launch<2, 256, 4, kWeightGrad>(*d, ma, mb, a, items, st);
 }
