@@ -32,13 +32,13 @@ namespace ops {
 namespace {
 using namespace tc;
 
-// warps of a CTA: sixteen, or eight with twice the registers where a warp has three columns of pairs
-constexpr __host__ __device__ int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+constexpr int kWarps = 16;
+constexpr int kThreads = kWarps * 32;
 constexpr int kRows = 32;                      // weight rows of a tile: two tiles of the MMA
 constexpr int kLineK = 256;                    // weights of a row in one 128-byte swizzled line
 constexpr int kLineBytes = kRows * kLineK / 2; // a stage: 4 KiB
-constexpr int kScaleBytes = 512;               // a stage's scales: up to eight groups x 32 rows
-constexpr int kMaxStages = 4;                  // of a warp
+constexpr __host__ __device__ int scale_bytes(int spg) { return 8 / spg * kRows * 2; }           // a stage's scales: up to eight groups x 32 rows
+constexpr int kMaxStages = 2;                  // of a warp
 constexpr int kMaxPairs = 2048;                // of one launch; a larger batch is split
 constexpr int kMaxSlots = 2048;
 constexpr int kMaxK = 16384;
@@ -303,9 +303,8 @@ __device__ __forceinline__ void line_products_16(float (&acc)[2][NT][4], const u
 // T: operand type; P: bytes of a number of x, 0: x in its own type; NT: columns of eight pairs a warp accumulates at a time; SPG: 32-weight
 // steps in a group
 template <class T, int P, int NT, int SPG>
-__global__ void __launch_bounds__(warps_of(NT) * 32, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ Args a) {
-    constexpr int kWarps = warps_of(NT), kThreads = kWarps * 32;
     const bool wide = P == 3 || (P == 0 && a.out_fp32);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -317,7 +316,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     volatile int *n_jobs_at = abort_flag + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t my_bars = smem_base + a.at_bars + warp * kMaxStages * 8;
-    const uint32_t my_ring = smem_base + warp * a.stages * kLineBytes, my_scales = smem_base + kWarps * a.stages * kLineBytes + warp * a.stages * kScaleBytes;
+    const uint32_t my_ring = smem_base + warp * a.stages * kLineBytes, my_scales = smem_base + kWarps * a.stages * kLineBytes + warp * a.stages * scale_bytes(SPG);
 
     if (lane == 0) {
         for (int s = 0; s < a.stages; ++s) mbar_init(my_bars + 8 * s, 1);
@@ -376,7 +375,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         // counts are added up per slot, and a pair's position is that sum plus its rank in its warp
         const int stretch = ((a.pairs + kThreads - 1) / kThreads) * 32, p_end = min(a.pairs, (warp + 1) * stretch);
         uint16_t *mine = before + warp * kinds;
-        constexpr int kMost = kMaxPairs / kThreads;
+        constexpr int kMost = (kMaxPairs + kThreads - 1) / kThreads;
         int s_of[kMost];
 #pragma unroll
         for (int j = 0; j < kMost; ++j) s_of[j] = slot_at(warp * stretch + 32 * j + lane, warp * stretch + 32 * j + lane < p_end);
@@ -466,25 +465,22 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             if (lane == 0) {
                 const int slot = jobs[ask.job].slot;
                 const uint32_t bar = my_bars + 8 * ask_stage;
-                mbar_expect_tx(bar, kLineBytes + (8 / SPG) * kRows * 2);
+                mbar_expect_tx(bar, kLineBytes + scale_bytes(SPG));
                 tma_load_2d(my_ring + ask_stage * kLineBytes, &map_q, ask.line * (kLineK / 2), slot * a.n + ask.tile * kRows, bar);
-                tma_load_2d(my_scales + ask_stage * kScaleBytes, &map_s, ask.tile * kRows, slot * groups + ask.line * (8 / SPG), bar);
+                tma_load_2d(my_scales + ask_stage * scale_bytes(SPG), &map_s, ask.tile * kRows, slot * groups + ask.line * (8 / SPG), bar);
             }
             if (++ask_stage == (uint32_t)a.stages) ask_stage = 0;
             --left_to_ask;
             advance(ask);
         };
-#pragma unroll 1
-        for (int s = 0; s < a.stages; ++s) issue();
-
-        // the batch's rows of x, a line at a time, while the first weights are on their way (they are contiguous in the
-        // order of the pairs)
+        // The batch's rows of x (contiguous in the order of the pairs), a line at a time, several lines at once where there are
+        // many: a line is a chain of a load and a dozen shuffles.  The first ones are asked for before the weights, behind
+        // which they would wait, and put in place while those are on their way.
         const int pair_at = jobs[job0].first;
-        // (several lines at a time where there are many: a line is a chain of a load and a dozen shuffles)
-        constexpr int kAtOnce = NT == 1 ? 1 : 8;
-        for (int row = warp / k_lines, line = warp - row * k_lines; row < rows;) {
-            uint4 raw[kAtOnce];
-            int rows_of[kAtOnce], lines_of[kAtOnce];
+        constexpr int kAtOnce = NT == 1 ? 2 : 8;
+        uint4 raw[kAtOnce];
+        int rows_of[kAtOnce], lines_of[kAtOnce], row = warp / k_lines, line = warp - row * k_lines;
+        auto fetch = [&]() {
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 rows_of[j] = row;
@@ -494,10 +490,15 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 if (row < rows && at_k < a.k) raw[j] = *reinterpret_cast<const uint4 *>(a.x + ((size_t)x_row[pair_at + row] * a.ldx + at_k) * 2);
                 for (line += kWarps; line >= k_lines; line -= k_lines) ++row;
             }
+        };
+        fetch();
+#pragma unroll 1
+        for (int s = 0; s < a.stages; ++s) issue();
+        while (rows_of[0] < rows) {
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j)
-            {
-                const bool there = rows_of[j] < rows && lines_of[j] * kLineK + lane * 8 < a.k;
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (rows_of[j] >= rows) break;
+                const bool there = lines_of[j] * kLineK + lane * 8 < a.k;
                 uint8_t *to = smem + a.at_x + rows_of[j] * a.x_bytes;
                 if constexpr (P == 0) {
                     if (there) *reinterpret_cast<uint4 *>(to + lines_of[j] * 512 + lane * 16) = raw[j];
@@ -505,6 +506,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     convert_line<T, P, SPG>(raw[j], lines_of[j], there, to, a);
                 }
             }
+            fetch();
         }
         __syncthreads();
 
@@ -541,7 +543,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 // (after an expired wait the warp walks on without data: the CTA's barriers still need it)
                 if (ok) ok = mbar_wait_warp(my_bars + 8 * stage, phase, abort_flag, a.err);
                 if (ok) {
-                    const uint32_t w_at = my_ring + stage * kLineBytes + r * 144 + c * 4, s_at = my_scales + stage * kScaleBytes + r * 2;
+                    const uint32_t w_at = my_ring + stage * kLineBytes + r * 144 + c * 4, s_at = my_scales + stage * scale_bytes(SPG) + r * 2;
                     const int left = a.k - at.line * kLineK;
                     if constexpr (P != 0) {
                         line_products<T, P, 1, NT, SPG>(acc, xb, xc, fac0, fac1, w_at, s_at, at.line, left);
@@ -619,7 +621,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 
 template <class T, int P, int NT, int SPG>
 ew_status_t launch(const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
-    return launched(launch_pdl(quant_mv_kernel<T, P, NT, SPG>, dim3(ctas), dim3(warps_of(NT) * 32), (size_t)smem, st, mq, ms, a), "4-bit product");
+    return launched(launch_pdl(quant_mv_kernel<T, P, NT, SPG>, dim3(ctas), dim3(kThreads), (size_t)smem, st, mq, ms, a), "4-bit product");
 }
 template <class T, int P, int NT>
 ew_status_t launch_group(int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
@@ -649,26 +651,37 @@ int lay_out(Args &a, int nt, int group, int pieces) {
     // rows of x start 64 bytes apart modulo 128: the two rows that a quarter of a warp reads lie in different banks
     a.x_wide = (a.k * 2 + 127) / 128 * 128 + 64;
     a.x_third = pieces == 3 ? (a.k + 127) / 128 * 128 : 0;
-    a.x_bytes = (a.x_wide + a.x_third + (pieces ? groups * 16 : 0) + 127) / 128 * 128 + 64;
-    const int warps = warps_of(nt);
-    for (a.stages = nt == 1 ? 2 : 4; a.stages >= 1; --a.stages) {
-        const int ring = warps * a.stages * (kLineBytes + kScaleBytes), bars = warps * kMaxStages * 8 + 16, red = warps * 1024 * nt;
-        const int fixed = 1024 + ring + 16 + bars + red + (a.n_slots + 1) * 4 + a.pairs * 12;
-        a.x_cap = (kSmemLimit - fixed) / a.x_bytes;
-        if (a.x_cap > a.pairs) a.x_cap = a.pairs;
-        if (a.stages > 1 && a.x_cap < 8 * nt && a.x_cap < a.pairs) continue;
-        if (a.x_cap < 1) return 0;
-        a.job_rows = a.x_cap < 8 * nt ? a.x_cap : 8 * nt;
+    a.x_bytes = pieces ? (a.x_wide + a.x_third + groups * 16 + 127) / 128 * 128 + 64 : a.x_wide;
+    const int live = a.pairs < a.n_slots ? a.pairs : a.n_slots;
+    for (a.stages = kMaxStages; a.stages >= 1; --a.stages) {
+        const int ring = kWarps * a.stages * (kLineBytes + scale_bytes(group / 32)), bars = kWarps * kMaxStages * 8 + 16, red = kWarps * 1024 * nt;
+        const int fixed = 1024 + ring + 16 + bars + red + (a.n_slots + 1) * 4 + a.pairs * 4;
+        // a row of x, and the jobs (eight bytes each) that jobs of so few rows can make
+        a.x_cap = 0;
+        int jobs = 0;
+        for (int rows = 8 * nt < a.pairs ? 8 * nt : a.pairs; rows >= 1; --rows) {
+            jobs = live + a.pairs / rows;
+            const int cap = (kSmemLimit - fixed - jobs * 8) / a.x_bytes;
+            if (cap < rows) continue;
+            a.x_cap = cap < a.pairs ? cap : a.pairs;
+            a.job_rows = rows;
+            break;
+        }
+        if (a.x_cap < 1) {
+            if (a.stages > 1) continue;
+            return 0;
+        }
+        if (a.stages > 1 && a.job_rows < 8 * nt && a.job_rows < a.pairs) continue;
         int o = ring;
         a.at_x = o; o += a.x_cap * a.x_bytes;
         a.at_bars = o = (o + 15) / 16 * 16; o += bars;
         a.at_red = o; o += red;
-        a.at_jobs = o; o += a.pairs * 8;
+        a.at_jobs = o; o += jobs * 8;
         a.at_start = o; o += (a.n_slots + 1) * 4;
         a.at_order = o; o += a.pairs * 2;
         a.at_row = o; o += a.pairs * 2;
         // the grouping tables lie where ring and rows of x will be
-        if (warps * (a.n_slots + 1) * 2 + a.pairs * 4 <= a.at_bars) return o + 1024;
+        if (kWarps * (a.n_slots + 1) * 2 + a.pairs * 4 <= a.at_bars) return o + 1024;
     }
     return 0;
 }
