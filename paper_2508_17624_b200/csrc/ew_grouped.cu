@@ -35,6 +35,10 @@ constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one s
 constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 12;
+// The tensor core cuts off, rather than rounds, what a product has below the running sum's last bit: over a sum of 2048
+// terms 1.2e-6 of the result (2-norm), growing with the length.  fp32 results are therefore summed 1024 terms at a time, and
+// the epilogue adds the parts up in fp32 in the output (always the same thread's part of it); 16-bit results do not see it.
+constexpr int kSumBlocks = 16;
 
 struct Args {
     const int32_t *offsets;
@@ -72,6 +76,7 @@ struct RowMaps { CUtensorMap m[4]; };
 
 struct Item {
     int g, f0, row0, cols, kb, tail;      // cols: output rows (c) of this item; kb: k-blocks; tail: live rows of the last one (dw)
+    int chunk;                            // k-blocks summed up in the tensor core at a time
 };
 
 __device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) { return smem_desc_sw128(addr); }
@@ -327,6 +332,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             it.kb = t_blocks;
             it.tail = kBlockK;
         }
+        const int chunks = a.out_kind == EW_FP32 ? (it.kb + kSumBlocks - 1) / kSumBlocks : 1;
+        it.chunk = chunks > 1 ? (it.kb + chunks - 1) / chunks : it.kb;
         return it;
     };
 
@@ -394,28 +401,30 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 if (DW && it.kb == 0) continue;                              // an empty group: the epilogue writes its zeros
                 const int n = DW ? NT : (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
-                if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
-                tc_fence_after();
-                const uint32_t d = tmem_base + acc * NT;
-                for (int kb = 0; kb < it.kb; ++kb) {
-                    if (!(ok = wait_on<CG == 2>(bar_in + 8 * stage, phase, abort_flag, a.err))) break;
+                for (int kb = 0; kb < it.kb && ok;) {
+                    if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
-                    const uint64_t da = WAY == kProduct ? desc_kmajor(sa) : desc_mnmajor(sa);
-                    const uint64_t db = DW ? desc_mnmajor(sb) : desc_kmajor(sb);
-                    // 16 summed elements a step: 32 bytes further along a K-major row, two groups of eight 128-byte rows
-                    // (2 KiB) further in an MN-major tile; descriptors count 16 bytes
-                    constexpr int kStepA = WAY == kProduct ? 2 : 128, kStepB = DW ? 128 : 2;
-                    const int steps = DW && kb == it.kb - 1 ? (it.tail + 15) >> 4 : kBlockK / 16;
+                    const uint32_t d = tmem_base + acc * NT;
+                    for (const int first = kb, end = min(it.kb, kb + it.chunk); kb < end; ++kb) {
+                        if (!(ok = wait_on<CG == 2>(bar_in + 8 * stage, phase, abort_flag, a.err))) break;
+                        tc_fence_after();
+                        const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
+                        const uint64_t da = WAY == kProduct ? desc_kmajor(sa) : desc_mnmajor(sa);
+                        const uint64_t db = DW ? desc_mnmajor(sb) : desc_kmajor(sb);
+                        // 16 summed elements a step: 32 bytes further along a K-major row, two groups of eight 128-byte
+                        // rows (2 KiB) further in an MN-major tile; descriptors count 16 bytes
+                        constexpr int kStepA = WAY == kProduct ? 2 : 128, kStepB = DW ? 128 : 2;
+                        const int steps = DW && kb == it.kb - 1 ? (it.tail + 15) >> 4 : kBlockK / 16;
 #pragma unroll
-                    for (int ki = 0; ki < kBlockK / 16; ++ki)
-                        if (!DW || ki < steps) mma<CG>(d, da + kStepA * ki, db + kStepB * ki, idesc, (kb | ki) ? 1u : 0u);
-                    commit<CG>(bar_empty + 8 * stage);
-                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                        for (int ki = 0; ki < kBlockK / 16; ++ki)
+                            if (!DW || ki < steps) mma<CG>(d, da + kStepA * ki, db + kStepB * ki, idesc, (kb != first || ki) ? 1u : 0u);
+                        commit<CG>(bar_empty + 8 * stage);
+                        if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                    }
+                    if (!ok) break;
+                    commit<CG>(bar_tfull + 8 * acc);
+                    if (++acc == 2) { acc = 0; acc_phase ^= 1; }
                 }
-                if (!ok) break;
-                commit<CG>(bar_tfull + 8 * acc);
-                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
             }
         }
     } else if (warp == kRelayWarp) {
@@ -458,26 +467,33 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     for (int j = turn; j < it.cols; j += EW / 4) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
                 continue;
             }
-            if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
-            tc_fence_after();
-            const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
+            for (int kb = 0; kb < it.kb; kb += it.chunk) {
+                if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
+                tc_fence_after();
+                const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
 #pragma unroll 1
-            for (int c0 = 32 * turn; c0 < it.cols; c0 += 8 * EW) {
-                uint32_t v[32];
-                tc_ld32(t0 + c0, v);                   // columns behind the item's last are in the accumulator set, not stored
-                tc_wait_ld();
-                const int lim = min(32, it.cols - c0);
-                const size_t to = at + (size_t)c0 * a.ldo;
-                if (f_ok) {
-                    if (a.out_kind == EW_FP32) put_columns<float, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
-                    else if (a.out_kind == EW_BF16) put_columns<__nv_bfloat16, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
-                    else put_columns<__half, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
+                for (int c0 = 32 * turn; c0 < it.cols; c0 += 8 * EW) {
+                    uint32_t v[32];
+                    tc_ld32(t0 + c0, v);               // columns behind the item's last are in the accumulator set, not stored
+                    tc_wait_ld();
+                    const int lim = min(32, it.cols - c0);
+                    const size_t to = at + (size_t)c0 * a.ldo;
+                    if (f_ok) {
+                        if (a.out_kind == EW_FP32) {
+                            if (WAY == kWeightAdd || kb > 0) add_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
+                            else store_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
+                        } else if (a.out_kind == EW_BF16) {
+                            put_columns<__nv_bfloat16, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
+                        } else {
+                            put_columns<__half, WAY == kWeightAdd>(a.out, to, a.ldo, v, lim);
+                        }
+                    }
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_leader<CG>(bar_tempty + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_leader<CG>(bar_tempty + 8 * acc);
-            if (++acc == 2) { acc = 0; acc_phase ^= 1; }
         }
     }
 

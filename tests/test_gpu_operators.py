@@ -100,6 +100,12 @@ def test_products_layer_sizes(rows, groups, n, k):
     check_three(make_counts(rows, groups, 1, empty=(1,)), n, k, BF16, FP32, seed=9)
 
 
+@pytest.mark.parametrize("counts,n,k", [([2100, 0, 1025], 264, 200), ([3, 40, 0, 7], 1100, 2056), ([300, 700], 2049, 1032)], ids=str)
+def test_products_long_sums_in_parts(counts, n, k):
+    """Contractions beyond 1024 terms with fp32 results: summed in parts, rows and gradients alike."""
+    check_three(counts, n, k, BF16, FP32, seed=11)
+
+
 def test_no_rows():
     w = randn((3, 16, 24), BF16, 0)
     offsets = torch.zeros(4, dtype=torch.int32, device="cuda")
