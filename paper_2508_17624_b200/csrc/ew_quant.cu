@@ -314,6 +314,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     Job *jobs = reinterpret_cast<Job *>(smem + a.at_jobs);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + a.at_bars + kWarps * kMaxStages * 8);
     volatile int *n_jobs_at = abort_flag + 1;
+    const uint32_t x_bar = smem_base + a.at_bars + kWarps * kMaxStages * 8 + 8;   // the rows of x of a batch (P = 0)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t my_bars = smem_base + a.at_bars + warp * kMaxStages * 8;
     const uint32_t my_ring = smem_base + warp * a.stages * kLineBytes, my_scales = smem_base + kWarps * a.stages * kLineBytes + warp * a.stages * scale_bytes(SPG);
@@ -323,6 +324,8 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 0) {
+        mbar_init(x_bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *abort_flag = 0;
         prefetch_map(&map_q);
         prefetch_map(&map_s);
@@ -437,7 +440,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     int job0 = first_item / a.tiles, tile0 = first_item - job0 * a.tiles;
     const int k_lines = (a.k + kLineK - 1) / kLineK, groups = a.k / (32 * SPG);
     const int r = lane >> 2, c = lane & 3;
-    uint32_t ask_stage = 0, stage = 0, phase = 0;                            // of the warp's ring, over all batches
+    uint32_t ask_stage = 0, stage = 0, phase = 0, x_phase = 0;                            // of the warp's ring, over all batches
     bool ok = true;
     while (left_items > 0) {
         int job1 = job0, rows = 0, items = -tile0;
@@ -448,67 +451,75 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         items = min(items, left_items);
         const int lines = items * k_lines, l0 = (int)((long long)lines * warp / kWarps), l1 = (int)((long long)lines * (warp + 1) / kWarps);
 
-        // the next line to ask for, and the one being worked on
-        struct Cursor { int job, tile, line; };
-        Cursor at = {job0, tile0 + l0 / k_lines, l0 % k_lines};
-        while (at.tile >= a.tiles) { at.tile -= a.tiles; ++at.job; }
-        Cursor ask = at;
-        int left_to_ask = l1 - l0;
-        auto advance = [&](Cursor &u) {
-            if (++u.line == k_lines) {
-                u.line = 0;
-                if (++u.tile == a.tiles) { u.tile = 0; ++u.job; }
-            }
-        };
+        // the line being worked on, and the next one to ask for with its rows in the two tensor maps
+        int job = job0, line = l0 % k_lines, tile = tile0 + l0 / k_lines;
+        while (tile >= a.tiles) { tile -= a.tiles; ++job; }
+        int left_to_ask = l1 - l0, ask_job = job, ask_line = line, ask_tile = tile;
+        int ask_slot = left_to_ask > 0 ? jobs[job].slot : 0;
         auto issue = [&]() {
             if (left_to_ask <= 0 || !ok) return;
             if (lane == 0) {
-                const int slot = jobs[ask.job].slot;
                 const uint32_t bar = my_bars + 8 * ask_stage;
                 mbar_expect_tx(bar, kLineBytes + scale_bytes(SPG));
-                tma_load_2d(my_ring + ask_stage * kLineBytes, &map_q, ask.line * (kLineK / 2), slot * a.n + ask.tile * kRows, bar);
-                tma_load_2d(my_scales + ask_stage * scale_bytes(SPG), &map_s, ask.tile * kRows, slot * groups + ask.line * (8 / SPG), bar);
+                tma_load_2d(my_ring + ask_stage * kLineBytes, &map_q, ask_line * (kLineK / 2), ask_slot * a.n + ask_tile * kRows, bar);
+                tma_load_2d(my_scales + ask_stage * scale_bytes(SPG), &map_s, ask_tile * kRows, ask_slot * groups + ask_line * (8 / SPG), bar);
             }
             if (++ask_stage == (uint32_t)a.stages) ask_stage = 0;
             --left_to_ask;
-            advance(ask);
-        };
-        // The batch's rows of x (contiguous in the order of the pairs), a line at a time, several lines at once where there are
-        // many: a line is a chain of a load and a dozen shuffles.  The first ones are asked for before the weights, behind
-        // which they would wait, and put in place while those are on their way.
-        const int pair_at = jobs[job0].first;
-        constexpr int kAtOnce = NT == 1 ? 2 : 8;
-        uint4 raw[kAtOnce];
-        int rows_of[kAtOnce], lines_of[kAtOnce], row = warp / k_lines, line = warp - row * k_lines;
-        auto fetch = [&]() {
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                rows_of[j] = row;
-                lines_of[j] = line;
-                raw[j] = make_uint4(0, 0, 0, 0);
-                const int at_k = line * kLineK + lane * 8;
-                if (row < rows && at_k < a.k) raw[j] = *reinterpret_cast<const uint4 *>(a.x + ((size_t)x_row[pair_at + row] * a.ldx + at_k) * 2);
-                for (line += kWarps; line >= k_lines; line -= k_lines) ++row;
-            }
-        };
-        fetch();
-#pragma unroll 1
-        for (int s = 0; s < a.stages; ++s) issue();
-        while (rows_of[0] < rows) {
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                if (rows_of[j] >= rows) break;
-                const bool there = lines_of[j] * kLineK + lane * 8 < a.k;
-                uint8_t *to = smem + a.at_x + rows_of[j] * a.x_bytes;
-                if constexpr (P == 0) {
-                    if (there) *reinterpret_cast<uint4 *>(to + lines_of[j] * 512 + lane * 16) = raw[j];
-                } else {
-                    convert_line<T, P, SPG>(raw[j], lines_of[j], there, to, a);
+            if (++ask_line == k_lines) {
+                ask_line = 0;
+                if (++ask_tile == a.tiles) {
+                    ask_tile = 0;
+                    if (left_to_ask > 0) ask_slot = jobs[++ask_job].slot;
                 }
             }
+        };
+        // The batch's rows of x: contiguous in the order of the pairs.
+        const int pair_at = jobs[job0].first;
+        if constexpr (P == 0) {
+            // as they are, one copy a row
+            if (warp == 0) {
+                if (lane == 0) mbar_expect_tx(x_bar, (uint32_t)rows * a.k * 2);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); // (the last batch's rows have been read)
+                __syncwarp();
+                for (int i = lane; i < rows; i += 32)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(smem_base + a.at_x + i * a.x_bytes), "l"(a.x + (size_t)x_row[pair_at + i] * a.ldx * 2), "r"(a.k * 2), "r"(x_bar) : "memory");
+            }
+#pragma unroll 1
+            for (int s = 0; s < a.stages; ++s) issue();
+            if (ok) ok = mbar_wait_warp(x_bar, x_phase, abort_flag, a.err);
+            x_phase ^= 1;
+        } else {
+            // a line at a time, a few at once: a line is a chain of a load and a dozen shuffles.  The first ones are asked for
+            // before the weights, behind which they would wait, and put in place while those are on their way.
+            constexpr int kAtOnce = 2;
+            uint4 raw[kAtOnce];
+            int rows_of[kAtOnce], lines_of[kAtOnce], next_row = warp / k_lines, next_line = warp - next_row * k_lines;
+            auto fetch = [&]() {
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    rows_of[j] = next_row;
+                    lines_of[j] = next_line;
+                    raw[j] = make_uint4(0, 0, 0, 0);
+                    const int at_k = next_line * kLineK + lane * 8;
+                    if (next_row < rows && at_k < a.k) raw[j] = *reinterpret_cast<const uint4 *>(a.x + ((size_t)x_row[pair_at + next_row] * a.ldx + at_k) * 2);
+                    for (next_line += kWarps; next_line >= k_lines; next_line -= k_lines) ++next_row;
+                }
+            };
             fetch();
+#pragma unroll 1
+            for (int s = 0; s < a.stages; ++s) issue();
+            while (rows_of[0] < rows) {
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    if (rows_of[j] >= rows) break;
+                    convert_line<T, P, SPG>(raw[j], lines_of[j], lines_of[j] * kLineK + lane * 8 < a.k, smem + a.at_x + rows_of[j] * a.x_bytes, a);
+                }
+                fetch();
+            }
+            __syncthreads();
         }
-        __syncthreads();
 
         float acc[2][NT][4];
         Job jb = {};
@@ -521,9 +532,9 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         for (int l = l0; l <= l1; ++l) {
             bool done = false;
             if (l < l1) {
-                if (l == l0 || at.line == 0) {
-                    jb = jobs[at.job];
-                    mine = at.line == 0;
+                if (l == l0 || line == 0) {
+                    jb = jobs[job];
+                    mine = line == 0;
                     const uint32_t base = smem_base + a.at_x + (jb.first - pair_at) * a.x_bytes, fac = a.x_wide + a.x_third;
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
@@ -544,22 +555,22 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 if (ok) ok = mbar_wait_warp(my_bars + 8 * stage, phase, abort_flag, a.err);
                 if (ok) {
                     const uint32_t w_at = my_ring + stage * kLineBytes + r * 144 + c * 4, s_at = my_scales + stage * scale_bytes(SPG) + r * 2;
-                    const int left = a.k - at.line * kLineK;
+                    const int left = a.k - line * kLineK;
                     if constexpr (P != 0) {
-                        line_products<T, P, 1, NT, SPG>(acc, xb, xc, fac0, fac1, w_at, s_at, at.line, left);
+                        line_products<T, P, 1, NT, SPG>(acc, xb, xc, fac0, fac1, w_at, s_at, line, left);
                     } else {
-                        if (jb.count <= 8) line_products_16<T, 1, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
-                        else if (jb.count <= 16) line_products_16<T, 2, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
-                        else line_products_16<T, 3, NT, SPG>(acc, xb, w_at, s_at, at.line, left);
+                        if (jb.count <= 8) line_products_16<T, 1, NT, SPG>(acc, xb, w_at, s_at, line, left);
+                        else if (jb.count <= 16) line_products_16<T, 2, NT, SPG>(acc, xb, w_at, s_at, line, left);
+                        else line_products_16<T, 3, NT, SPG>(acc, xb, w_at, s_at, line, left);
                     }
                     if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
                     __syncwarp();                                            // all lanes have read the stage
                     issue();
                 }
-                const bool last = at.line == k_lines - 1;
+                const bool last = line == k_lines - 1;
                 if (mine) {
                     done = last;
-                    if (!last && l == l1 - 1) pending = at.line;
+                    if (!last && l == l1 - 1) pending = line;
                 } else if (last || l == l1 - 1) {
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
@@ -597,14 +608,17 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                             const size_t to = (size_t)(a.pair0 + order[jb.first + at_pair]) * a.ldo;
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
-                                const int row = at.tile * kRows + m * 16 + r;
+                                const int row = tile * kRows + m * 16 + r;
                                 if (row < a.n) put<T>(a.out, to + row, acc[m][t][e], wide);
                                 if (row + 8 < a.n) put<T>(a.out, to + row + 8, acc[m][t][2 + e], wide);
                             }
                         }
                     }
             }
-            if (l < l1) advance(at);
+            if (l < l1 && ++line == k_lines) {
+                line = 0;
+                if (++tile == a.tiles) { tile = 0; ++job; }
+            }
         }
         left_items -= items;
         job0 = job1;
