@@ -520,7 +520,7 @@ template <int CG, int NT, int EW, int WAY>
 ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, long long max_items,
                    cudaStream_t st) {
     using C = Cfg<CG, NT>;
-    if (max_items > 0x7fffffff) return refuse("grouped product: too many output tiles");
+    if (max_items > 0x7fff0000) return refuse("grouped product: too many output tiles");
     a.table_bytes = (3 * a.groups + 1) * 4;
     const int room = kSmemLimit - 1024 - kBarBytes - a.table_bytes;
     a.stages = room / C::kStageBytes < kMaxStages ? room / C::kStageBytes : kMaxStages;
@@ -554,7 +554,9 @@ bool bad_matrix(const void *p, long long ld, long long width) {
 ew_status_t check_common(int32_t dtype, int32_t out_dtype, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k,
                          const void *out) {
     if (!is_16bit(dtype) || (out_dtype != dtype && out_dtype != EW_FP32)) return refuse("grouped product: operands are bf16 or fp16, results of the same type or fp32");
-    if (rows < 0 || groups < 1 || groups > kMaxGroups || n < 1 || k < 1) return refuse("grouped product: size out of range");
+    constexpr int32_t kMostSize = 0x7fff0000;                                // (indexes run a tile past the end)
+    if (rows < 0 || rows > kMostSize || groups < 1 || groups > kMaxGroups || n < 1 || n > kMostSize || k < 1 || k > kMostSize)
+        return refuse("grouped product: size out of range");
     if (!offsets || ((uintptr_t)offsets & 3) || !out || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)))
         return refuse("grouped product: null or misaligned pointer");
     return EW_OK;

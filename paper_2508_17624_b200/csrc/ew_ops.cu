@@ -24,7 +24,7 @@ ew_status_t resolve(Device *d, int device) {
     if (e != cudaSuccess) return launched((int)e, "operator set-up");
     d->encode = reinterpret_cast<EncodeTiled>(fn);
     d->err = static_cast<int *>(err);
-    return launched(grouped_setup() | quant_setup(), "operator set-up");
+    return launched(grouped_setup() | quant_setup() | swiglu_setup(), "operator set-up");
 }
 
 }  // namespace

@@ -33,6 +33,7 @@ ew_status_t device_state(int device, const Device **out);
 // Per-file attributes of the operators' kernels, set once per device by device_state().
 int grouped_setup();
 int quant_setup();
+int swiglu_setup();
 
 inline bool is_16bit(int dtype) { return dtype == EW_BF16 || dtype == EW_FP16; }
 inline int elem_bytes(int dtype) { return dtype == EW_FP32 ? 4 : 2; }

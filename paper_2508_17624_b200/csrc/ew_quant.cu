@@ -11,11 +11,12 @@
 // they are: one mask, or a shift and a mask, turns a word into four bytes 0..15, and the 8-bit integer m16n8k32
 // instruction multiplies 512 weights with eight pairs (2.1 cycles of an SM measured, what bf16 takes for 256; the 8-bit
 // floating-point form is made of 16-bit ones on this machine and slower).  x goes in as fixed-point numbers: a group of x,
-// which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 16319 (16 bits,
-// for 16-bit results) or above 4177919 (24 bits, for fp32 results), rounded to whole numbers and cut into signed
-// bytes.  That rounding is below 2^-15 (2^-23) of the group's largest x, and none at all for bf16 values down to a 128th
-// of it (a 2^15th).  The products' sums are exact integers, the offset 8 is their first value (-8 sum x); only then come
-// fp32 numbers: group sum times scale, added up over the groups.
+// which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 4177919, rounded
+// to whole numbers and cut into three signed bytes.  That rounding is below 2^-23 of the group's largest x, and none at
+// all for bf16 values down to a 2^15th of it (two bytes would cost 9 to 13 % less time, but a group with one large value
+// would leave its small ones six bits).  The products' sums are exact integers, the offset 8 is their first value
+// (-8 sum x); only then come fp32 numbers: group sum times scale, added up over the groups.  A slot with many pairs repays
+// the unpacking: there the weights become 16-bit numbers (q - 8, exact) and x stays as it is.
 //
 // A warp owns 32 weight rows and streams them through a ring of its own with TMA, a line of 256 weights of each row (4 KiB)
 // at a time; the products' order within a line is arbitrary as long as both operands agree, so a lane's word of eight
@@ -57,7 +58,8 @@ struct Args {
     int out_fp32;
     int job_rows;               // most pairs of a job
     int stages;                 // of a warp's ring
-    // shared memory: the rows of x being worked on (capacity, bytes a row, of that the first two pieces and the third)
+    // shared memory: the rows of x being worked on (capacity, bytes a row, of that the two higher bytes - or x itself - and the
+    // lowest byte of its numbers)
     int x_cap, x_bytes, x_wide, x_third;
     int at_x, at_bars, at_red, at_jobs, at_start, at_order, at_row;
 };
@@ -121,11 +123,10 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
 constexpr int kFloatBits = 0x4B400000;
 constexpr float kFloat = 12582912.f;
 
-// A line of a row of x (a lane: eight k) into P bytes a number, highest first; per group of 32 SPG its scale 2^-e and the
+// A line of a row of x (a lane: eight k) into three bytes a number, highest first; per group of 32 SPG its scale 2^-e and the
 // sums' first values -8 sum of each byte (the weights' offset).  A group with an infinity or NaN gets the scale NaN.
-template <class T, int P, int SPG>
+template <class T, int SPG>
 __device__ __forceinline__ void convert_line(const uint4 raw, int line, bool there, uint8_t *to, const Args &a) {
-    static_assert(P == 2 || P == 3, "bytes of a number");
     const int lane = threadIdx.x & 31, at_k = line * kLineK + lane * 8;
     const T *v = reinterpret_cast<const T *>(&raw);
     float f[8], most = 0.f;
@@ -139,22 +140,22 @@ __device__ __forceinline__ void convert_line(const uint4 raw, int line, bool the
     if (odd) most = __int_as_float(0x7f800000);
 #pragma unroll
     for (int m = 1; m < 4 * SPG; m <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
-    // signed bytes reach 127 (1 + 256 (+ 65536)): the largest x goes to [2^14, 2^15) ([2^22, 2^23)), or half of that
-    constexpr int kTop = P == 2 ? 14 : 22, kMost = P == 2 ? 32639 : 8355711;
+    // signed bytes reach 127 (1 + 256 + 65536) = 8355711: the largest x goes to [2^22, 2^23), or half of that
+    constexpr int kTop = 22, kMost = 8355711;
     const int e = __float_as_int(most) >> 23;                                // biased exponent of the largest
     int up = min(254 + kTop - e, 253);                                       // biased exponent of the scale
     if (most * __int_as_float(max(up, 1) << 23) > (float)kMost) --up;
     up = max(up, 1);
     const float scale = __int_as_float(up << 23), back = e == 255 ? __int_as_float(0x7fc00000) : __int_as_float((254 - up) << 23);
-    uint32_t u[8], lo[P], hi[P];
-    int sums[P];
+    uint32_t u[8], lo[3], hi[3];
+    int sums[3];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        // number = sum of (byte_j - 128) 256^j for the bytes of number + 0x80 (1 + 256 (+ 65536)); the same bytes with their top
-        // bit turned are byte_j - 128
-        u[i] = (uint32_t)(__float2int_rn(e == 255 ? 0.f : f[i] * scale) + (P == 2 ? 0x8080 : 0x808080)) ^ (P == 2 ? 0x8080u : 0x808080u);
+        // number = sum of (byte_j - 128) 256^j for the bytes of number + 0x808080; the same bytes with their top bit turned are
+        // byte_j - 128
+        u[i] = (uint32_t)(__float2int_rn(e == 255 ? 0.f : f[i] * scale) + 0x808080) ^ 0x808080u;
 #pragma unroll
-    for (int j = 0; j < P; ++j) {                                            // in the order in which a word's nibbles come out
+    for (int j = 0; j < 3; ++j) {                                            // in the order in which a word's nibbles come out
         lo[j] = bytes(u, 0, 4, 1, 5, j);
         hi[j] = bytes(u, 2, 6, 3, 7, j);
         sums[j] = __dp4a((int)lo[j], 0x01010101, __dp4a((int)hi[j], 0x01010101, 0));
@@ -164,16 +165,16 @@ __device__ __forceinline__ void convert_line(const uint4 raw, int line, bool the
 #pragma unroll
     for (int m = 1; m < 4 * SPG; m <<= 1) {
         low += __shfl_xor_sync(0xffffffffu, low, m);
-        if (P == 3) sums[P - 1] += __shfl_xor_sync(0xffffffffu, sums[P - 1], m);
+        sums[2] += __shfl_xor_sync(0xffffffffu, sums[2], m);
     }
     sums[0] = (int)(int16_t)low;
     sums[1] = (low - sums[0]) >> 16;
     if (!there) return;
-    *reinterpret_cast<uint4 *>(to + line * 512 + lane * 16) = make_uint4(lo[P - 1], hi[P - 1], lo[P - 2], hi[P - 2]);
-    if (P == 3) *reinterpret_cast<uint2 *>(to + a.x_wide + line * 256 + lane * 8) = make_uint2(lo[0], hi[0]);
+    *reinterpret_cast<uint4 *>(to + line * 512 + lane * 16) = make_uint4(lo[2], hi[2], lo[1], hi[1]);
+    *reinterpret_cast<uint2 *>(to + a.x_wide + line * 256 + lane * 8) = make_uint2(lo[0], hi[0]);
     if (lane % (4 * SPG) == 0)
         *reinterpret_cast<int4 *>(to + a.x_wide + a.x_third + (at_k / (32 * SPG)) * 16) =
-            make_int4(__float_as_int(back), kFloatBits - 8 * sums[P - 1], kFloatBits - 8 * sums[P - 2], P == 3 ? kFloatBits - 8 * sums[0] : 0);
+            make_int4(__float_as_int(back), kFloatBits - 8 * sums[2], kFloatBits - 8 * sums[1], kFloatBits - 8 * sums[0]);
 }
 
 __device__ __forceinline__ int4 lds4(uint32_t at) {
@@ -182,59 +183,46 @@ __device__ __forceinline__ int4 lds4(uint32_t at) {
     return v;
 }
 
-// One line (N columns of pairs): acc += scale 2^-e (sum of q x 2^e - 8 sum of x 2^e).  w_at: this lane's word of the line's
-// first 32-weight step; 16-byte piece i of row r lies at piece i ^ (r mod 8) of its line, one exclusive-or of the address.
-// xb, xc: this lane's operand bytes of the row's first step, fac0, fac1: of its first group, for the columns 2c and 2c + 1.
-template <class T, int P, int N, int NT, int SPG>
-__device__ __forceinline__ void line_products(float (&acc)[2][NT][4], const uint32_t (&xb)[NT], const uint32_t (&xc)[NT], const uint32_t (&fac0)[NT],
-                                              const uint32_t (&fac1)[NT], uint32_t w_at, uint32_t s_at, int line, int left) {
-    // (with one column a group a pass of the loop, not unrolled: small calls run this code cold, and fetching it is what they
-    // wait for)
-#pragma unroll(NT == 1 ? 1 : 8 / SPG)
+// One line and one column of eight pairs: acc += scale 2^-e (sum of q x 2^e - 8 sum of x 2^e).  w_at: this lane's word of the
+// line's first 32-weight step; 16-byte piece i of row r lies at piece i ^ (r mod 8) of its line, one exclusive-or of the
+// address.  xb, xc: this lane's operand bytes of the row's first step (two higher bytes, lowest byte), fac0, fac1: of its
+// first group, for the columns 2c and 2c + 1.
+template <class T, int SPG>
+__device__ __forceinline__ void line_products(float (&acc)[2][1][4], uint32_t xb, uint32_t xc, uint32_t fac0, uint32_t fac1, uint32_t w_at, uint32_t s_at, int line,
+                                              int left) {
+    // (a group a pass of the loop, not unrolled: small calls run this code cold, and fetching it is what they wait for)
+#pragma unroll 1
     for (int i0 = 0; i0 < 8 && 32 * i0 < left; i0 += SPG) {
-        int sum[P][2][N][4];
-        float f0[N], f1[N];
         const uint32_t g16 = (uint32_t)(line * (8 / SPG) + i0 / SPG) * 16;
+        const int4 v0 = lds4(fac0 + g16), v1 = lds4(fac1 + g16);
+        const float f0 = __int_as_float(v0.x), f1 = __int_as_float(v1.x);
+        int sum[3][2][4];
 #pragma unroll
-        for (int t = 0; t < N; ++t) {
-            const int4 v0 = lds4(fac0[t] + g16), v1 = lds4(fac1[t] + g16);
-            f0[t] = __int_as_float(v0.x);
-            f1[t] = __int_as_float(v1.x);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                sum[0][m][t][0] = sum[0][m][t][2] = v0.y;
-                sum[0][m][t][1] = sum[0][m][t][3] = v1.y;
-                sum[1][m][t][0] = sum[1][m][t][2] = v0.z;
-                sum[1][m][t][1] = sum[1][m][t][3] = v1.z;
-                if (P == 3) {
-                    sum[P - 1][m][t][0] = sum[P - 1][m][t][2] = v0.w;
-                    sum[P - 1][m][t][1] = sum[P - 1][m][t][3] = v1.w;
-                }
+            for (int e = 0; e < 4; ++e) {
+                sum[0][m][e] = e & 1 ? v1.y : v0.y;
+                sum[1][m][e] = e & 1 ? v1.z : v0.z;
+                sum[2][m][e] = e & 1 ? v1.w : v0.w;
             }
-        }
 #pragma unroll
         for (int j = 0; j < SPG; ++j) {
             const int i = i0 + j;
-            uint32_t w[4];
+            uint32_t w[4], lo[4], hi[4], d0, d1;
             asm volatile("ld.shared.b32 %0, [%4];\n\tld.shared.b32 %1, [%4 + 1024];\n\tld.shared.b32 %2, [%4 + 2048];\n\tld.shared.b32 %3, [%4 + 3072];"
                          : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(w_at ^ (i << 4)));
-            uint32_t lo[4], hi[4];
+            const int4 b = lds4(xb + line * 512 + i * 64);
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(d0), "=r"(d1) : "r"(xc + line * 256 + i * 32));
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 lo[h] = w[h] & 0x0F0F0F0Fu;
                 hi[h] = (w[h] >> 4) & 0x0F0F0F0Fu;
             }
 #pragma unroll
-            for (int t = 0; t < N; ++t) {
-                const int4 b = lds4(xb[t] + line * 512 + i * 64);
-                uint32_t d0 = 0, d1 = 0;
-                if (P == 3) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(d0), "=r"(d1) : "r"(xc[t] + line * 256 + i * 32));
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    mma8(sum[0][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.x, b.y);
-                    mma8(sum[1][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.z, b.w);
-                    if (P == 3) mma8(sum[P - 1][m][t], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], d0, d1);
-                }
+            for (int m = 0; m < 2; ++m) {
+                mma8(sum[0][m], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.x, b.y);
+                mma8(sum[1][m], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], b.z, b.w);
+                mma8(sum[2][m], lo[2 * m], lo[2 * m + 1], hi[2 * m], hi[2 * m + 1], d0, d1);
             }
         }
 #pragma unroll
@@ -244,13 +232,11 @@ __device__ __forceinline__ void line_products(float (&acc)[2][NT][4], const uint
             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r1) : "r"(s_at + ((i0 / SPG) * kRows + m * 16) * 2 + 16));
             const float s0 = to_f<T>(*reinterpret_cast<T *>(&r0)), s1 = to_f<T>(*reinterpret_cast<T *>(&r1));
 #pragma unroll
-            for (int t = 0; t < N; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = fmaf(__int_as_float(sum[0][m][t][e]) - kFloat, 256.f, __int_as_float(sum[1][m][t][e]) - kFloat);
-                    if (P == 3) v = fmaf(v, 256.f, __int_as_float(sum[P - 1][m][t][e]) - kFloat);
-                    acc[m][t][e] += ((e < 2 ? s0 : s1) * (e & 1 ? f1[t] : f0[t])) * v;
-                }
+            for (int e = 0; e < 4; ++e) {
+                float v = fmaf(__int_as_float(sum[0][m][e]) - kFloat, 256.f, __int_as_float(sum[1][m][e]) - kFloat);
+                v = fmaf(v, 256.f, __int_as_float(sum[2][m][e]) - kFloat);
+                acc[m][0][e] += ((e < 2 ? s0 : s1) * (e & 1 ? f1 : f0)) * v;
+            }
         }
     }
 }
@@ -300,12 +286,13 @@ __device__ __forceinline__ void line_products_16(float (&acc)[2][NT][4], const u
     }
 }
 
-// T: operand type; P: bytes of a number of x, 0: x in its own type; NT: columns of eight pairs a warp accumulates at a time; SPG: 32-weight
-// steps in a group
-template <class T, int P, int NT, int SPG>
+// T: operand type; NT: columns of eight pairs a warp accumulates at a time, one (x in bytes) or three (x as it is); SPG:
+// 32-weight steps in a group
+template <class T, int NT, int SPG>
 __global__ void __launch_bounds__(kThreads, 1)
 quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ Args a) {
-    const bool wide = P == 3 || (P == 0 && a.out_fp32);
+    constexpr bool BYTES = NT == 1;
+    const bool wide = a.out_fp32;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -314,7 +301,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     Job *jobs = reinterpret_cast<Job *>(smem + a.at_jobs);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + a.at_bars + kWarps * kMaxStages * 8);
     volatile int *n_jobs_at = abort_flag + 1;
-    const uint32_t x_bar = smem_base + a.at_bars + kWarps * kMaxStages * 8 + 8;   // the rows of x of a batch (P = 0)
+    const uint32_t x_bar = smem_base + a.at_bars + kWarps * kMaxStages * 8 + 8;   // the rows of x of a batch that come as they are
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t my_bars = smem_base + a.at_bars + warp * kMaxStages * 8;
     const uint32_t my_ring = smem_base + warp * a.stages * kLineBytes, my_scales = smem_base + kWarps * a.stages * kLineBytes + warp * a.stages * scale_bytes(SPG);
@@ -476,7 +463,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         };
         // The batch's rows of x: contiguous in the order of the pairs.
         const int pair_at = jobs[job0].first;
-        if constexpr (P == 0) {
+        if constexpr (!BYTES) {
             // as they are, one copy a row
             if (warp == 0) {
                 if (lane == 0) mbar_expect_tx(x_bar, (uint32_t)rows * a.k * 2);
@@ -514,7 +501,7 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     if (rows_of[j] >= rows) break;
-                    convert_line<T, P, SPG>(raw[j], lines_of[j], lines_of[j] * kLineK + lane * 8 < a.k, smem + a.at_x + rows_of[j] * a.x_bytes, a);
+                    convert_line<T, SPG>(raw[j], lines_of[j], lines_of[j] * kLineK + lane * 8 < a.k, smem + a.at_x + rows_of[j] * a.x_bytes, a);
                 }
                 fetch();
             }
@@ -556,8 +543,8 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 if (ok) {
                     const uint32_t w_at = my_ring + stage * kLineBytes + r * 144 + c * 4, s_at = my_scales + stage * scale_bytes(SPG) + r * 2;
                     const int left = a.k - line * kLineK;
-                    if constexpr (P != 0) {
-                        line_products<T, P, 1, NT, SPG>(acc, xb, xc, fac0, fac1, w_at, s_at, line, left);
+                    if constexpr (BYTES) {
+                        line_products<T, SPG>(acc, xb[0], xc[0], fac0[0], fac1[0], w_at, s_at, line, left);
                     } else {
                         if (jb.count <= 8) line_products_16<T, 1, NT, SPG>(acc, xb, w_at, s_at, line, left);
                         else if (jb.count <= 16) line_products_16<T, 2, NT, SPG>(acc, xb, w_at, s_at, line, left);
@@ -633,39 +620,35 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
 }
 
-template <class T, int P, int NT, int SPG>
+template <class T, int NT, int SPG>
 ew_status_t launch(const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
-    return launched(launch_pdl(quant_mv_kernel<T, P, NT, SPG>, dim3(ctas), dim3(kThreads), (size_t)smem, st, mq, ms, a), "4-bit product");
+    return launched(launch_pdl(quant_mv_kernel<T, NT, SPG>, dim3(ctas), dim3(kThreads), (size_t)smem, st, mq, ms, a), "4-bit product");
 }
-template <class T, int P, int NT>
+template <class T, int NT>
 ew_status_t launch_group(int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
-    if (group == 32) return launch<T, P, NT, 1>(mq, ms, a, smem, ctas, st);
-    if (group == 64) return launch<T, P, NT, 2>(mq, ms, a, smem, ctas, st);
-    return launch<T, P, NT, 4>(mq, ms, a, smem, ctas, st);
+    if (group == 32) return launch<T, NT, 1>(mq, ms, a, smem, ctas, st);
+    if (group == 64) return launch<T, NT, 2>(mq, ms, a, smem, ctas, st);
+    return launch<T, NT, 4>(mq, ms, a, smem, ctas, st);
 }
 template <class T>
-ew_status_t launch_type(int pieces, int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
-    if (pieces == 0) return launch_group<T, 0, 3>(group, mq, ms, a, smem, ctas, st);
-    if (pieces == 2) return launch_group<T, 2, 1>(group, mq, ms, a, smem, ctas, st);
-    return launch_group<T, 3, 1>(group, mq, ms, a, smem, ctas, st);
+ew_status_t launch_type(int nt, int group, const CUtensorMap &mq, const CUtensorMap &ms, const Args &a, int smem, int ctas, cudaStream_t st) {
+    return nt == 1 ? launch_group<T, 1>(group, mq, ms, a, smem, ctas, st) : launch_group<T, 3>(group, mq, ms, a, smem, ctas, st);
 }
-template <class T, int P, int NT>
+template <class T, int NT>
 int setup_one() {
-    return (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
-           (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
-           (int)cudaFuncSetAttribute(quant_mv_kernel<T, P, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    return (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(quant_mv_kernel<T, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
 }
-template <class T>
-int setup_type() { return setup_one<T, 0, 3>() | setup_one<T, 2, 1>() | setup_one<T, 3, 1>(); }
 
 // Shared memory of a launch: ring and scales, rows of x, barriers, partial tiles, job and pair tables.  As many
 // stages a warp as leave room for the rows of x of a whole job.  Returns the bytes, 0 if not even one row fits.
-int lay_out(Args &a, int nt, int group, int pieces) {
+int lay_out(Args &a, int nt, int group) {
     const int groups = a.k / group;
     // rows of x start 64 bytes apart modulo 128: the two rows that a quarter of a warp reads lie in different banks
     a.x_wide = (a.k * 2 + 127) / 128 * 128 + 64;
-    a.x_third = pieces == 3 ? (a.k + 127) / 128 * 128 : 0;
-    a.x_bytes = pieces ? (a.x_wide + a.x_third + groups * 16 + 127) / 128 * 128 + 64 : a.x_wide;
+    a.x_third = nt == 1 ? (a.k + 127) / 128 * 128 : 0;
+    a.x_bytes = nt == 1 ? (a.x_wide + a.x_third + groups * 16 + 127) / 128 * 128 + 64 : a.x_wide;
     const int live = a.pairs < a.n_slots ? a.pairs : a.n_slots;
     for (a.stages = kMaxStages; a.stages >= 1; --a.stages) {
         const int ring = kWarps * a.stages * (kLineBytes + scale_bytes(group / 32)), bars = kWarps * kMaxStages * 8 + 16, red = kWarps * 1024 * nt;
@@ -739,7 +722,10 @@ __global__ void __launch_bounds__(256) quant_pack_kernel(const T *w, long long l
 }  // namespace
 
 int quant_setup() {
-    return setup_type<__nv_bfloat16>() | setup_type<__half>();
+    // (the packing kernels too: everything is loaded before a graph may be captured)
+    cudaFuncAttributes fa;
+    return setup_one<__nv_bfloat16, 1>() | setup_one<__nv_bfloat16, 3>() | setup_one<__half, 1>() | setup_one<__half, 3>() |
+           (int)cudaFuncGetAttributes(&fa, quant_pack_kernel<__nv_bfloat16>) | (int)cudaFuncGetAttributes(&fa, quant_pack_kernel<__half>);
 }
 
 }  // namespace ops
@@ -793,12 +779,12 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
         // One column of eight pairs where a slot has four pairs or fewer on average, up to three otherwise: what a slot has
         // more is another job, which reads its weights again.
         const int nt = a.pairs <= 8 || a.pairs <= 4 * n_slots ? 1 : 3;
-        const int pieces = nt > 1 ? 0 : out_dtype == EW_FP32 ? 3 : 2, smem = lay_out(a, nt, group, pieces);
+        const int smem = lay_out(a, nt, group);
         if (!smem) return refuse("4-bit product: k is too large for a row of x in shared memory");
         const long long most = ((long long)a.pairs / a.job_rows + (a.pairs < n_slots ? a.pairs : n_slots)) * a.tiles;
         const int grid = (int)(most < d->sm_count ? most : d->sm_count);
         cudaStream_t st = (cudaStream_t)cuda_stream;
-        s = dtype == EW_BF16 ? launch_type<__nv_bfloat16>(pieces, group, mq, ms, a, smem, grid, st) : launch_type<__half>(pieces, group, mq, ms, a, smem, grid, st);
+        s = dtype == EW_BF16 ? launch_type<__nv_bfloat16>(nt, group, mq, ms, a, smem, grid, st) : launch_type<__half>(nt, group, mq, ms, a, smem, grid, st);
         if (s != EW_OK) return s;
     }
     return EW_OK;

@@ -128,7 +128,21 @@ ew_status_t swiglu(bool grad, int32_t device, int32_t dtype, const void *da, int
 #undef EW_PICK
 }
 
+template <class T, int V>
+int load_one() {
+    constexpr int kWarps = kThreads / 32;
+    cudaFuncAttributes fa;
+    return (int)cudaFuncGetAttributes(&fa, swiglu_kernel<T, V, 1, false>) | (int)cudaFuncGetAttributes(&fa, swiglu_kernel<T, V, kWarps, false>) |
+           (int)cudaFuncGetAttributes(&fa, swiglu_kernel<T, V, 1, true>) | (int)cudaFuncGetAttributes(&fa, swiglu_kernel<T, V, kWarps, true>);
+}
+
 }  // namespace
+
+// Loads the kernels (a first launch inside a graph capture would have to).
+int swiglu_setup() {
+    return load_one<__nv_bfloat16, 1>() | load_one<__nv_bfloat16, 8>() | load_one<__half, 1>() | load_one<__half, 8>();
+}
+
 }  // namespace ops
 }  // namespace ew
 
