@@ -92,41 +92,6 @@ __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr) {
     return d;
 }
 
-// Bounded waits.  The thread sleeps in the barrier's hardware wait for up to kNap at a time: the products run at the GPU's
-// power limit, where warps that poll cost clock.
-constexpr uint32_t kNapNs = 4000;
-template <bool PEER>
-__device__ __forceinline__ bool try_nap(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    if constexpr (PEER)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
-    return ok != 0;
-}
-// PEER: on a barrier that receives arrivals from the peer CTA
-template <bool PEER>
-__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
-    if (try_nap<PEER>(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (;;) {
-        if (try_nap<PEER>(bar, parity)) return true;
-        if (*abort_flag) return false;
-        if (clock64() - t0 > kWaitLimitCycles) {
-            *abort_flag = 1;
-            atomicOr(err, 2);
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
-    int ok = 1;
-    if ((threadIdx.x & 31) == 0) ok = wait_on<false>(bar, parity, abort_flag, err) ? 1 : 0;
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
-}
-
 template <int CG>
 __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar) {
     if constexpr (CG == 1) tma_load_2d(dst, m, x, y, bar);
