@@ -17,6 +17,19 @@
 // in steps of 16: a group of few rows costs few tensor-core cycles and the kernel is then a stream of its weights.  The
 // operand whose summed axis is contiguous is staged K-major, the other MN-major: the tensor core transposes, nothing is
 // moved for it.
+//
+// Three tile widths, by the rows a group has on average: up to 32 rows, 64 columns on one CTA (nine stages of 24 KiB: with 32
+// columns and twelve stages the smallest calls were 3 % slower); up to 96, 128 columns; beyond, a CTA pair with 256 f x 256
+// columns, every operand byte crossing from L2 once per 256 x 256 tile.
+//
+// Measured (one B200; copy bandwidth 6551 GB/s, cuBLAS bf16 1655 TFLOP/s in a burst, 1403 sustained):
+//   y,  1536 rows, 96 groups, 2816 x 2048   174 us = 6.44 TB/s, 98 % of the copy bandwidth (bound by the weights' bytes)
+//   y, 49152 rows, 64 groups, 2816 x 2048   500 us sustained = 1130 TFLOP/s (1337 in a burst), bound by the tensor cores at
+//                                           the power limit; the MMA thread waits for data 17 % of the time
+//   dx, 24582 rows, 64 groups, 2048 x 1408  150 to 170 us: 384 rows a group leave 192-column tiles, and a tile costs 218 ns a
+//                                           k-block plus 0.7 ns a column whatever its width
+//   dw, 12289 rows, 32 groups, fp32         185 to 215 us = 4.2 TB/s: 738 MB of results leave at the write bandwidth
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
