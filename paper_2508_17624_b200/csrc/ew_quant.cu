@@ -11,8 +11,8 @@
 // they are: one mask, or a shift and a mask, turns a word into four bytes 0..15, and the 8-bit integer m16n8k32
 // instruction multiplies 512 weights with eight pairs (2.1 cycles of an SM measured, what bf16 takes for 256; the 8-bit
 // floating-point form is made of 16-bit ones on this machine and slower).  x goes in as fixed-point numbers: a group of x,
-// which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 4177919, rounded
-// to whole numbers and cut into three signed bytes.  That rounding is below 2^-23 of the group's largest x, and none at
+// which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 4177855, rounded
+// to whole numbers and cut into three signed bytes.  That rounding is below 1/8355711 of the group's largest x, and none at
 // all for bf16 values down to a 2^15th of it (two bytes would cost 9 to 13 % less time, but a group with one large value
 // would leave its small ones six bits).  The products' sums are exact integers, the offset 8 is their first value
 // (-8 sum x); only then come fp32 numbers: group sum times scale, added up over the groups.  A slot with many pairs repays
@@ -145,7 +145,8 @@ __device__ __forceinline__ void convert_line(const uint4 raw, int line, bool the
     if (odd) most = __int_as_float(0x7f800000);
 #pragma unroll
     for (int m = 1; m < 4 * SPG; m <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
-    // signed bytes reach 127 (1 + 256 + 65536) = 8355711: the largest x goes to [2^22, 2^23), or half of that
+    // signed bytes reach 127 (1 + 256 + 65536) = 8355711: the largest x goes to [2^22, 2^23), or half of that if it
+    // is more, i.e. above 4177855
     constexpr int kTop = 22, kMost = 8355711;
     const int e = __float_as_int(most) >> 23;                                // biased exponent of the largest
     int up = min(254 + kTop - e, 253);                                       // biased exponent of the scale
@@ -517,8 +518,9 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 }
                 fetch();
             }
-            __syncthreads();
         }
+        // (the rows of x are in place, and the last batch's partial tiles have been read)
+        __syncthreads();
 
         float acc[2][NT][4];
         Job jb = {};

@@ -146,10 +146,10 @@ def check_quant(slots, n_slots, n, k, group, dtype=BF16, out_dtype=None, per_row
             assert not y[at].any()
             continue
         xd = x[[i // step for i in at]].double()
-        # x may enter as fixed-point numbers whose largest in a group is above 4177919: rounding them costs at most 1/2, i.e.
-        # 2^-23 of the group's largest x, a weight
+        # x may enter as fixed-point numbers whose largest in a group is above 4177855: rounding them costs at most 1/2, i.e.
+        # 1/8355711 of the group's largest x, a weight
         most = xd.view(len(at), k // group, group).abs().amax(2, keepdim=True).expand(-1, -1, group).reshape(len(at), k)
-        near(y[at], xd @ w[s].t(), xd.abs() @ w[s].abs().t(), 2 * k, ("slot", s), 2.0 ** -23 * (most @ w[s].abs().t()))
+        near(y[at], xd @ w[s].t(), xd.abs() @ w[s].abs().t(), 2 * k, ("slot", s), (most / 8355711 @ w[s].abs().t()))
 
 
 def some_slots(tokens, per, n_slots, seed=0):
@@ -194,9 +194,9 @@ def test_quant_outliers_leave_the_other_values_their_bits(dtype):
     ref = x.double() @ unpacked(q, scales)[0].t()
     rest = x.double().clone()
     rest[0, 77] = 0
-    # fixed point: half a step of 6000 / 4177920 a value, against sums of 255 values of about 1
+    # fixed point: half a step, 6000 / 8355711, a value, against sums of 255 values of about 1
     assert (y - ref).norm() / ref.norm() <= 1e-3
-    assert ((y - ref).abs() <= 0.5 * 6000 / 4177920 * unpacked(q, scales)[0].abs().sum(1) + 1e-5 * (rest.abs() @ unpacked(q, scales)[0].abs().t())).all()
+    assert ((y - ref).abs() <= 6000 / 8355711 * unpacked(q, scales)[0].abs().sum(1) + 1e-5 * (rest.abs() @ unpacked(q, scales)[0].abs().t())).all()
 
 
 def test_quant_rows_do_not_touch_one_another():

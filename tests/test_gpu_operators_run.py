@@ -164,6 +164,16 @@ def test_two_streams_and_repeated_calls_give_the_same_bits():
             assert torch.equal(a, b)
 
 
+def test_busy_slots_in_several_batches_give_the_same_bits_every_time():
+    """1536 pairs over 20 slots: a CTA works through several batches of rows, partial tiles in each."""
+    x = torch.randn((256, 2048), device="cuda").to(BF16)
+    q, s = binding.quant_pack((torch.randn((20, 328, 2048), device="cuda") * 0.05).to(BF16), 64)
+    slots = torch.randint(0, 20, (256, 6), dtype=torch.int32, device="cuda")
+    first = binding.quant_mv(x, q, s, slots, out_dtype=FP32)
+    for _ in range(40):
+        assert torch.equal(first, binding.quant_mv(x, q, s, slots, out_dtype=FP32))
+
+
 def test_captured_and_replayed_with_new_inputs():
     """Two graphs over the same weights, replayed in turn with changing inputs, offsets and slots."""
     w = (torch.randn((6, 264, 256), device="cuda") * 0.05).to(BF16)
