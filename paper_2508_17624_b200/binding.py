@@ -348,7 +348,7 @@ def _good(t, dev, dtype, ndim) -> bool:
 
 def _matrix(t, dev, dtype, name, like):
     """(rows, width, elements between rows) of a matrix; one row alone has no stride of its own."""
-    if not _good(t, dev, dtype, 2) or dev < 0:
+    if t.get_device() != dev or t.dtype is not dtype or t.dim() != 2 or dev < 0:
         _on(t, like, 2, name, dtype)
     (rows, width), (ld, one) = t.shape, t.stride()
     if one != 1 and width > 1 and rows:
@@ -358,7 +358,7 @@ def _matrix(t, dev, dtype, name, like):
 
 def _matrices(t, dev, dtype, name, like):
     """(matrices, rows, width, elements between rows, between matrices)."""
-    if not _good(t, dev, dtype, 3) or dev < 0:
+    if t.get_device() != dev or t.dtype is not dtype or t.dim() != 3 or dev < 0:
         _on(t, like, 3, name, dtype)
     (g, n, k), (stride, ld, one) = t.shape, t.stride()
     if one != 1 and k > 1:
@@ -368,10 +368,11 @@ def _matrices(t, dev, dtype, name, like):
 
 
 def _offsets(offsets, dev, T, like):
-    if offsets.get_device() != dev or offsets.dtype is not T.int32 or offsets.dim() != 1 or offsets.shape[0] < 2 or offsets.stride(0) != 1:
+    n = offsets.numel()
+    if offsets.get_device() != dev or offsets.dtype is not T.int32 or offsets.dim() != 1 or n < 2 or not offsets.is_contiguous():
         _on(offsets, like, 1, "offsets")
         raise ValueError("offsets: a contiguous int32 tensor with one more entry than groups is wanted")
-    return offsets.shape[0] - 1
+    return n - 1
 
 
 def _result(out, shape, dtype, like, name="out"):
@@ -396,7 +397,7 @@ def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
         out_dtype = dtype if out is None else out.dtype
     wide = k if grad else n
     if out is None:
-        out, ldo = a.new_empty((rows, wide), dtype=out_dtype), wide
+        out, ldo = a.new_empty((rows, wide)) if out_dtype is dtype else a.new_empty((rows, wide), dtype=out_dtype), wide
     else:
         out = _result(out, (rows, wide), out_dtype, a)
         ldo = out.stride(0) if rows > 1 else wide
@@ -475,7 +476,7 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     if not _good(scales, dev, dtype, 3):
         _on(scales, x, 3, "scales", dtype)
     (n_slots, n, half), (s_slots, groups, s_n) = q.shape, scales.shape
-    if half * 2 != k or groups < 1 or k % groups or s_slots != n_slots or s_n != n or not (q.is_contiguous() and scales.is_contiguous()):
+    if half * 2 != k or groups < 1 or k % groups or s_slots != n_slots or s_n != n or not q.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"x {tuple(x.shape)}, q {tuple(q.shape)} and scales {tuple(scales.shape)} do not belong together")
     pairs, slots_at, per_row = rows, None, 1
     if slots is not None:
@@ -488,7 +489,7 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     if out_dtype is None:
         out_dtype = dtype if out is None else out.dtype
     if out is None:
-        out, ldo = x.new_empty((pairs, n), dtype=out_dtype), n
+        out, ldo = x.new_empty((pairs, n)) if out_dtype is dtype else x.new_empty((pairs, n), dtype=out_dtype), n
     else:
         out = _result(out, (pairs, n), out_dtype, x)
         ldo = out.stride(0) if pairs > 1 else n

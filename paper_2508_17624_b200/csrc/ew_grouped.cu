@@ -509,13 +509,20 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     cfg.dynamicSmemBytes = (size_t)a.stages * C::kStageBytes + 1024 + kBarBytes + a.table_bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    int attrs = 0;
+    if (CG > 1) {
+        attr[attrs].id = cudaLaunchAttributeClusterDimension;
+        attr[attrs].val.clusterDim.x = CG;
+        attr[attrs].val.clusterDim.y = attr[attrs].val.clusterDim.z = 1;
+        ++attrs;
+    }
+    if (pdl_enabled()) {
+        attr[attrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[attrs].val.programmaticStreamSerializationAllowed = 1;
+        ++attrs;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    cfg.numAttrs = attrs;
     return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, EW, WAY>, ma, mb, a), "grouped product");
 }
 

@@ -1,6 +1,7 @@
 // What the stand-alone operators keep per device: its size, the tensor-map encoder and one error word.
 #include "ew_ops.h"
 
+#include <atomic>
 #include <mutex>
 
 namespace ew {
@@ -12,7 +13,7 @@ __device__ int g_operator_error;
 
 std::mutex g_mutex;
 Device g_devices[kMaxDevices];
-bool g_ready[kMaxDevices];
+std::atomic<bool> g_ready[kMaxDevices];
 
 ew_status_t resolve(Device *d, int device) {
     void *fn = nullptr, *err = nullptr;
@@ -31,11 +32,13 @@ ew_status_t resolve(Device *d, int device) {
 
 ew_status_t device_state(int device, const Device **out) {
     if (device >= kMaxDevices) return refuse("device ordinal out of range");
-    std::lock_guard<std::mutex> lock(g_mutex);
-    if (!g_ready[device]) {
-        const ew_status_t s = resolve(&g_devices[device], device);
-        if (s != EW_OK) return s;
-        g_ready[device] = true;
+    if (!g_ready[device].load(std::memory_order_acquire)) {
+        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!g_ready[device].load(std::memory_order_relaxed)) {
+            const ew_status_t s = resolve(&g_devices[device], device);
+            if (s != EW_OK) return s;
+            g_ready[device].store(true, std::memory_order_release);
+        }
     }
     *out = &g_devices[device];
     return EW_OK;
