@@ -183,6 +183,12 @@ __device__ __forceinline__ void convert_line(const uint4 raw, int line, bool the
             make_int4(__float_as_int(back), kFloatBits - 8 * sums[2], kFloatBits - 8 * sums[1], kFloatBits - 8 * sums[0]);
 }
 
+template <int OFFSET>
+__device__ __forceinline__ uint32_t lds(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1 + %2];" : "=r"(v) : "r"(at), "n"(OFFSET));
+    return v;
+}
 __device__ __forceinline__ int4 lds4(uint32_t at) {
     int4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -216,8 +222,11 @@ __device__ __forceinline__ void line_products(float (&acc)[2][1][4], uint32_t xb
         for (int j = 0; j < SPG; ++j) {
             const int i = i0 + j;
             uint32_t w[4], lo[4], hi[4], d0, d1;
-            asm volatile("ld.shared.b32 %0, [%4];\n\tld.shared.b32 %1, [%4 + 1024];\n\tld.shared.b32 %2, [%4 + 2048];\n\tld.shared.b32 %3, [%4 + 3072];"
-                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(w_at ^ (i << 4)));
+            const uint32_t piece = w_at ^ (i << 4);
+            w[0] = lds<0>(piece);
+            w[1] = lds<1024>(piece);
+            w[2] = lds<2048>(piece);
+            w[3] = lds<2048 + 1024>(piece);
             const int4 b = lds4(xb + line * 512 + i * 64);
             asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(d0), "=r"(d1) : "r"(xc + line * 256 + i * 32));
 #pragma unroll
@@ -259,8 +268,11 @@ __device__ __forceinline__ void line_products_16(float (&acc)[2][NT][4], const u
         for (int j = 0; j < SPG; ++j) {
             const int i = i0 + j;
             uint32_t w[4];
-            asm volatile("ld.shared.b32 %0, [%4];\n\tld.shared.b32 %1, [%4 + 1024];\n\tld.shared.b32 %2, [%4 + 2048];\n\tld.shared.b32 %3, [%4 + 3072];"
-                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(w_at ^ (i << 4)));
+            const uint32_t piece = w_at ^ (i << 4);
+            w[0] = lds<0>(piece);
+            w[1] = lds<1024>(piece);
+            w[2] = lds<2048>(piece);
+            w[3] = lds<2048 + 1024>(piece);
             int4 b[N];
 #pragma unroll
             for (int t = 0; t < N; ++t) b[t] = lds4(xb[t] + line * 512 + i * 64);

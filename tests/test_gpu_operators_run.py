@@ -224,6 +224,27 @@ def test_offsets_out_of_order_or_range_are_clamped_and_reported(offsets):
     assert binding.last_operator_error() == 1 and torch.equal(dw[0], dw[1])
 
 
+def test_results_beyond_two_to_the_31_elements():
+    """2.2 G elements of y, of dh and of dw: the last rows against the formula."""
+    rows, n, k = 1_100_003, 2048, 64
+    x, w = torch.randn((rows, k), device="cuda").to(BF16), torch.randn((3, n, k), device="cuda").to(BF16)
+    offsets = torch.tensor([0, 500_001, 500_001, rows], dtype=torch.int32, device="cuda")
+    y = binding.grouped_mm(x, w, offsets)
+    for at, g in ((slice(0, 70), 0), (slice(rows - 70, rows), 2)):
+        assert rel(y[at], x[at].double() @ w[g].double().t()) <= HALF_STEP
+    dh = binding.swiglu_grad(y[:, :1024], y)
+    g, u, d = y[-9:, :1024].double(), y[-9:, 1024:].double(), y[-9:, :1024].double()
+    sig = torch.sigmoid(g)
+    assert rel(dh[-9:], torch.cat((d * u * sig * (1 + g * (1 - sig)), d * g * sig), 1)) <= HALF_STEP
+    del y, dh
+    groups, n, k = 540, 2040, 2048
+    dy, x = torch.randn((groups, n), device="cuda").to(FP16), torch.randn((groups, k), device="cuda").to(FP16)
+    dw = binding.grouped_mm_dw(dy, x, torch.arange(groups + 1, dtype=torch.int32, device="cuda"))
+    for g in (0, groups - 1):
+        assert rel(dw[g], torch.outer(dy[g].double(), x[g].double())) <= 2.0 ** -11
+    assert binding.last_operator_error() == 0
+
+
 def test_more_pairs_than_one_launch_takes():
     """5000 pairs of 250 tokens, 20 a token, over 40 slots, some without one: the launches divide inside a token's pairs."""
     slots = torch.randint(-1, 40, (250, 20), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5))
