@@ -342,9 +342,9 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         prefetch_map(&map_q);
         prefetch_map(&map_s);
     }
-    // (the tables from which the pairs are grouped - per warp and slot the pairs before it, per pair its place - lie where the
-    // ring and the rows of x will be)
-    uint16_t *before = reinterpret_cast<uint16_t *>(smem), *place = before + kWarps * (a.n_slots + 1), *slot_of = place + a.pairs;
+    // (the table from which the pairs are grouped - per warp and slot the pairs before it - lies where the ring and the rows of x
+    // will be)
+    uint16_t *before = reinterpret_cast<uint16_t *>(smem);
     const int kinds = a.n_slots + 1;                                         // the last one: pairs without a slot
     const bool few = a.pairs <= 32;
     if (!few)
@@ -391,22 +391,19 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         const int stretch = ((a.pairs + kThreads - 1) / kThreads) * 32, p_end = min(a.pairs, (warp + 1) * stretch);
         uint16_t *mine = before + warp * kinds;
         constexpr int kMost = (kMaxPairs + kThreads - 1) / kThreads;
-        int s_of[kMost];
+        int s_of[kMost], place[kMost];
 #pragma unroll
-        for (int j = 0; j < kMost; ++j) s_of[j] = slot_at(warp * stretch + 32 * j + lane, warp * stretch + 32 * j + lane < p_end);
+        for (int j = 0; j < kMost; ++j) s_of[j] = 32 * j < stretch ? slot_at(warp * stretch + 32 * j + lane, warp * stretch + 32 * j + lane < p_end) : -1;
 #pragma unroll
         for (int j = 0; j < kMost; ++j) {
-            const int p = warp * stretch + 32 * j + lane, s = s_of[j];
-            const bool there = p < p_end;
+            if (32 * j >= stretch) break;
+            const int s = s_of[j];
             const uint32_t same = __match_any_sync(0xffffffffu, s);
-            const int rank = __popc(same & ((1u << lane) - 1)), prior = there ? mine[s] : 0;
+            const int rank = __popc(same & ((1u << lane) - 1)), prior = s >= 0 ? mine[s] : 0;
             __syncwarp();
-            if (there && rank == 0) mine[s] = (uint16_t)(prior + __popc(same));
+            if (s >= 0 && rank == 0) mine[s] = (uint16_t)(prior + __popc(same));
             __syncwarp();
-            if (there) {
-                place[p] = (uint16_t)(prior + rank);
-                slot_of[p] = (uint16_t)s;
-            }
+            place[j] = prior + rank;
         }
         __syncthreads();
         for (int g = threadIdx.x; g < kinds; g += kThreads) {
@@ -435,11 +432,13 @@ quant_mv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             if (lane == 0) *n_jobs_at = jobs_before;
         }
         __syncthreads();
-        for (int p = threadIdx.x; p < a.pairs; p += kThreads) {
-            const int s = slot_of[p], to = start[s] + before[(p / stretch) * kinds + s] + place[p];
-            order[to] = (uint16_t)p;
-            x_row[to] = (uint16_t)((p + a.lead) / a.share);
-        }
+#pragma unroll
+        for (int j = 0; j < kMost; ++j)
+            if (s_of[j] >= 0) {
+                const int p = warp * stretch + 32 * j + lane, to = start[s_of[j]] + mine[s_of[j]] + place[j];
+                order[to] = (uint16_t)p;
+                x_row[to] = (uint16_t)((p + a.lead) / a.share);
+            }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the ring belongs to the copies from here on
     }
     __syncthreads();
@@ -703,8 +702,8 @@ int lay_out(Args &a, int nt, int group) {
         a.at_start = o; o += (a.n_slots + 1) * 4;
         a.at_order = o; o += a.pairs * 2;
         a.at_row = o; o += a.pairs * 2;
-        // the grouping tables lie where ring and rows of x will be
-        if (kWarps * (a.n_slots + 1) * 2 + a.pairs * 4 <= a.at_bars) return o + 1024;
+        // the grouping table lies where ring and rows of x will be
+        if (kWarps * (a.n_slots + 1) * 2 <= a.at_bars) return o + 1024;
     }
     return 0;
 }

@@ -171,6 +171,15 @@ def test_quant_batches(tokens, per, n_slots, per_row):
     check_quant(some_slots(tokens, per, n_slots, 3), n_slots, 72, 512, 64, BF16, FP32, per_row=per if per_row == "token" else 1, seed=2)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+def test_quant_longest_rows(group):
+    """k = 16384: few rows of x fit a CTA at a time."""
+    check_quant(some_slots(3, 2, 4), 4, 24, 16384, group, BF16, per_row=2)
+    check_quant(None, 1, 40, 16384, group, FP16, FP32, per_row=50, seed=3)
+    slots = torch.arange(2048, dtype=torch.int32, device="cuda").flip(0).contiguous()
+    check_quant(slots, 2048, 8, 128, group, BF16, per_row=1)
+
+
 def test_quant_pairs_without_a_slot():
     slots = some_slots(12, 6, 20, 5)
     slots[3] = -1
