@@ -315,14 +315,30 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
         it.chunk = chunks > 1 ? (it.kb + chunks - 1) / chunks : it.kb;
         return it;
     };
+    // A role's walk through this unit's items.  Finding an item takes a few hundred cycles of divisions and look-ups, which for a
+    // weight gradient of few rows was most of the copying thread's time: the warp finds 32 items at once, a lane each.
+    Item found = {};
+    auto next_item = [&](int i, int turn) -> Item {
+        if ((turn & 31) == 0) found = item_at(min(i + lane * units, n_items - 1));
+        Item it;
+        const int from = turn & 31;
+        it.g = __shfl_sync(0xffffffffu, found.g, from);
+        it.f0 = __shfl_sync(0xffffffffu, found.f0, from);
+        it.row0 = __shfl_sync(0xffffffffu, found.row0, from);
+        it.cols = __shfl_sync(0xffffffffu, found.cols, from);
+        it.kb = __shfl_sync(0xffffffffu, found.kb, from);
+        it.tail = __shfl_sync(0xffffffffu, found.tail, from);
+        it.chunk = __shfl_sync(0xffffffffu, found.chunk, from);
+        return it;
+    };
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
-        if (lane == 0) {
-            uint32_t stage = 0, phase = 0;
-            bool ok = true;
-            for (int i = unit; i < n_items && ok; i += units) {
-                const Item it = item_at(i);
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
+            const Item it = next_item(i, turn);
+            if (lane == 0) {
                 const int n = (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const int n_cta = n / CG;                                    // c of this item that each CTA stages
                 const int f = it.f0 + (int)rank * 128;
@@ -365,22 +381,23 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
                 }
             }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (the leader CTA's)
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
             const uint32_t type = a.fp16 ? 0u : (1u << 7) | (1u << 10);
             const uint32_t base = (1u << 4) | type | (WAY != kProduct ? 1u << 15 : 0u) | (DW ? 1u << 16 : 0u) |
                                   ((uint32_t)(C::kTile >> 4) << 24);
             const uint32_t bar_in = DW ? bar_ready : bar_full;
             bool ok = true;
-            for (int i = unit; i < n_items && ok; i += units) {
-                const Item it = item_at(i);
+            for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
+                const Item it = next_item(i, turn);
                 if (DW && it.kb == 0) continue;                              // an empty group: the epilogue writes its zeros
                 const int n = DW ? NT : (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
-                for (int kb = 0; kb < it.kb && ok;) {
+                for (int kb = 0; lane == 0 && kb < it.kb && ok;) {
                     if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + acc * NT;
@@ -404,6 +421,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     commit<CG>(bar_tfull + 8 * acc);
                     if (++acc == 2) { acc = 0; acc_phase ^= 1; }
                 }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
             }
         }
     } else if (warp == kRelayWarp) {
@@ -413,8 +431,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
         if (DW) {
             uint32_t stage = 0, phase = 0;
             bool ok = true;
-            for (int i = unit; i < n_items && ok; i += units) {
-                const Item it = item_at(i);
+            for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
+                const Item it = next_item(i, turn);
                 for (int kb = 0; kb < it.kb; ++kb) {
                     if (!(ok = wait_warp(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
                     if (kb == it.kb - 1 && (it.tail & 15)) {
@@ -433,17 +451,17 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
         }
     } else {
         // ------------------------------------------------------------------ epilogue (EW warps of each CTA)
-        const int lg = warp & 3, turn = (warp - 2) >> 2;                     // the TMEM lanes this warp may read; its columns
+        const int lg = warp & 3, half = (warp - 2) >> 2;                     // the TMEM lanes this warp may read; its columns
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
-        for (int i = unit; i < n_items && ok; i += units) {
-            const Item it = item_at(i);
+        for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
+            const Item it = next_item(i, turn);
             const int f = it.f0 + (int)rank * 128 + lg * 32 + lane;
             const bool f_ok = f < a.f_size;
             const size_t at = (DW ? (size_t)it.g * a.group_out : 0) + (size_t)it.row0 * a.ldo + f;
             if (DW && it.kb == 0) {
                 if (f_ok && WAY == kWeightGrad)
-                    for (int j = turn; j < it.cols; j += EW / 4) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
+                    for (int j = half; j < it.cols; j += EW / 4) store_zero(a.out, at + (size_t)j * a.ldo, a.out_kind);
                 continue;
             }
             for (int kb = 0; kb < it.kb; kb += it.chunk) {
@@ -451,7 +469,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 tc_fence_after();
                 const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
 #pragma unroll 1
-                for (int c0 = 32 * turn; c0 < it.cols; c0 += 8 * EW) {
+                for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * EW) {
                     uint32_t v[32];
                     tc_ld32(t0 + c0, v);               // columns behind the item's last are in the accumulator set, not stored
                     tc_wait_ld();
