@@ -23,8 +23,8 @@
 // weights meets the same eight k of x without any shuffling.  A CTA's tiles are contiguous and its lines are dealt to
 // its warps evenly; a tile that crosses from one warp to the next is added up in shared memory, in order.
 //
-// Measured (one B200, copy bandwidth 6551 GB/s), 2816 x 2048 weights unless said: one token's six experts 9.0 us (18 MB; 2.7 us
-// of bytes behind a launch, the slots' way from memory and the first line's); 48 experts of a pair each 32 us = 4.5 TB/s; 96
+// Measured (one B200, copy bandwidth 6551 GB/s), 2816 x 2048 weights unless said: one token's six experts 8.9 us (18 MB; 2.7 us
+// of bytes behind a launch, the slots' way from memory and the first line's); 96
 // pairs over 96 slots of 2048 x 1408 27 us = 3.4 TB/s; 256 tokens, some sixteen pairs a slot, 114 us = 2.7 TB/s, bound by the
 // instructions around the products (73 % of the issue slots while a line is worked on).
 #include <cuda_bf16.h>
