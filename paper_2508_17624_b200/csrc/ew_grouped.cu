@@ -18,9 +18,9 @@
 // operand whose summed axis is contiguous is staged K-major, the other MN-major: the tensor core transposes, nothing is
 // moved for it.
 //
-// Three tile widths, by the rows a group has on average: up to 32 rows, 64 columns on one CTA (nine stages of 24 KiB: with 32
-// columns and twelve stages the smallest calls were 3 % slower); up to 96, 128 columns; beyond, a CTA pair with 256 f x 256
-// columns, every operand byte crossing from L2 once per 256 x 256 tile.
+// Two tile widths, by the rows a group has on average: up to 128 rows, 128 columns on one CTA (64 columns and nine stages were
+// up to 8 % slower from 16 rows a group on, 32 columns and twelve stages 3 % slower for one); beyond, a CTA pair with 256 f x
+// 256 columns, every operand byte crossing from L2 once per 256 x 256 tile.
 //
 // Measured (one B200; copy bandwidth 6551 GB/s, cuBLAS bf16 1655 TFLOP/s in a burst, 1403 sustained):
 //   y,  1536 rows, 96 groups, 2816 x 2048   174 us = 6.44 TB/s, 98 % of the copy bandwidth (bound by the weights' bytes)
@@ -596,8 +596,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     }
     if (s != EW_OK) return s;
     const uint64_t xd[2] = {(uint64_t)t, (uint64_t)rows}, xs[1] = {(uint64_t)ldx * 2};
-    const int most_boxes = rows <= 32ll * groups ? 2 : 4;                    // (the narrowest form stages up to 64 rows)
-    for (int i = 0; i < most_boxes; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const uint32_t box[2] = {64, 32u * (i + 1)};
         if ((s = encode_map(*d, &mb.m[i], map_type(dtype), x, 2, xd, xs, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
     }
@@ -621,8 +620,9 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
         const long long items = (live + rows / NT) * a.f_tiles;                                                               \
         return grad ? launch<CG, NT, 4, kInputGrad>(*d, ma, mb, a, items, st) : launch<CG, NT, 4, kProduct>(*d, ma, mb, a, items, st); \
     } while (0)
-    if (rows <= 32ll * groups) EW_LAUNCH(1, 64);
-    if (rows <= 96ll * groups) EW_LAUNCH(1, 128);
+    // (64 groups of 2816 x 2048, one CTA with 128 columns against the pair: 96 rows a group 127.7 and 130.0 us, 128 rows 134.1 and
+    // 134.7, 160 rows 214 and 141)
+    if (rows <= 128ll * groups) EW_LAUNCH(1, 128);
     EW_LAUNCH(2, 256);
 #undef EW_LAUNCH
 }
@@ -630,7 +630,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
 }  // namespace
 
 int grouped_setup() {
-    return setup_one<1, 64, 4, kProduct>() | setup_one<1, 64, 4, kInputGrad>() | setup_one<1, 128, 4, kProduct>() | setup_one<1, 128, 4, kInputGrad>() |
+    return setup_one<1, 128, 4, kProduct>() | setup_one<1, 128, 4, kInputGrad>() |
            setup_one<2, 256, 4, kProduct>() | setup_one<2, 256, 4, kInputGrad>() | setup_one<2, 256, 4, kWeightGrad>() | setup_one<2, 256, 8, kWeightGrad>() |
            setup_one<2, 256, 8, kWeightAdd>();
 }

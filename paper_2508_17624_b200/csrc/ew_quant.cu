@@ -801,9 +801,11 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
         a.x = (const uint8_t *)x + (size_t)(p0 / pairs_per_row) * ldx * 2;
         a.lead = p0 % pairs_per_row;
         a.slots = slots ? slots + p0 : nullptr;
-        // One column of eight pairs where a slot has four pairs or fewer on average, up to three otherwise: what a slot has
-        // more is another job, which reads its weights again.
-        const int nt = a.pairs <= 8 || a.pairs <= 4 * n_slots ? 1 : 3;
+        // One column of eight pairs with x in bytes, or up to three with x as it is: what a slot has more is another job, which
+        // reads its weights again.  The bytes' sums are scaled group by group, so they pay with long groups and few pairs.
+        // Measured (64 slots of 2816 x 2048; bytes, then 16 bits): groups of 128 with 2 pairs a slot 42 and 48 us, 4: 52 and 53,
+        // 8: 70 and 60; groups of 64 with 1 pair 37.6 and 38.4, 3: 57 and 56, 6: 71 and 62.
+        const int nt = a.pairs <= 8 || 24ll * a.pairs <= (long long)n_slots * group ? 1 : 3;
         const int smem = lay_out(a, nt, group);
         if (!smem) return refuse("4-bit product: k is too large for a row of x in shared memory");
         const long long most = ((long long)a.pairs / a.job_rows + (a.pairs < n_slots ? a.pairs : n_slots)) * a.tiles;
