@@ -768,7 +768,8 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
     if (bad_group(group, k) || k > kMaxK) return refuse("4-bit product: groups of 32, 64 or 128 weights that divide k, k at most 16384");
     if (pairs < 0 || pairs_per_row < 1 || pairs % pairs_per_row || n_slots < 1 || n_slots > kMaxSlots || n < 8 || n % 8 || (int64_t)n_slots * n > 0x7fffffff || (int64_t)kMaxPairs * ((n + kRows - 1) / kRows) > 0x7fffffff)
         return refuse("4-bit product: size out of range (n in multiples of 8, at most 2048 slots)");
-    if (!slots && n_slots != 1) return refuse("4-bit product: without slot ids there is one matrix");
+    // (a tensor without entries may have no address)
+    if (pairs > 0 && !slots && n_slots != 1) return refuse("4-bit product: without slot ids there is one matrix");
     if (ldx < k || (ldx & 7) || ldy < n || !q || !scales || (((uintptr_t)q | (uintptr_t)scales) & 15) || ((uintptr_t)slots & 3) ||
         (pairs > 0 && (!x || ((uintptr_t)x & 15) || !y || ((uintptr_t)y & (elem_bytes(out_dtype) - 1)))))
         return refuse("4-bit product: null or misaligned pointer, or overlapping rows (x, q and scales on 16 bytes, ldx a multiple of 8)");
