@@ -329,7 +329,10 @@ typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2 } ew_dtype_t;
 /* Matrix product grouped by expert (Section 2.1's grouped matrix multiplication, on its own): for every group g and
  * its rows offsets[g] <= r < offsets[g+1]
  *     y[r, :] = x[r, :] w[g]^T        x [rows, k], w [groups, n, k] (group_stride elements between groups), y [rows, n]
- * accumulated in fp32 and rounded once.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
+ * summed in fp32 and rounded once.  The tensor core cuts the running sum off instead of rounding it; sums are made in parts
+ * (1024 terms for fp32 results, 8192 for fp16, 65536 for bf16) that are added up rounded, so that the result is off by at most
+ * 1e-5 (fp32 results) or an eighth of half a step of its type (16-bit ones) of sum |x w| besides its own rounding, whatever the
+ * length.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
  * they need not start at 0 nor end at `rows`, and rows outside them are left as they were.  An offset below the one
  * before it or outside [0, rows] is clamped and reported as EW_ERR_INVALID_ARG.
  * dtype: EW_BF16 or EW_FP16; out_dtype: the same or EW_FP32.  x and w are 16-byte aligned with ldx, ldw and

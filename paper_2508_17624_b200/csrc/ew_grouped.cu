@@ -49,10 +49,13 @@ constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one s
 constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 12;
-// The tensor core cuts off, rather than rounds, what a product has below the running sum's last bit: over a sum of 2048
-// terms 1.2e-6 of the result (2-norm), growing with the length.  fp32 results are therefore summed 1024 terms at a time, and
-// the epilogue adds the parts up in fp32 in the output (always the same thread's part of it); 16-bit results do not see it.
-constexpr int kSumBlocks = 16;
+// The tensor core cuts off, rather than rounds, what a product has below the running sum's last bit.  Over terms of one sign
+// that takes 6.4e-9 of the result a term (5.8e-6 at 1024, 4.1e-4 at 65536: measured), over random ones a tenth of it.  Long
+// sums are therefore made in parts of so many k-blocks, which the epilogue adds up in fp32: fp32 results 1024 terms at a time
+// (in the output, always the same thread's part of it), 16-bit ones when the loss would pass an eighth of half their step: 8192
+// terms for fp16, 65536 for bf16.  Their running sum stays in the accumulator set that the parts do not use, which costs such
+// an item the overlap of its parts (weight gradient of one group of 40000 rows, 2048 x 1408, fp16: 236 -> 243 us).  No wait is for more than a part, however many rows a group has.
+constexpr int sum_blocks(int out_dtype) { return out_dtype == EW_FP32 ? 16 : out_dtype == EW_FP16 ? 128 : 1024; }
 
 struct Args {
     const int32_t *offsets;
@@ -66,6 +69,7 @@ struct Args {
     int t_size;             // product, dx: length of the summed axis
     int f_tiles, c_tiles;
     int out_kind;           // ew_dtype_t
+    int sum_blocks;         // most k-blocks that are summed up in the tensor core
     int a_pairs, b_pairs;   // operands with a contiguous f (c): 1 = two 64-wide boxes come in one copy
     int fp16;               // operand type
     int stages;
@@ -188,7 +192,8 @@ __device__ __forceinline__ void store_zero(void *out, size_t at, int kind) {
     else reinterpret_cast<uint16_t *>(out)[at] = 0;
 }
 
-template <int CG, int NT, int EW, int WAY>
+// LONG: 16-bit results whose sums may have several parts (without that code the others' weight gradients are 1 to 3 % faster)
+template <int CG, int NT, int EW, int WAY, bool LONG>
 __global__ void __launch_bounds__(threads_of(EW), 1)
 grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ Args a) {
     using C = Cfg<CG, NT>;
@@ -311,10 +316,13 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             it.kb = t_blocks;
             it.tail = kBlockK;
         }
-        const int chunks = a.out_kind == EW_FP32 ? (it.kb + kSumBlocks - 1) / kSumBlocks : 1;
+        const int chunks = (it.kb + a.sum_blocks - 1) / a.sum_blocks;
         it.chunk = chunks > 1 ? (it.kb + chunks - 1) / chunks : it.kb;
         return it;
     };
+    // Whether an item's parts are added up in tensor memory: they all use one accumulator set, the running sum is in the other,
+    // and the next item begins with the set of the parts, so that its first wait frees both.
+    auto sums_here = [&](const Item &it) { return LONG && it.chunk < it.kb; };
     // A role's walk through this unit's items.  Finding an item takes a few hundred cycles of divisions and look-ups, which for a
     // weight gradient of few rows was most of the copying thread's time: the warp finds 32 items at once, a lane each.
     Item found = {};
@@ -386,7 +394,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (the leader CTA's)
         if (rank == 0) {
-            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phases = 0;          // (a bit a set)
             const uint32_t type = a.fp16 ? 0u : (1u << 7) | (1u << 10);
             const uint32_t base = (1u << 4) | type | (WAY != kProduct ? 1u << 15 : 0u) | (DW ? 1u << 16 : 0u) |
                                   ((uint32_t)(C::kTile >> 4) << 24);
@@ -398,7 +406,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 const int n = DW ? NT : (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
                 for (int kb = 0; lane == 0 && kb < it.kb && ok;) {
-                    if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, acc_phase ^ 1, abort_flag, a.err))) break;
+                    if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, (acc_phases >> acc & 1) ^ 1, abort_flag, a.err))) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + acc * NT;
                     for (const int first = kb, end = min(it.kb, kb + it.chunk); kb < end; ++kb) {
@@ -419,7 +427,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     }
                     if (!ok) break;
                     commit<CG>(bar_tfull + 8 * acc);
-                    if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+                    acc_phases ^= 1u << acc;
+                    if (!sums_here(it)) acc ^= 1;
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
             }
@@ -452,7 +461,7 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     } else {
         // ------------------------------------------------------------------ epilogue (EW warps of each CTA)
         const int lg = warp & 3, half = (warp - 2) >> 2;                     // the TMEM lanes this warp may read; its columns
-        uint32_t acc = 0, acc_phase = 0;
+        uint32_t acc = 0, acc_phases = 0;
         bool ok = true;
         for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
             const Item it = next_item(i, turn);
@@ -465,11 +474,31 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 continue;
             }
             for (int kb = 0; kb < it.kb; kb += it.chunk) {
-                if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phase, abort_flag, a.err))) break;
+                if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phases >> acc & 1, abort_flag, a.err))) break;
                 tc_fence_after();
-                const uint32_t t0 = tmem_base + ((uint32_t)(lg * 32) << 16) + acc * NT;
+                const uint32_t lanes = tmem_base + ((uint32_t)(lg * 32) << 16), t0 = lanes + acc * NT;
+                const bool here = sums_here(it);
+                int to_store = it.cols;
+                if (here) {
+                    // the running sum and this part, to where the sum stays, the last time to where the results are stored from
+                    const bool last = kb + it.chunk >= it.kb;
+                    const uint32_t t_sum = lanes + (acc ^ 1) * NT;
 #pragma unroll 1
-                for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * EW) {
+                    for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * EW) {
+                        uint32_t v[32], sum[32];
+                        tc_ld32(t0 + c0, v);
+                        tc_ld32(t_sum + c0, sum);
+                        tc_wait_ld();
+                        if (kb > 0)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(v[j]));
+                        tc_st32((last ? t0 : t_sum) + c0, v);
+                    }
+                    tc_wait_st();
+                    if (!last) to_store = 0;
+                }
+#pragma unroll 1
+                for (int c0 = 32 * half; c0 < to_store; c0 += 8 * EW) {
                     uint32_t v[32];
                     tc_ld32(t0 + c0, v);               // columns behind the item's last are in the accumulator set, not stored
                     tc_wait_ld();
@@ -489,7 +518,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_leader<CG>(bar_tempty + 8 * acc);
-                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+                acc_phases ^= 1u << acc;
+                if (!here) acc ^= 1;
             }
         }
     }
@@ -513,8 +543,9 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
 
 constexpr int kBarBytes = (3 * kMaxStages + 6) * 8;
 
+// terms: of the longest sum there can be
 template <int CG, int NT, int EW, int WAY>
-ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, long long max_items,
+ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, long long max_items, int terms,
                    cudaStream_t st) {
     using C = Cfg<CG, NT>;
     if (max_items > 0x7fff0000) return refuse("grouped product: too many output tiles");
@@ -542,12 +573,16 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     }
     cfg.attrs = attr;
     cfg.numAttrs = attrs;
-    return launched((int)cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, EW, WAY>, ma, mb, a), "grouped product");
+    a.sum_blocks = sum_blocks(a.out_kind);
+    const bool long_sums = a.out_kind != EW_FP32 && terms > a.sum_blocks * kBlockK;
+    return launched((int)(long_sums ? cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, EW, WAY, true>, ma, mb, a)
+                                    : cudaLaunchKernelEx(&cfg, grouped_product_kernel<CG, NT, EW, WAY, false>, ma, mb, a)), "grouped product");
 }
 
 template <int CG, int NT, int EW, int WAY>
 int setup_one() {
-    return (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, EW, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    return (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, EW, WAY, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(grouped_product_kernel<CG, NT, EW, WAY, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
 }
 
 // A row-major matrix's row stride: multiples of eight elements keep every TMA copy on a 16-byte boundary.
@@ -618,7 +653,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     do {                                                                                                                      \
         a.f_tiles = (f + 128 * CG - 1) / (128 * CG);                                                                          \
         const long long items = (live + rows / NT) * a.f_tiles;                                                               \
-        return grad ? launch<CG, NT, 4, kInputGrad>(*d, ma, mb, a, items, st) : launch<CG, NT, 4, kProduct>(*d, ma, mb, a, items, st); \
+        return grad ? launch<CG, NT, 4, kInputGrad>(*d, ma, mb, a, items, t, st) : launch<CG, NT, 4, kProduct>(*d, ma, mb, a, items, t, st); \
     } while (0)
     // (64 groups of 2816 x 2048, one CTA with 128 columns against the pair: 96 rows a group 127.7 and 130.0 us, 128 rows 134.1 and
     // 134.7, 160 rows 214 and 141)
@@ -707,8 +742,8 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
     a.out_kind = out_dtype;
     a.fp16 = dtype == EW_FP16;
     const long long items = (long long)groups * a.c_tiles * a.f_tiles;
-    if (accumulate) return launch<2, 256, 8, kWeightAdd>(*d, ma, mb, a, items, st);
+    if (accumulate) return launch<2, 256, 8, kWeightAdd>(*d, ma, mb, a, items, rows, st);
     // Few rows a group: the results' way out is what counts, and eight warps walk it (192 rows: 80 us against 95); many: the
     // arithmetic does, at the power limit, where four cost less (768 rows: 259 against 270).
-    return rows <= 256ll * groups ? launch<2, 256, 8, kWeightGrad>(*d, ma, mb, a, items, st) : launch<2, 256, 4, kWeightGrad>(*d, ma, mb, a, items, st);
+    return rows <= 256ll * groups ? launch<2, 256, 8, kWeightGrad>(*d, ma, mb, a, items, rows, st) : launch<2, 256, 4, kWeightGrad>(*d, ma, mb, a, items, rows, st);
 }

@@ -1,4 +1,4 @@
-"""Limits of the stand-alone operators on the device: empty batches."""
+"""Limits of the stand-alone operators on the device: empty batches, long sums."""
 import pytest
 import torch
 
@@ -28,4 +28,90 @@ def test_no_tokens(top_k, n_slots):
     assert binding.swiglu(y).shape == (0, 8) and binding.swiglu(y, p).shape == (0, 8)
     dh, dp = binding.swiglu_grad(torch.empty((0, 8), dtype=BF16, device="cuda"), y, p)
     assert dh.shape == (0, 16) and dp.shape == (0,)
+    assert binding.last_operator_error() == 0
+
+
+# ---------------------------------------------------------------------------------------------- long sums
+# The tensor core adds 16 products to the running sum at a time and cuts off at most two units of 2^-23 of it.  A running sum of
+# terms of one sign averages half its end, so a part of `part` terms loses at most part / 16 units of its end, all parts
+# together as much of the whole; the parts are added up in fp32, half a unit each.
+PART = {FP16: 8192, BF16: 65536, FP32: 1024}
+UNIT = 2.0 ** -23
+
+
+def one_sign(shape, dtype, seed, top):
+    """Values in (top / 2, top)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return ((torch.rand(shape, device="cuda", generator=g) * 0.5 + 0.5) * top).to(dtype)
+
+
+def near_long(got, ref, mag, terms):
+    part = min(terms, PART[got.dtype])
+    tol = torch.finfo(got.dtype).eps / 2 * ref.abs() + (part / 16 + terms / part) * UNIT * mag + (2.0 ** -25 if got.dtype == FP16 else 0)
+    off = (got.double() - ref).abs()
+    assert (off <= tol).all(), float((off / tol).max())
+
+
+@pytest.mark.parametrize("dtype,out_dtype,terms", [(FP16, FP16, 70001), (BF16, BF16, 300001), (FP16, FP32, 20003)], ids=str)
+def test_long_sums_of_one_sign_keep_their_mean(dtype, out_dtype, terms):
+    """A sum that is cut off term by term drifts towards zero; one made in parts does not, whatever its length."""
+    dy, x = one_sign((terms, 64), dtype, 1, 16384 / terms), one_sign((terms, 72), dtype, 2, 1.0)
+    ref = dy.double().t() @ x.double()
+    ends = torch.tensor([0, terms], dtype=torch.int32, device="cuda")
+    wide = terms + (-terms) % 8
+    flat = [torch.nn.functional.pad(t.t(), (0, wide - terms)).contiguous()[:, :terms] for t in (dy, x)]
+    results = [binding.grouped_mm_dw(dy, x, ends, out_dtype=out_dtype)[0]]
+    # the same sums as a product and as an input gradient; 1 row block a group on one CTA, five on CTA pairs
+    for copies in (1, 5):
+        rows = flat[0].repeat(copies, 1) if copies > 1 else flat[0]
+        rows = torch.nn.functional.pad(rows, (0, wide - terms)).contiguous()[:, :terms]
+        o = torch.tensor([0, rows.shape[0]], dtype=torch.int32, device="cuda")
+        y = binding.grouped_mm(rows, flat[1][None], o, out_dtype=out_dtype)
+        dx = binding.grouped_mm_dx(rows, x[None], o, out_dtype=out_dtype)
+        results += list(y.split(64)) + list(dx.split(64))
+    half = torch.finfo(out_dtype).eps / 2
+    for got in results:
+        near_long(got, ref, ref, terms)
+        # roundings of either sign: uniform within half a step, their mean over the elements within four deviations of zero
+        drift = float(((got.double() - ref) / ref).mean())
+        assert abs(drift) <= PART[out_dtype] / 16 * UNIT + 4 * half / (3 * ref.numel()) ** 0.5 + terms / PART[out_dtype] * UNIT, drift
+
+
+@pytest.mark.parametrize("out_dtype", [FP16, FP32], ids=str)
+@pytest.mark.parametrize("empty", [0, 400])
+def test_long_and_short_groups_in_turn(empty, out_dtype):
+    """Groups of many parts, of one and of none take turns in a CTA pair's accumulators; results repeat to the bit."""
+    counts = [9000, 10, 17000, 0, 300, 8193, 8192, 64, 24577, 0, 16384, 1] + [0] * empty
+    ends = torch.tensor([0] + counts, device="cuda").cumsum(0).int()
+    g = torch.Generator(device="cuda").manual_seed(7)
+    dy, x = ((torch.randn((sum(counts), w), device="cuda", generator=g) * 0.1).to(FP16) for w in (1000, 1096))
+    dw = binding.grouped_mm_dw(dy, x, ends, out_dtype=out_dtype)
+    more = binding.grouped_mm_dw(dy, x, ends, out=torch.ones_like(dw), accumulate=True)
+    at = 0
+    for i, c in enumerate(counts):
+        a, b = dy[at:at + c].double(), x[at:at + c].double()
+        at += c
+        ref, mag = a.t() @ b, a.abs().t() @ b.abs()
+        near_long(dw[i], ref, mag, max(c, 16))
+        near_long(more[i], ref + 1, mag + 1, max(c, 16))
+    for _ in range(5):
+        assert torch.equal(dw, binding.grouped_mm_dw(dy, x, ends, out_dtype=out_dtype))
+    assert binding.last_operator_error() == 0
+
+
+@pytest.mark.parametrize("rows", [40, 700])
+def test_long_contractions_over_many_tiles(rows):
+    """y and dx of 16-bit results with a summed axis of several parts, more tiles than CTAs; short sums before and after."""
+    k, n, groups = 8192 * 2 + 72, 1096, 6
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    offsets = torch.tensor([0, 5, 5, rows // 2, rows - 9, rows - 8, rows], dtype=torch.int32, device="cuda")
+    x, w = torch.randn((rows, k), device="cuda", generator=g).to(FP16), (torch.randn((groups, n, k), device="cuda", generator=g) * 0.05).to(FP16)
+    y = binding.grouped_mm(x, w, offsets)
+    wt = w.transpose(1, 2).contiguous()
+    dx = binding.grouped_mm_dx(x, wt, offsets)
+    for s, (i, j) in enumerate(zip(offsets.tolist()[:-1], offsets.tolist()[1:])):
+        ref, mag = x[i:j].double() @ w[s].double().t(), x[i:j].double().abs() @ w[s].double().abs().t()
+        near_long(y[i:j], ref, mag, k)
+        near_long(dx[i:j], ref, mag, k)
+    assert torch.equal(y, binding.grouped_mm(x, w, offsets)) and torch.equal(dx, binding.grouped_mm_dx(x, wt, offsets))
     assert binding.last_operator_error() == 0
