@@ -394,7 +394,8 @@ ew_status_t ew_swiglu_grad(int32_t device, int32_t dtype, const void *dact, int6
                            float *drow_weights, void *cuda_stream);
 
 /* Read and clear the operators' error word of a device (waits for all work on it).  *code receives EW_OK,
- * EW_ERR_INVALID_ARG (an index in device memory was outside its range) or EW_ERR_TIMEOUT (a bounded wait expired). */
+ * EW_ERR_INVALID_ARG (an index in device memory was outside its range) or EW_ERR_TIMEOUT (a bounded wait expired).  Where both
+ * happened the first call reports the timeout, the next one the index; what happens during the call is left for the next one. */
 ew_status_t ew_last_operator_error(int32_t device, int32_t *code);
 
 /* Device address of slot `slot` of a layer's fused gate|up tensor (which = 0) or down tensor

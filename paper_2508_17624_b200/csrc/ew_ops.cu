@@ -9,7 +9,14 @@ namespace ops {
 namespace {
 
 constexpr int kMaxDevices = 64;
-__device__ int g_operator_error;
+__device__ int g_operator_error[2];                  // the error word; what the last reader took from it
+
+// Takes what one status can report out of the error word: an expired wait, or else the index.  What is not reported stays, and
+// so does a bit that a kernel sets meanwhile.
+__global__ void take_error_kernel(int *err) {
+    const int seen = *(volatile int *)err, report = (seen & 2) ? 2 : seen;
+    err[1] = atomicAnd(err, ~report) & report;
+}
 
 std::mutex g_mutex;
 Device g_devices[kMaxDevices];
@@ -25,10 +32,21 @@ ew_status_t resolve(Device *d, int device) {
     if (e != cudaSuccess) return launched((int)e, "operator set-up");
     d->encode = reinterpret_cast<EncodeTiled>(fn);
     d->err = static_cast<int *>(err);
-    return launched(grouped_setup() | quant_setup() | swiglu_setup(), "operator set-up");
+    cudaFuncAttributes fa;
+    return launched((int)cudaFuncGetAttributes(&fa, take_error_kernel) | grouped_setup() | quant_setup() | swiglu_setup(), "operator set-up");
 }
 
 }  // namespace
+
+ew_status_t take_error(const Device &d, int *bits) {
+    std::lock_guard<std::mutex> lock(g_mutex);       // (readers take turns at the second word)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = cfg.blockDim = dim3(1);
+    ew_status_t s = launched((int)cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+    if (s == EW_OK) s = launched((int)cudaLaunchKernelEx(&cfg, take_error_kernel, d.err), "operator error");
+    if (s == EW_OK) s = launched((int)cudaMemcpy(bits, d.err + 1, 4, cudaMemcpyDeviceToHost), "cudaMemcpy");
+    return s;
+}
 
 ew_status_t device_state(int device, const Device **out) {
     if (device >= kMaxDevices) return refuse("device ordinal out of range");
@@ -56,10 +74,8 @@ extern "C" ew_status_t ew_last_operator_error(int32_t device, int32_t *code) {
     ew_status_t s = ops::launched((int)guard.enter(device), "cudaSetDevice");
     const ops::Device *d = nullptr;
     if (s == EW_OK) s = ops::device_state(device, &d);
-    if (s == EW_OK) s = ops::launched((int)cudaDeviceSynchronize(), "cudaDeviceSynchronize");
-    int32_t v = 0;
-    if (s == EW_OK) s = ops::launched((int)cudaMemcpy(&v, d->err, 4, cudaMemcpyDeviceToHost), "cudaMemcpy");
-    if (s == EW_OK && v) s = ops::launched((int)cudaMemset(d->err, 0, 4), "cudaMemset");
+    int v = 0;
+    if (s == EW_OK) s = ops::take_error(*d, &v);
     if (s == EW_OK) *code = (v & 2) ? EW_ERR_TIMEOUT : (v & ops::kErrBadIndex) ? EW_ERR_INVALID_ARG : EW_OK;
     return s;
 }

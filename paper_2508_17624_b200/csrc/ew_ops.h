@@ -30,6 +30,9 @@ struct Device {
 // The device's constants, resolved on first use (thread-safe).  The caller has made the device current.
 ew_status_t device_state(int device, const Device **out);
 
+// Waits for the device and takes one status' bits out of its error word.
+ew_status_t take_error(const Device &d, int *bits);
+
 // Per-file attributes of the operators' kernels, set once per device by device_state().
 int grouped_setup();
 int quant_setup();

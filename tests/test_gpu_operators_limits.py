@@ -1,4 +1,6 @@
-"""Limits of the stand-alone operators on the device: empty batches, long sums."""
+"""Limits of the stand-alone operators on the device: empty batches, long sums, the error word."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -115,3 +117,20 @@ def test_long_contractions_over_many_tiles(rows):
         near_long(dx[i:j], ref, mag, k)
     assert torch.equal(y, binding.grouped_mm(x, w, offsets)) and torch.equal(dx, binding.grouped_mm_dx(x, wt, offsets))
     assert binding.last_operator_error() == 0
+
+
+# ---------------------------------------------------------------------------------------------- the error word
+class _Device(C.Structure):                             # what the library keeps of a device
+    _fields_ = [("sm_count", C.c_int), ("err", C.c_void_p), ("encode", C.c_void_p)]
+
+
+def test_what_was_not_reported_stays_in_the_error_word():
+    """A timeout and a bad index: the first call reports the one, the second the other.  (No operator's wait runs out, so the
+    word is written by the test.)"""
+    assert binding.last_operator_error() == 0
+    device = C.POINTER(_Device)()
+    assert binding.lib()._ZN2ew3ops12device_stateEiPPKNS0_6DeviceE(0, C.byref(device)) == 0
+    for bits, codes in ((2 | 4, [7, 1, 0]), (2, [7, 0]), (4, [1, 0])):
+        word = C.c_int(bits)
+        assert C.CDLL("libcuda.so.1").cuMemcpyHtoD_v2(C.c_uint64(device.contents.err), C.byref(word), C.c_size_t(4)) == 0
+        assert [binding.last_operator_error() for _ in codes] == codes
