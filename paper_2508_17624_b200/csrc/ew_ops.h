@@ -70,6 +70,7 @@ inline ew_status_t encode_map(const Device &d, CUtensorMap *out, CUtensorMapData
 
 inline ew_status_t launched(int rc, const char *what) {
     if (rc == 0) return EW_OK;
+    (void)cudaGetLastError();                            // reported here: not once more by the thread's next call that asks
     set_last_error(std::string(what) + ": " + cudaGetErrorString((cudaError_t)rc));
     return EW_ERR_CUDA;
 }

@@ -1,10 +1,11 @@
-"""Limits of the stand-alone operators on the device: empty batches, long sums, the error word."""
+"""Limits of the stand-alone operators on the device: empty batches, long sums, the error word, failed calls."""
 import ctypes as C
 
 import pytest
 import torch
 
 from paper_2508_17624_b200 import binding, build
+from paper_2508_17624_b200 import workloads as wl
 
 pytestmark = pytest.mark.gpu
 BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
@@ -134,3 +135,20 @@ def test_what_was_not_reported_stays_in_the_error_word():
         word = C.c_int(bits)
         assert C.CDLL("libcuda.so.1").cuMemcpyHtoD_v2(C.c_uint64(device.contents.err), C.byref(word), C.c_size_t(4)) == 0
         assert [binding.last_operator_error() for _ in codes] == codes
+
+
+def test_a_failed_call_does_not_fail_the_next_one():
+    """An operator on a device that is not there fails; the pool's next call of the same thread does not see that error."""
+    cfg = wl.CONFIGS["c0"]
+    pool = binding.Pool.from_config(cfg)
+    binding.load_model(pool, cfg, adapters=[])
+    ids = torch.zeros((8, cfg.top_k), dtype=torch.int32, device="cuda")
+    aid = torch.full((8,), -1, dtype=torch.int32, device="cuda")
+    h, out = torch.zeros((4, 32), dtype=BF16, device="cuda"), torch.zeros((4, 16), dtype=BF16, device="cuda")
+    lib = binding.lib()
+    assert lib.ew_swiglu(63, 0, h.data_ptr(), 32, None, 4, 16, out.data_ptr(), 16, None) == 6          # EW_ERR_CUDA
+    assert lib.ew_last_error_string()
+    pool.reroute(0, ids, aid)
+    assert lib.ew_last_operator_error(63, C.byref(C.c_int32())) == 6
+    pool.reroute(0, ids, aid)
+    pool.destroy()
