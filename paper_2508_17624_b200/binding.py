@@ -302,7 +302,8 @@ class Pool:
 # ---------------------------------------------------------------------------------------------------------------------
 # Stand-alone operators (no pool): argument checks, output allocation, one library call on the current stream.  A small
 # call takes the GPU less time than the host, so the checks of a good call are a handful of comparisons; only when one of
-# them fails does `_on` find out which and say so.
+# them fails does `_on` find out which and say so.  autograd does not see the calls: an operand that it is recording is
+# refused, since a result without a gradient would go unnoticed (torch.autograd.Function runs its two halves unrecorded).
 class _Torch:
     """What the operators need of torch, resolved on first use (the package imports without it)."""
     ready = False
@@ -312,6 +313,7 @@ class _Torch:
         import torch
         cls.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         cls.int32, cls.float32, cls.uint8 = torch.int32, torch.float32, torch.uint8
+        cls.recording = torch.is_grad_enabled
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         cls.ready = True
         return cls
@@ -332,6 +334,11 @@ def _on(t, like=None, ndim=2, name="operand", dtype=None):
     if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the innermost dimension is not contiguous")
     return t
+
+
+def _recorded(where):
+    raise ValueError(f"{where}: autograd is recording an operand and would lose its gradient here; call it under torch.no_grad() or inside "
+                     "a torch.autograd.Function, and the gradient's operators in its backward")
 
 
 def _code(T, dtype) -> int:
@@ -386,6 +393,8 @@ def _result(out, shape, dtype, like, name="out"):
 
 def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
     T, dev, dtype = _torch(), a.get_device(), a.dtype
+    if (a.requires_grad or w.requires_grad) and T.recording():
+        _recorded(where)
     code = _code(T, dtype)
     rows, width, lda = _matrix(a, dev, dtype, "the rows' operand", None)
     groups, n, k, ldw, stride = _matrices(w, dev, dtype, "w", a)
@@ -424,6 +433,8 @@ def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
     """The gradient of `grouped_mm` with respect to w: dw[g] = dy_g^T x_g -> [groups, n, k]; a group without rows gets zeros.
     accumulate: adds to `out` instead (required then), as over the steps of a large batch."""
     T, dev, dtype = _torch(), dy.get_device(), dy.dtype
+    if (dy.requires_grad or x.requires_grad) and T.recording():
+        _recorded("ew_grouped_mm_dw")
     code = _code(T, dtype)
     rows, n, lddy = _matrix(dy, dev, dtype, "dy", None)
     x_rows, k, ldx = _matrix(x, dev, dtype, "x", dy)
@@ -449,7 +460,7 @@ def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
 
 def quant_pack(w, group, out=None):
     """4-bit weights and group scales of w [slots, n, k] (bf16 or fp16) for `quant_mv`: (q uint8 [slots, n, k/2], scales
-    [slots, k/group, n] of w's type).  The header has the format."""
+    [slots, k/group, n] of w's type).  The header has the format.  Not differentiable: w may be a parameter, the result is data."""
     T, dev, dtype = _torch(), w.get_device(), w.dtype
     code = _code(T, dtype)
     slots, n, k, ld, stride = _matrices(w, dev, dtype, "w", None)
@@ -469,6 +480,8 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     pair in any shape ([tokens, top_k] as the router writes it), per_row = pairs / rows of x; negative: a row of zeros.
     slots None: one matrix, a pair a row.  -> [pairs, n]; out_dtype: x's type or float32."""
     T, dev, dtype = _torch(), x.get_device(), x.dtype
+    if (x.requires_grad or scales.requires_grad) and T.recording():
+        _recorded("ew_quant_mv")
     code = _code(T, dtype)
     rows, k, ldx = _matrix(x, dev, dtype, "x", None)
     if not _good(q, dev, T.uint8, 3):
@@ -514,6 +527,8 @@ def swiglu(h, row_weights=None, out=None):
     """row_weights[r] * silu(h[r, :inter]) * h[r, inter:] -> [rows, inter]: the activation between an expert's linears, the
     routing weights (float32, or None) folded in."""
     T, dev, dtype = _torch(), h.get_device(), h.dtype
+    if (h.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
+        _recorded("ew_swiglu")
     code = _code(T, dtype)
     rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     if two < 2 or two % 2:
@@ -534,6 +549,8 @@ def swiglu(h, row_weights=None, out=None):
 def swiglu_grad(dact, h, row_weights=None, out=None):
     """The gradient of `swiglu`: dh [rows, 2 inter], and with row_weights also theirs, float32 [rows] -> dh or (dh, dp)."""
     T, dev, dtype = _torch(), h.get_device(), h.dtype
+    if (h.requires_grad or dact.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
+        _recorded("ew_swiglu_grad")
     code = _code(T, dtype)
     rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     d_rows, inter, ldd = _matrix(dact, dev, dtype, "dact", h)

@@ -1,4 +1,4 @@
-"""Limits of the stand-alone operators on the device: empty batches, long sums, the error word, failed calls."""
+"""Limits of the stand-alone operators on the device: empty batches, long sums, the error word, failed calls, autograd."""
 import ctypes as C
 
 import pytest
@@ -152,3 +152,48 @@ def test_a_failed_call_does_not_fail_the_next_one():
     assert lib.ew_last_operator_error(63, C.byref(C.c_int32())) == 6
     pool.reroute(0, ids, aid)
     pool.destroy()
+
+
+# ---------------------------------------------------------------------------------------------- autograd
+class Experts(torch.autograd.Function):
+    """An expert FFN over sorted rows, the operators in both of its halves."""
+
+    @staticmethod
+    def forward(ctx, x, w13, w2, p, offsets):
+        h = binding.grouped_mm(x, w13, offsets)
+        act = binding.swiglu(h, p)
+        ctx.save_for_backward(x, w13, w2, p, offsets, h, act)
+        return binding.grouped_mm(act, w2, offsets)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w13, w2, p, offsets, h, act = ctx.saved_tensors
+        dh, dp = binding.swiglu_grad(binding.grouped_mm_dx(dy, w2, offsets), h, p)
+        return binding.grouped_mm_dx(dh, w13, offsets), binding.grouped_mm_dw(dh, x, offsets), binding.grouped_mm_dw(dy, act, offsets), dp, None
+
+
+def test_operators_inside_an_autograd_function():
+    """Parameters that need gradients reach the operators through a Function; by themselves they are refused, except for packing."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    offsets = torch.tensor([0, 7, 7, 30], dtype=torch.int32, device="cuda")
+    x, w13, w2 = (torch.randn(s, device="cuda", generator=g).mul_(f).to(FP16).requires_grad_() for s, f in (((30, 64), 1.0), ((3, 96, 64), 0.1), ((3, 64, 48), 0.1)))
+    p = torch.rand(30, device="cuda", generator=g).requires_grad_()
+    with pytest.raises(ValueError, match="autograd"):
+        binding.grouped_mm(x, w13, offsets)
+    y = Experts.apply(x, w13, w2, p, offsets)
+    dy = torch.randn(y.shape, device="cuda", generator=g).to(FP16)
+    y.backward(dy)
+    x64, a64, b64, p64 = (t.detach().double().requires_grad_() for t in (x, w13, w2, p))
+    parts = []
+    for s, (i, j) in enumerate(((0, 7), (7, 7), (7, 30))):
+        gate, up = (x64[i:j] @ a64[s].t()).chunk(2, 1)
+        parts.append((p64[i:j, None] * gate * torch.sigmoid(gate) * up) @ b64[s].t())
+    ref = torch.cat(parts)
+    ref.backward(dy.double())
+    # the fp16 roundings on the way (h, act, d_act, dh, the result) are half a step each, h's through silu's slope on both halves
+    for got, want in ((y, ref), (x.grad, x64.grad), (w13.grad, a64.grad), (w2.grad, b64.grad), (p.grad, p64.grad)):
+        assert float((got.detach().double() - want.detach()).norm() / want.detach().norm()) <= 6 * 2.0 ** -11
+    q, scales = binding.quant_pack(w13, 32)
+    assert not scales.requires_grad
+    with torch.no_grad():
+        assert not binding.quant_mv(x, q[:1], scales[:1]).requires_grad

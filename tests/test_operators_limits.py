@@ -1,5 +1,6 @@
 """Limits of the stand-alone operators' arguments, on the host: nothing is launched, no GPU is needed."""
 import pytest
+import torch
 
 from paper_2508_17624_b200 import binding, build
 
@@ -22,3 +23,20 @@ def test_an_empty_batch_needs_no_slot_ids(lib):
     """A tensor without entries has no address: [0, top_k] slot ids are not the call without slot ids."""
     assert mv(lib, pairs=0, slots=None, x=None, y=None, n_slots=64) == NO_DEVICE
     assert mv(lib, pairs=6, slots=None, n_slots=64) == INVALID
+
+
+def test_operands_that_autograd_records_are_refused():
+    """A result without a gradient would go unnoticed."""
+    x, w = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros((2, 64, 64), dtype=torch.bfloat16)
+    offsets, p, q, scales = torch.zeros(3, dtype=torch.int32), torch.ones(4), torch.zeros((2, 64, 32), dtype=torch.uint8), torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    recorded = [t.clone().requires_grad_() for t in (x, w, p, scales)]
+    xr, wr, pr, sr = recorded
+    calls = [lambda: binding.grouped_mm(xr, w, offsets), lambda: binding.grouped_mm(x, wr, offsets), lambda: binding.grouped_mm_dx(xr, w, offsets),
+             lambda: binding.grouped_mm_dx(x, wr, offsets), lambda: binding.grouped_mm_dw(xr, x, offsets), lambda: binding.grouped_mm_dw(x, xr, offsets),
+             lambda: binding.quant_mv(xr, q, scales), lambda: binding.quant_mv(x, q, sr), lambda: binding.swiglu(xr), lambda: binding.swiglu(x, pr),
+             lambda: binding.swiglu_grad(xr, x), lambda: binding.swiglu_grad(x[:, :32], xr), lambda: binding.swiglu_grad(x[:, :32], x, pr)]
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA tensor"):      # the next check
+            call()
