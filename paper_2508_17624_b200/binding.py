@@ -348,6 +348,13 @@ def _code(T, dtype) -> int:
     return code
 
 
+_MOST = 2 ** 31 - 1                                     # of a size: the library takes 32-bit ones, and ctypes would cut a larger one down
+
+
+def _too_large(what, *sizes):
+    raise ValueError(f"{what}: sizes of {', '.join(map(str, sizes))}; the library takes up to {_MOST}")
+
+
 def _good(t, dev, dtype, ndim) -> bool:
     """Whether `t` is what `_on` wants (contiguity of the last dimension apart)."""
     return t.get_device() == dev and t.dtype is dtype and t.dim() == ndim
@@ -360,6 +367,8 @@ def _matrix(t, dev, dtype, name, like):
     (rows, width), (ld, one) = t.shape, t.stride()
     if one != 1 and width > 1 and rows:
         _on(t, like, 2, name, dtype)
+    if rows > _MOST or width > _MOST:
+        _too_large(name, rows, width)
     return rows, width, ld if rows > 1 else (width + 7) // 8 * 8
 
 
@@ -370,6 +379,8 @@ def _matrices(t, dev, dtype, name, like):
     (g, n, k), (stride, ld, one) = t.shape, t.stride()
     if one != 1 and k > 1:
         _on(t, like, 3, name, dtype)
+    if g > _MOST or n > _MOST or k > _MOST:
+        _too_large(name, g, n, k)
     ld = ld if n > 1 else (k + 7) // 8 * 8
     return g, n, k, ld, stride if g > 1 else n * ld
 
@@ -379,6 +390,8 @@ def _offsets(offsets, dev, T, like):
     if offsets.get_device() != dev or offsets.dtype is not T.int32 or offsets.dim() != 1 or n < 2 or not offsets.is_contiguous():
         _on(offsets, like, 1, "offsets")
         raise ValueError("offsets: a contiguous int32 tensor with one more entry than groups is wanted")
+    if n - 1 > _MOST:
+        _too_large("offsets", n)
     return n - 1
 
 
@@ -499,6 +512,8 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
         if pairs and (rows == 0 or pairs % rows):
             raise ValueError(f"{pairs} pairs for {rows} rows of x")
         per_row = pairs // rows if pairs else 1
+    if pairs > _MOST or n_slots > _MOST or n > _MOST:
+        _too_large("slots and q", pairs, n_slots, n)
     if out_dtype is None:
         out_dtype = dtype if out is None else out.dtype
     if out is None:

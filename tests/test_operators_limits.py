@@ -40,3 +40,55 @@ def test_operands_that_autograd_records_are_refused():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="CUDA tensor"):      # the next check
             call()
+
+
+class Huge:
+    """What the binding asks of a device tensor, for one of any size; its address is what the library would be called with."""
+    requires_grad = False
+
+    def __init__(self, *shape, dtype=torch.bfloat16):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def get_device(self):
+        return 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self, d=None):
+        strides = [self.shape[i + 1:].numel() for i in range(len(self.shape))]
+        return tuple(strides) if d is None else strides[d]
+
+    def new_empty(self, shape, dtype=None):
+        return Huge(*shape, dtype=dtype or self.dtype)
+
+    def data_ptr(self):
+        raise AssertionError("the call went on")
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """The library's sizes have 32 bits and ctypes cuts larger ones down to them: 2^32 + 5 rows would have been five."""
+    far, i32, f32, u8 = 2 ** 32 + 5, torch.int32, torch.float32, torch.uint8
+    offsets = Huge(3, dtype=i32)
+    calls = [lambda: binding.grouped_mm(Huge(far, 8), Huge(2, 8, 8), offsets), lambda: binding.grouped_mm(Huge(4, 8), Huge(2, far, 8), offsets),
+             lambda: binding.grouped_mm_dx(Huge(4, far), Huge(2, far, 8), offsets), lambda: binding.grouped_mm(Huge(4, far), Huge(2, 8, far), offsets),
+             lambda: binding.grouped_mm(Huge(4, 8), Huge(far, 8, 8), Huge(far + 1, dtype=i32)), lambda: binding.grouped_mm_dw(Huge(far, 8), Huge(far, 8), offsets),
+             lambda: binding.grouped_mm_dw(Huge(4, far), Huge(4, 8), offsets), lambda: binding.grouped_mm_dw(Huge(4, 8), Huge(4, 8), Huge(far + 1, dtype=i32)),
+             lambda: binding.quant_mv(Huge(1, 32), Huge(2, 8, 16, dtype=u8), Huge(2, 1, 8), Huge(far, dtype=i32)),
+             lambda: binding.quant_mv(Huge(1, 32), Huge(far, 8, 16, dtype=u8), Huge(far, 1, 8), Huge(1, dtype=i32)),
+             lambda: binding.quant_mv(Huge(1, 32), Huge(2, far, 16, dtype=u8), Huge(2, 1, far), Huge(1, dtype=i32)),
+             lambda: binding.quant_mv(Huge(far, 32), Huge(1, 8, 16, dtype=u8), Huge(1, 1, 8)),
+             lambda: binding.quant_pack(Huge(far, 8, 32), 32), lambda: binding.quant_pack(Huge(1, far, 32), 32),
+             lambda: binding.swiglu(Huge(far, 2)), lambda: binding.swiglu(Huge(4, 2 * far)), lambda: binding.swiglu(Huge(far, 2), Huge(far, dtype=f32)),
+             lambda: binding.swiglu_grad(Huge(far, 1), Huge(far, 2))]
+    for call in calls:
+        with pytest.raises(ValueError, match="the library takes up to"):
+            call()
+    with pytest.raises(AssertionError, match="went on"):
+        binding.swiglu(Huge(2 ** 31 - 1, 2))
