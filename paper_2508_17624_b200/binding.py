@@ -504,11 +504,11 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     (n_slots, n, half), (s_slots, groups, s_n) = q.shape, scales.shape
     if half * 2 != k or groups < 1 or k % groups or s_slots != n_slots or s_n != n or not q.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"x {tuple(x.shape)}, q {tuple(q.shape)} and scales {tuple(scales.shape)} do not belong together")
-    pairs, slots_at, per_row = rows, None, 1
+    pairs, per_row = rows, 1
     if slots is not None:
         if slots.get_device() != dev or slots.dtype is not T.int32 or not slots.is_contiguous():
             raise ValueError("slots: a contiguous int32 tensor on x's device is wanted")
-        pairs, slots_at = slots.numel(), slots.data_ptr()
+        pairs = slots.numel()
         if pairs and (rows == 0 or pairs % rows):
             raise ValueError(f"{pairs} pairs for {rows} rows of x")
         per_row = pairs // rows if pairs else 1
@@ -521,7 +521,7 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     else:
         out = _result(out, (pairs, n), out_dtype, x)
         ldo = out.stride(0) if pairs > 1 else n
-    rc = lib().ew_quant_mv(dev, code, _code(T, out_dtype), x.data_ptr(), ldx, q.data_ptr(), scales.data_ptr(), slots_at, pairs, per_row, n_slots, n, k,
+    rc = lib().ew_quant_mv(dev, code, _code(T, out_dtype), x.data_ptr(), ldx, q.data_ptr(), scales.data_ptr(), None if slots is None else slots.data_ptr(), pairs, per_row, n_slots, n, k,
                            k // groups, out.data_ptr(), ldo, T.stream(dev))
     if rc:
         _check(rc, "ew_quant_mv")
