@@ -369,7 +369,7 @@ ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, c
  *   x       [pairs / pairs_per_row, k];  x, q and scales 16-byte aligned, ldx a multiple of 8;  y [pairs, n]
  * A row of x with an infinity or NaN in it gives rows of infinities and NaN, other rows do not see it.
  * Every pair count is taken; beyond some 32 rows a slot the 16-bit weights' ew_grouped_mm is the better call.
- * n_slots <= 2048, k <= 16384.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
+ * n_slots <= 2048, k <= 16384, n <= 33554400, n_slots * n < 2^31.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
 ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *q,
                         const void *scales, const int32_t *slots, int32_t pairs, int32_t pairs_per_row, int32_t n_slots,
                         int32_t n, int32_t k, int32_t group, void *y, int64_t ldy, void *cuda_stream);

@@ -766,7 +766,7 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
                                    int64_t ldy, void *cuda_stream) {
     if (!is_16bit(dtype) || (out_dtype != dtype && out_dtype != EW_FP32)) return refuse("4-bit product: x is bf16 or fp16, results of the same type or fp32");
     if (bad_group(group, k) || k > kMaxK) return refuse("4-bit product: groups of 32, 64 or 128 weights that divide k, k at most 16384");
-    if (pairs < 0 || pairs_per_row < 1 || pairs % pairs_per_row || n_slots < 1 || n_slots > kMaxSlots || n < 8 || n % 8 || (int64_t)n_slots * n > 0x7fffffff || (int64_t)kMaxPairs * ((n + kRows - 1) / kRows) > 0x7fffffff)
+    if (pairs < 0 || pairs_per_row < 1 || pairs % pairs_per_row || n_slots < 1 || n_slots > kMaxSlots || n < 8 || n % 8 || (int64_t)n_slots * n > 0x7fffffff || kMaxPairs * (((int64_t)n + kRows - 1) / kRows) > 0x7fffffff)
         return refuse("4-bit product: size out of range (n in multiples of 8, at most 2048 slots)");
     // (a tensor without entries may have no address)
     if (pairs > 0 && !slots && n_slots != 1) return refuse("4-bit product: without slot ids there is one matrix");
@@ -796,11 +796,11 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
     a.n_slots = n_slots;
     a.out_fp32 = out_dtype == EW_FP32;
     a.tiles = (n + kRows - 1) / kRows;
-    for (int32_t p0 = 0; p0 < pairs; p0 += kMaxPairs) {
-        a.pair0 = p0;
-        a.pairs = pairs - p0 < kMaxPairs ? pairs - p0 : kMaxPairs;
+    for (int64_t p0 = 0; p0 < pairs; p0 += kMaxPairs) {                      // (the step behind the last launch may pass 2^31)
+        a.pair0 = (int)p0;
+        a.pairs = pairs - p0 < kMaxPairs ? (int)(pairs - p0) : kMaxPairs;
         a.x = (const uint8_t *)x + (size_t)(p0 / pairs_per_row) * ldx * 2;
-        a.lead = p0 % pairs_per_row;
+        a.lead = (int)(p0 % pairs_per_row);
         a.slots = slots ? slots + p0 : nullptr;
         // One column of eight pairs with x in bytes, or up to three with x as it is: what a slot has more is another job, which
         // reads its weights again.  The bytes' sums are scaled group by group, so they pay with long groups and few pairs.

@@ -197,3 +197,18 @@ def test_operators_inside_an_autograd_function():
     assert not scales.requires_grad
     with torch.no_grad():
         assert not binding.quant_mv(x, q[:1], scales[:1]).requires_grad
+
+
+def test_as_many_pairs_as_a_call_takes():
+    """2^31 - 1 pairs of one row of x, a million launches: the last ones, and some of the others."""
+    pairs = 2 ** 31 - 1
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, (q, scales) = torch.randn((1, 32), device="cuda", generator=g).to(BF16), binding.quant_pack(torch.randn((3, 8, 32), device="cuda", generator=g).to(BF16), 32)
+    slots = torch.zeros((pairs,), dtype=torch.int32, device="cuda")
+    slots[-9:] = torch.tensor([1, 2, 0, -1, 2, 1, 0, 0, 2], dtype=torch.int32)
+    slots[1000003::1000003] = 1
+    every = torch.cat([binding.quant_mv(x, q, scales, torch.full((1,), s, dtype=torch.int32, device="cuda")) for s in (0, 1, 2, -1)])
+    y = binding.quant_mv(x, q, scales, slots)
+    for at in (slice(0, 5000), slice(pairs - 5000, pairs), slice(1000003, None, 1000003), slice(7, None, 999983)):
+        assert torch.equal(y[at], every[slots[at].long()])
+    assert binding.last_operator_error() == 0

@@ -92,3 +92,10 @@ def test_sizes_beyond_32_bits_are_refused():
             call()
     with pytest.raises(AssertionError, match="went on"):
         binding.swiglu(Huge(2 ** 31 - 1, 2))
+
+
+def test_quant_mv_widths_near_two_to_the_31(lib):
+    """The widths that the header names, and nothing beyond them, wherever a sum of sizes may pass 31 bits."""
+    assert mv(lib, n_slots=1, n=33554400, ldy=33554400) == NO_DEVICE
+    for n_slots, n in ((1, 33554408), (1, 0x7ffffff8), (1, 0x7fffffe8), (64, 33554432), (2048, 1048576)):
+        assert mv(lib, n_slots=n_slots, n=n, ldy=n) == INVALID, (n_slots, n)
