@@ -336,7 +336,7 @@ typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2 } ew_dtype_t;
  * they need not start at 0 nor end at `rows`, and rows outside them are left as they were.  An offset below the one
  * before it or outside [0, rows] is clamped and reported as EW_ERR_INVALID_ARG.
  * dtype: EW_BF16 or EW_FP16; out_dtype: the same or EW_FP32.  x and w are 16-byte aligned with ldx, ldw and
- * group_stride multiples of 8 (n and k may be anything up to them); y needs its element's alignment only.
+ * group_stride multiples of 8 (n and k may be anything up to them; groups lie one behind the other or interleave their rows); y needs its element's alignment only.
  * groups <= 2048.  rows = 0 is a no-op.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
 ew_status_t ew_grouped_mm(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *w,
                           int64_t ldw, int64_t group_stride, const int32_t *offsets, int32_t rows, int32_t groups,
@@ -350,7 +350,8 @@ ew_status_t ew_grouped_mm_dx(int32_t device, int32_t dtype, int32_t out_dtype, c
 /* Its gradient with respect to w:  dw[g] = dy_g^T x_g over the rows of group g, or dw[g] += with accumulate != 0
  * (added in fp32 and rounded to out_dtype).  dw [groups, n, k]; the gradient of a group without rows is zero (with
  * accumulate: stays as it is).  To take the gradient of some groups only, pass their part of offsets and dw.
- * lddw and group_stride may be any strides that keep rows apart; all else as above. */
+ * lddw and group_stride may be any strides that lay the groups one behind the other or interleave their rows (dw as the
+ * middle dimension of an [n, groups, k] tensor); all else as above. */
 ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, const void *dy, int64_t lddy,
                              const void *x, int64_t ldx, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n,
                              int32_t k, int32_t accumulate, void *dw, int64_t lddw, int64_t group_stride,

@@ -608,7 +608,7 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
     // (a tensor without rows may have no address)
     ew_status_t s = check_common(dtype, out_dtype, offsets, rows, groups, n, k, rows == 0 ? w : out);
     if (s != EW_OK) return s;
-    if ((rows > 0 && bad_matrix(x, ldx, t)) || bad_matrix(w, ldw, k) || ldo < f || (groups > 1 && (group_stride < (int64_t)(n - 1) * ldw + k || (group_stride & 7) || group_stride >= (1ll << 38))))
+    if ((rows > 0 && bad_matrix(x, ldx, t)) || bad_matrix(w, ldw, k) || ldo < f || !rows_apart(groups, group_stride, n, ldw, k) || (groups > 1 && ((group_stride & 7) || group_stride >= (1ll << 38))))
         return refuse("grouped product: operands need 16-byte aligned rows (strides in multiples of eight elements) that do not overlap");
     if (device < 0) return EW_ERR_NO_DEVICE;
     if (rows == 0) return EW_OK;
@@ -693,7 +693,7 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
                                         int32_t accumulate, void *dw, int64_t lddw, int64_t group_stride, void *cuda_stream) {
     ew_status_t s = check_common(dtype, out_dtype, offsets, rows, groups, n, k, dw);
     if (s != EW_OK) return s;
-    if (lddw < k || (groups > 1 && group_stride < (int64_t)(n - 1) * lddw + k))
+    if (lddw < k || !rows_apart(groups, group_stride, n, lddw, k))
         return refuse("grouped product: the weight gradient's rows overlap");
     if (rows > 0 && (bad_matrix(dy, lddy, n) || bad_matrix(x, ldx, k)))
         return refuse("grouped product: operands need 16-byte aligned rows (strides in multiples of eight elements) that do not overlap");

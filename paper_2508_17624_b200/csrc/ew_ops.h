@@ -44,6 +44,12 @@ inline CUtensorMapDataType map_type(int dtype) {
     return dtype == EW_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
 }
 
+// Whether `count` row-major matrices [rows, width] keep their rows apart: they lie one behind the other, or take turns row by row
+// (as the middle dimension of a [rows, count, width] tensor).
+inline bool rows_apart(int64_t count, int64_t stride, int64_t rows, int64_t ld, int64_t width) {
+    return count < 2 || stride >= (__int128)(rows - 1) * ld + width || (stride >= width && ld >= (__int128)(count - 1) * stride + width);
+}
+
 inline ew_status_t refuse(const char *why) {
     set_last_error(why);
     return EW_ERR_INVALID_ARG;

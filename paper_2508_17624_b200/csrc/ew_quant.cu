@@ -823,7 +823,7 @@ extern "C" ew_status_t ew_quant_pack(int32_t device, int32_t dtype, const void *
     if (!is_16bit(dtype)) return refuse("packing: weights are bf16 or fp16");
     if (bad_group(group, k)) return refuse("packing: groups of 32, 64 or 128 weights that divide k");
     if (n_slots < 1 || n < 8 || n % 8) return refuse("packing: size out of range (n in multiples of 8)");
-    if (ldw < k || (n_slots > 1 && slot_stride < (int64_t)(n - 1) * ldw + k) || !w || !q || !scales || ((uintptr_t)w & 1) ||
+    if (ldw < k || !rows_apart(n_slots, slot_stride, n, ldw, k) || !w || !q || !scales || ((uintptr_t)w & 1) ||
         (((uintptr_t)q | (uintptr_t)scales) & 15))
         return refuse("packing: null or misaligned pointer, or overlapping rows (q and scales on 16 bytes)");
     if (device < 0) return EW_ERR_NO_DEVICE;

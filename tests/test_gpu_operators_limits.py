@@ -212,3 +212,28 @@ def test_as_many_pairs_as_a_call_takes():
     for at in (slice(0, 5000), slice(pairs - 5000, pairs), slice(1000003, None, 1000003), slice(7, None, 999983)):
         assert torch.equal(y[at], every[slots[at].long()])
     assert binding.last_operator_error() == 0
+
+
+@pytest.mark.parametrize("n,k", [(72, 136), (300, 264)])
+def test_groups_that_take_turns_row_by_row(n, k):
+    """w, dw and what is packed as the middle dimension of an [n, groups, k] tensor: the same bits as with groups apart."""
+    groups, counts = 4, [5, 0, 150, 70]
+    offsets = torch.tensor([0] + counts, device="cuda").cumsum(0).int()
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x, dy = (torch.randn((sum(counts), v), device="cuda", generator=g).to(BF16) for v in (k, (n + 7) // 8 * 8))
+    dy = dy[:, :n]
+    w = (torch.randn((groups, n, k), device="cuda", generator=g) * 0.05).to(BF16)
+    turns = w.transpose(0, 1).contiguous().transpose(0, 1)
+    assert turns.stride() == (k, groups * k, 1)
+    for fn, rows in ((binding.grouped_mm, x), (binding.grouped_mm_dx, dy)):
+        assert torch.equal(fn(rows, turns, offsets), fn(rows, w, offsets))
+    for rows in (slice(None), slice(0, 0)):
+        ends = offsets if rows == slice(None) else torch.zeros_like(offsets)
+        whole = torch.full((n, groups + 1, k), 7.0, device="cuda")
+        out = whole[:, :groups].transpose(0, 1)
+        want = binding.grouped_mm_dw(dy[rows], x[rows], ends, out_dtype=FP32)
+        assert torch.equal(binding.grouped_mm_dw(dy[rows], x[rows], ends, out=out), want) and (whole[:, groups] == 7).all()
+        assert torch.equal(binding.grouped_mm_dw(dy[rows], x[rows], ends, out=out, accumulate=True), 2 * want)
+    if n % 8 == 0:
+        for a, b in zip(binding.quant_pack(turns[:, :, :128], 64), binding.quant_pack(w[:, :, :128], 64)):
+            assert torch.equal(a, b)

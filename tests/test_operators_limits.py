@@ -99,3 +99,24 @@ def test_quant_mv_widths_near_two_to_the_31(lib):
     assert mv(lib, n_slots=1, n=33554400, ldy=33554400) == NO_DEVICE
     for n_slots, n in ((1, 33554408), (1, 0x7ffffff8), (1, 0x7fffffe8), (64, 33554432), (2048, 1048576)):
         assert mv(lib, n_slots=n_slots, n=n, ldy=n) == INVALID, (n_slots, n)
+
+
+def test_strides_of_groups(lib):
+    """Groups one behind the other or row by row; a stride whose product with the rows passes 64 bits is not taken for a small one."""
+    def mm(fn, ld, stride, groups=3, n=64, k=64):
+        return getattr(lib, fn)(-1, BF16, BF16, X, 64, W, ld, stride, OFF, 8, groups, n, k, OUT, max(n, k), None)
+
+    def dw(ld, stride, groups=3, n=64, k=64):
+        return lib.ew_grouped_mm_dw(-1, BF16, FP32, X, max(n, 64), W, 64, OFF, 8, groups, n, k, 0, OUT, ld, stride, None)
+
+    def pack(ld, stride, groups=3, n=64, k=64):
+        return lib.ew_quant_pack(-1, BF16, X, ld, stride, groups, n, k, 32, W, OUT, None)
+
+    for call in (lambda *a, **b: mm("ew_grouped_mm", *a, **b), lambda *a, **b: mm("ew_grouped_mm_dx", *a, **b), dw, pack):
+        assert call(64, 64 * 64) == call(72, 63 * 72 + 64) == call(3 * 64, 64) == call(2 * 72 + 64, 72) == NO_DEVICE
+        assert call(64, 0, groups=1) == NO_DEVICE and (call is pack or call(64, 64, n=1) == NO_DEVICE)
+        for ld, stride in ((64, 63 * 64), (72, 63 * 72 + 56), (2 * 64 + 56, 64), (3 * 64, 56), (3 * 64, 0), (64, -64 * 64), (3 * 64, -64)):
+            assert call(ld, stride) == INVALID, (ld, stride)
+    # (2^31 - 65536) rows of 2^37 elements pass 2^64
+    assert dw(2 ** 37, 64, n=0x7fff0000) == NO_DEVICE and dw(2 ** 37, 56, n=0x7fff0000) == INVALID
+    assert dw(2 ** 33 + 2 ** 18, 2 ** 40, n=0x7fff0000) == INVALID and mm("ew_grouped_mm", 2 ** 37, 2 ** 37 + 8, n=0x7fff0000) == INVALID
