@@ -331,8 +331,8 @@ typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2 } ew_dtype_t;
  *     y[r, :] = x[r, :] w[g]^T        x [rows, k], w [groups, n, k] (group_stride elements between groups), y [rows, n]
  * summed in fp32 and rounded once.  The tensor core cuts the running sum off instead of rounding it; sums are made in parts
  * (1024 terms for fp32 results, 8192 for fp16, 65536 for bf16) that are added up rounded, so that the result is off by at most
- * 1e-5 (fp32 results) or an eighth of half a step of its type (16-bit ones) of sum |x w| besides its own rounding, whatever the
- * length.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
+ * 1e-5 (fp32 results) or an eighth of half a step of its type (16-bit ones) of sum |x w| besides its own rounding and half a step
+ * of fp32 a part.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
  * they need not start at 0 nor end at `rows`, and rows outside them are left as they were.  An offset below the one
  * before it or outside [0, rows] is clamped and reported as EW_ERR_INVALID_ARG.
  * dtype: EW_BF16 or EW_FP16; out_dtype: the same or EW_FP32.  x and w are 16-byte aligned with ldx, ldw and
@@ -368,7 +368,8 @@ ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t out_dtype, c
  *           the weight 2i and bits 16+4i..16+4i+3 the weight 2i + 1, i = 0..3
  *   scales  of x's type [n_slots, k/group, n];  group 32, 64 or 128, a divisor of k;  n a multiple of 8
  *   x       [pairs / pairs_per_row, k];  x, q and scales 16-byte aligned, ldx a multiple of 8;  y [pairs, n]
- * A row of x with an infinity or NaN in it gives rows of infinities and NaN, other rows do not see it.
+ * A row of x with an infinity or NaN in it gives rows of infinities and NaN, other rows do not see it.  With few pairs a slot x
+ * enters as whole numbers, a group at a time: off by at most 1/8355711 of the group's largest, or 2^-127 where that is more.
  * Every pair count is taken; beyond some 32 rows a slot the 16-bit weights' ew_grouped_mm is the better call.
  * n_slots <= 2048, k <= 16384, n <= 33554400, n_slots * n < 2^31.  Errors: EW_ERR_INVALID_ARG, EW_ERR_NO_DEVICE, EW_ERR_CUDA. */
 ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dtype, const void *x, int64_t ldx, const void *q,
@@ -383,7 +384,7 @@ ew_status_t ew_quant_pack(int32_t device, int32_t dtype, const void *w, int64_t 
 
 /* SwiGLU between an expert's two linears (Section 2.1's expert FFN), with the routing weight of a row folded in:
  *     act[r, i] = row_weights[r] * silu(h[r, i]) * h[r, inter + i]     h [rows, 2 inter]: gate block, then up block
- * computed in fp32, rounded once.  row_weights: fp32 [rows], or null for 1.  h and act: dtype EW_BF16 or EW_FP16; any
+ * computed in fp32, rounded once; silu of a gate below -87.3 is 0 (it is above -1.1e-36).  row_weights: fp32 [rows], or null for 1.  h and act: dtype EW_BF16 or EW_FP16; any
  * alignment is taken, rows on 16-byte boundaries are fastest. */
 ew_status_t ew_swiglu(int32_t device, int32_t dtype, const void *h, int64_t ldh, const float *row_weights, int32_t rows,
                       int32_t inter, void *act, int64_t ldact, void *cuda_stream);

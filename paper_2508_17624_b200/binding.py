@@ -432,7 +432,8 @@ def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
 
 def grouped_mm(x, w, offsets, out=None, out_dtype=None):
     """y[r] = x[r] w[g]^T for the rows offsets[g] <= r < offsets[g+1] of each group: x [rows, k], w [groups, n, k], offsets
-    int32 [groups + 1] (all on one device).  Rows outside the offsets are left as they were in `out`.  out_dtype: x's type
+    int32 [groups + 1] (all on one device).  Rows outside the offsets are left as they were in `out`, and undefined in a
+    new result.  out_dtype: x's type
     or float32.  See the header for alignment."""
     return _rows_product(lib().ew_grouped_mm, "ew_grouped_mm", x, w, offsets, out, out_dtype, False)
 

@@ -48,7 +48,7 @@ constexpr int threads_of(int epilogue_warps) { return (3 + epilogue_warps) * 32;
 constexpr int kATile = 128 * kBlockK * 2;              // 16 KiB: 128 f of one stage
 constexpr int kMaxGroups = 2048;                       // bounds the group table in shared memory
 constexpr int kSmemLimit = 227 * 1024;
-constexpr int kMaxStages = 12;
+constexpr int kMaxStages = 7;                          // of 32 KiB
 // The tensor core cuts off, rather than rounds, what a product has below the running sum's last bit.  Over terms of one sign
 // that takes 6.4e-9 of the result a term (5.8e-6 at 1024, 4.1e-4 at 65536: measured), over random ones a tenth of it.  Long
 // sums are therefore made in parts of so many k-blocks, which the epilogue adds up in fp32: fp32 results 1024 terms at a time
@@ -83,8 +83,9 @@ struct Cfg {
     static constexpr int kBRows = NT / CG;                                   // c staged by each CTA
     static constexpr int kStageBytes = kATile + kBRows * kBlockK * 2;
     static constexpr int kTile = 128 * CG;                                   // f of an item
-    static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+    static constexpr int kTmemCols = 2 * NT;                                 // two accumulator sets
     static constexpr int kStep = 16 * CG;                                    // granularity of an MMA's N
+    static_assert((kSmemLimit - 1024) / kStageBytes <= kMaxStages, "barriers for every stage that fits");
 };
 
 // The row operand's tensor maps: boxes of 32, 64, 96 and 128 rows (weight gradient: one map).  A stage's rows come in one
@@ -308,7 +309,8 @@ grouped_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
             it.kb = (cnt + kBlockK - 1) / kBlockK;
             it.tail = cnt - (it.kb - 1) * kBlockK;
         } else {
-            // the group's rows in equal blocks (multiples of the MMA's step): 257 rows make 144 + 113, not 256 + 1
+            // the group's rows in equal blocks, rounded up to the MMA's step: 257 rows make 160 + 97 (pair) or 96 + 96 + 65, not
+            // 256 + 1 (2049 rows, whose nine equal blocks round up to 256 each, still make eight of 256 and one of 1)
             const int nb = t_pre[lo + 1] - t_pre[lo];
             const int size = ((cnt + nb - 1) / nb + C::kStep - 1) / C::kStep * C::kStep;
             it.row0 = t_lo[lo] + b * size;
@@ -551,7 +553,7 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     if (max_items > 0x7fff0000) return refuse("grouped product: too many output tiles");
     a.table_bytes = (3 * a.groups + 1) * 4;
     const int room = kSmemLimit - 1024 - kBarBytes - a.table_bytes;
-    a.stages = room / C::kStageBytes < kMaxStages ? room / C::kStageBytes : kMaxStages;
+    a.stages = room / C::kStageBytes;
     cudaLaunchConfig_t cfg = {};
     const long long units = d.sm_count / CG;
     cfg.gridDim = dim3((unsigned)(CG * (max_items < units ? max_items : units)));
@@ -656,7 +658,8 @@ ew_status_t rows_product(bool grad, int32_t device, int32_t dtype, int32_t out_d
         return grad ? launch<CG, NT, 4, kInputGrad>(*d, ma, mb, a, items, t, st) : launch<CG, NT, 4, kProduct>(*d, ma, mb, a, items, t, st); \
     } while (0)
     // (64 groups of 2816 x 2048, one CTA with 128 columns against the pair: 96 rows a group 127.7 and 130.0 us, 128 rows 134.1 and
-    // 134.7, 160 rows 214 and 141)
+    // 134.7, 160 rows 214 and 141.  The host knows only how many groups there are, not which have rows: offsets over many empty
+    // slots make the groups look shorter than they are, and the one-CTA form may be taken where the pair would be faster)
     if (rows <= 128ll * groups) EW_LAUNCH(1, 128);
     EW_LAUNCH(2, 256);
 #undef EW_LAUNCH
@@ -744,6 +747,6 @@ extern "C" ew_status_t ew_grouped_mm_dw(int32_t device, int32_t dtype, int32_t o
     const long long items = (long long)groups * a.c_tiles * a.f_tiles;
     if (accumulate) return launch<2, 256, 8, kWeightAdd>(*d, ma, mb, a, items, rows, st);
     // Few rows a group: the results' way out is what counts, and eight warps walk it (192 rows: 80 us against 95); many: the
-    // arithmetic does, at the power limit, where four cost less (768 rows: 259 against 270).
+    // arithmetic does, at the power limit, where four cost less (768 rows: 259 against 270).  Empty groups count as above.
     return rows <= 256ll * groups ? launch<2, 256, 8, kWeightGrad>(*d, ma, mb, a, items, rows, st) : launch<2, 256, 4, kWeightGrad>(*d, ma, mb, a, items, rows, st);
 }

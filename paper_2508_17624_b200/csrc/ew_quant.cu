@@ -12,8 +12,8 @@
 // instruction multiplies 512 weights with eight pairs (2.1 cycles of an SM measured, what bf16 takes for 256; the 8-bit
 // floating-point form is made of 16-bit ones on this machine and slower).  x goes in as fixed-point numbers: a group of x,
 // which the scales split off anyway, is scaled by a power of two so that its largest magnitude lies above 4177855, rounded
-// to whole numbers and cut into three signed bytes.  That rounding is below 1/8355711 of the group's largest x, and none at
-// all for bf16 values down to a 2^15th of it (two bytes would cost 9 to 13 % less time, but a group with one large value
+// to whole numbers and cut into three signed bytes.  That rounding is below 1/8355711 of the group's largest x (or 2^-127, the most
+// that the scale's power of two goes down to), and none at all for bf16 values down to a 2^15th of it (two bytes would cost 9 to 13 % less time, but a group with one large value
 // would leave its small ones six bits).  The products' sums are exact integers, the offset 8 is their first value
 // (-8 sum x); only then come fp32 numbers: group sum times scale, added up over the groups.  A slot with many pairs repays
 // the unpacking: there the weights become 16-bit numbers (q - 8, exact) and x stays as it is.
@@ -26,7 +26,8 @@
 // Measured (one B200, copy bandwidth 6551 GB/s), 2816 x 2048 weights unless said: one token's six experts 8.9 us (18 MB; 2.7 us
 // of bytes behind a launch, the slots' way from memory and the first line's); 96
 // pairs over 96 slots of 2048 x 1408 27 us = 3.4 TB/s; 256 tokens, some sixteen pairs a slot, 114 us = 2.7 TB/s, bound by the
-// instructions around the products (73 % of the issue slots while a line is worked on).
+// instructions around the products together with the latencies between them (55 % of the issue slots of the active cycles, 40 % of the
+// tensor pipe's; 127 registers leave room for sixteen warps).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -805,7 +806,8 @@ extern "C" ew_status_t ew_quant_mv(int32_t device, int32_t dtype, int32_t out_dt
         // One column of eight pairs with x in bytes, or up to three with x as it is: what a slot has more is another job, which
         // reads its weights again.  The bytes' sums are scaled group by group, so they pay with long groups and few pairs.
         // Measured (64 slots of 2816 x 2048; bytes, then 16 bits): groups of 128 with 2 pairs a slot 42 and 48 us, 4: 52 and 53,
-        // 8: 70 and 60; groups of 64 with 1 pair 37.6 and 38.4, 3: 57 and 56, 6: 71 and 62.
+        // 8: 70 and 60; groups of 64 with 1 pair 37.6 and 38.4, 3: 57 and 56, 6: 71 and 62.  The pairs are counted against all slots,
+        // since the host does not know which of them the batch uses: over mostly unused slots this takes bytes longer than it should.
         const int nt = a.pairs <= 8 || 24ll * a.pairs <= (long long)n_slots * group ? 1 : 3;
         const int smem = lay_out(a, nt, group);
         if (!smem) return refuse("4-bit product: k is too large for a row of x in shared memory");
