@@ -398,6 +398,8 @@ def _offsets(offsets, dev, T, like):
 def _result(out, shape, dtype, like, name="out"):
     if out is None:
         return like.new_empty(shape, dtype=dtype)
+    if out.requires_grad and _torch().recording():
+        raise ValueError(f"{name}: autograd is recording it and would not see it overwritten; pass it under torch.no_grad(), or a tensor of its own")
     _on(out, like, len(shape), name)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise ValueError(f"{name}: {tuple(shape)} of {dtype} is wanted, got {tuple(out.shape)} of {out.dtype}")

@@ -120,3 +120,20 @@ def test_strides_of_groups(lib):
     # (2^31 - 65536) rows of 2^37 elements pass 2^64
     assert dw(2 ** 37, 64, n=0x7fff0000) == NO_DEVICE and dw(2 ** 37, 56, n=0x7fff0000) == INVALID
     assert dw(2 ** 33 + 2 ** 18, 2 ** 40, n=0x7fff0000) == INVALID and mm("ew_grouped_mm", 2 ** 37, 2 ** 37 + 8, n=0x7fff0000) == INVALID
+
+
+def test_results_that_autograd_records_are_refused():
+    """Written by the library, they would change under autograd's hands."""
+    def out(*shape, dtype=torch.bfloat16):
+        t = Huge(*shape, dtype=dtype)
+        t.requires_grad = True
+        return t
+
+    x, w, offsets = Huge(4, 64), Huge(2, 64, 64), Huge(3, dtype=torch.int32)
+    calls = [lambda: binding.grouped_mm(x, w, offsets, out=out(4, 64)), lambda: binding.grouped_mm_dx(x, w, offsets, out=out(4, 64)),
+             lambda: binding.grouped_mm_dw(x, x, offsets, out=out(2, 64, 64), accumulate=True), lambda: binding.swiglu(x, out=out(4, 32)),
+             lambda: binding.swiglu_grad(Huge(4, 32), x, out=out(4, 64)),
+             lambda: binding.quant_mv(x, Huge(1, 64, 32, dtype=torch.uint8), Huge(1, 2, 64), out=out(4, 64))]
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
