@@ -23,12 +23,12 @@
 // 256 columns, every operand byte crossing from L2 once per 256 x 256 tile.
 //
 // Measured (one B200; copy bandwidth 6551 GB/s, cuBLAS bf16 1655 TFLOP/s in a burst, 1403 sustained):
-//   y,  1536 rows, 96 groups, 2816 x 2048   174 us = 6.44 TB/s, 98 % of the copy bandwidth (bound by the weights' bytes)
-//   y, 49152 rows, 64 groups, 2816 x 2048   510 us sustained = 1110 TFLOP/s (1337 in a burst), bound by the tensor cores at
+//   y,  1536 rows, 96 groups, 2816 x 2048   174 to 181 us = 6.2 to 6.4 TB/s, 95 to 98 % of the copy bandwidth (bound by the weights' bytes)
+//   y, 49152 rows, 64 groups, 2816 x 2048   490 to 551 us sustained = 1030 to 1160 TFLOP/s (1337 in a burst), bound by the tensor cores at
 //                                           the power limit; the MMA thread waits for data 17 % of the time
-//   dx, 24582 rows, 64 groups, 2048 x 1408  143 to 168 us: 384 rows a group leave 192-column tiles, and a tile costs 218 ns a
+//   dx, 24582 rows, 64 groups, 2048 x 1408  143 to 174 us: 384 rows a group leave 192-column tiles, and a tile costs 218 ns a
 //                                           k-block plus 0.7 ns a column whatever its width
-//   dw, 12289 rows, 32 groups, fp32         183 to 215 us = 4.3 TB/s: 738 MB of results, 128 bytes every five cycles of
+//   dw, 12289 rows, 32 groups, fp32         183 to 222 us = 3.9 to 4.7 TB/s: 738 MB of results, 128 bytes every five cycles of
 //                                           an SM while the epilogue stores, which it does 70 % of the time
 
 #include <cuda_bf16.h>
