@@ -316,7 +316,8 @@ ew_status_t ew_selftest_bounded_wait(ew_pool_t *pool, void *cuda_stream);
 /* ------------------------------------------------------------------------------------------------------------
  * Stand-alone operators: the pieces of an expert outside a forward, for callers that tune an adapter's experts (the
  * products' gradients, which ew_load_adapter's weights come from) or serve them in four bits.  They take no pool.
- *   device       CUDA device ordinal that all pointers and the stream belong to; -1 gives EW_ERR_NO_DEVICE
+ *   device       CUDA device ordinal that all pointers and the stream belong to (its primary context); -1 gives
+ *                EW_ERR_NO_DEVICE
  *   dtype        type of the operands; out_dtype of the results (ew_dtype_t)
  *   ld*          elements between the rows of a row-major matrix; the innermost dimension is contiguous
  * All pointers are DEVICE memory; results may not overlap operands; calls are asynchronous on cuda_stream, allocate

@@ -105,15 +105,19 @@ namespace ew {
 
 void set_last_error(const std::string &s);
 
-// Makes a device current for the duration of an entry point and puts the caller's device back on exit.  It is set even where it
-// is the thread's device already: a thread that has made no CUDA call yet is on device 0 without a context, and the tensor-map
-// encoder, a driver function, wants one (57 ns a call).
+// Whether a context is current on this thread.  A thread that has made no CUDA call yet is on device 0 without one.
+bool thread_has_context();
+
+// Makes a device current for the duration of an entry point and puts the caller's device back on exit.  Where it is the thread's
+// device already it is set only if the thread has no context yet, which the tensor-map encoder, a driver function, wants (setting
+// it every time would take a thread with a context of its own making out of that).
 struct DeviceGuard {
     int prev = -1;
     bool switched = false;
     cudaError_t enter(int device) {
         cudaError_t e = cudaGetDevice(&prev);
         if (e != cudaSuccess) return e;
+        if (prev == device && thread_has_context()) return e;
         e = cudaSetDevice(device);
         switched = e == cudaSuccess && prev != device;
         return e;

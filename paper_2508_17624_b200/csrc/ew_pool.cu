@@ -10,6 +10,17 @@
 namespace ew {
 static thread_local std::string g_last_error;
 void set_last_error(const std::string &s) { g_last_error = s; }
+
+bool thread_has_context() {
+    using GetCurrent = CUresult (*)(CUcontext *);
+    static const GetCurrent get = [] {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuCtxGetCurrent", &fn, cudaEnableDefault, &q) == cudaSuccess ? reinterpret_cast<GetCurrent>(fn) : nullptr;
+    }();
+    CUcontext c = nullptr;
+    return get && get(&c) == CUDA_SUCCESS && c;
+}
 bool fat_enabled() {
     static const bool on = [] { const char *e = getenv("EW_DISABLE_FAT"); return !(e && e[0] == '1'); }();
     return on;

@@ -1,4 +1,5 @@
 """The stand-alone operators and the pool's forward called from other threads than the main one."""
+import ctypes as C
 import threading
 
 import pytest
@@ -97,3 +98,24 @@ def test_several_threads_at_once_on_streams_of_their_own():
             for a, b in zip(some, want):
                 assert torch.equal(a, b)
     assert binding.last_operator_error() == 0
+
+
+def test_a_threads_own_context_stays_current():
+    """A thread that works in a context it made itself is still in it after a call.  (The call sees the device and has nothing to
+    do, so nothing of the main context is used in the other one.)"""
+    cu, lib = C.CDLL("libcuda.so.1"), binding.lib()
+    x = torch.ones((4, 32), dtype=BF16, device="cuda")
+    want = binding.swiglu(x)                            # the device's constants are there
+
+    def call():
+        mine, now = C.c_void_p(), C.c_void_p()
+        assert cu.cuCtxCreate_v2(C.byref(mine), 0, 0) == 0
+        # no rows, added to what is there
+        assert lib.ew_grouped_mm_dw(0, 0, 2, None, 64, None, 64, 0x1000, 0, 1, 64, 64, 1, 0x1000, 64, 0, None) == 0
+        assert cu.cuCtxGetCurrent(C.byref(now)) == 0
+        same = now.value == mine.value
+        assert cu.cuCtxDestroy_v2(mine) == 0
+        return same
+
+    assert in_threads([call]) == [True]
+    assert torch.equal(binding.swiglu(x), want)
