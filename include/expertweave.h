@@ -314,8 +314,8 @@ ew_status_t ew_last_device_error(ew_pool_t *pool, int32_t *code);
 ew_status_t ew_selftest_bounded_wait(ew_pool_t *pool, void *cuda_stream);
 
 /* ------------------------------------------------------------------------------------------------------------
- * Stand-alone operators: the pieces of an expert outside a forward, for callers that tune an adapter's experts (the
- * products' gradients, which ew_load_adapter's weights come from) or serve them in four bits.  They take no pool.
+ * Stand-alone operators: the pieces of an expert outside a forward and the norm before it, for callers that tune an adapter's experts (the
+ * products' gradients, which ew_load_adapter's weights come from) or serve them in eight or four bits.  They take no pool.
  *   device       CUDA device ordinal that all pointers and the stream belong to (its primary context); -1 gives
  *                EW_ERR_NO_DEVICE
  *   dtype        type of the operands; out_dtype of the results (ew_dtype_t)
@@ -325,7 +325,7 @@ ew_status_t ew_selftest_bounded_wait(ew_pool_t *pool, void *cuda_stream);
  * that device outside a capture.  An index in device memory that lies outside its range cannot fail the call: it is
  * clamped or skipped as said below and reported by ew_last_operator_error.
  * ------------------------------------------------------------------------------------------------------------ */
-typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2 } ew_dtype_t;
+typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2, EW_E4M3 = 3, EW_E5M2 = 4 } ew_dtype_t;   /* the last two: 8-bit floats */
 
 /* Matrix product grouped by expert (Section 2.1's grouped matrix multiplication, on its own): for every group g and
  * its rows offsets[g] <= r < offsets[g+1]
@@ -395,6 +395,64 @@ ew_status_t ew_swiglu(int32_t device, int32_t dtype, const void *h, int64_t ldh,
 ew_status_t ew_swiglu_grad(int32_t device, int32_t dtype, const void *dact, int64_t lddact, const void *h, int64_t ldh,
                            const float *row_weights, int32_t rows, int32_t inter, void *dh, int64_t lddh,
                            float *drow_weights, void *cuda_stream);
+
+/* 8-bit floating point in blocks.  A block of 128 values is held as 8-bit floats q (EW_E4M3, largest 448, or EW_E5M2, 57344) and
+ * one exponent byte c, and stands for q 2^(c - 127); c = 255 is NaN.  The operators that write blocks choose the smallest c >= 0
+ * with which the block's largest finite value fits the type, and round a value once, to nearest even; an infinity or NaN
+ * becomes the type's NaN and takes no part in the scale.
+ *   rows     q [rows, width] with ldq elements between rows, scales [rows, ceil(width / 128)] with ldscales bytes between
+ *            rows: a scale for 128 neighbouring values of a row (the last of a row may be shorter)
+ *   weights  q [n_slots, n, k], scales [n_slots, ceil(n / 128), ceil(k / 128)] without gaps: a scale for 128 x 128 values
+ * The products below read q from 16-byte aligned rows (ldq and strides multiples of 16) and the rows' scales from 4-byte aligned ones (ldscales
+ * a multiple of 4); the operators that write them take any strides.  Bytes behind a row's end are neither read nor written. */
+
+/* Rows x [rows, width] (bf16 or fp16) as blocks of q_type. */
+ew_status_t ew_scaled_rows(int32_t device, int32_t dtype, int32_t q_type, const void *x, int64_t ldx, int32_t rows, int32_t width,
+                           void *q, int64_t ldq, void *scales, int64_t ldscales, void *cuda_stream);
+
+/* Weights w [n_slots, n, k] (bf16 or fp16; slot_stride elements between matrices) as blocks of 128 x 128 in EW_E4M3.  q_stride: elements between
+ * the matrices of q.  n_slots <= 2048. */
+ew_status_t ew_scaled_pack(int32_t device, int32_t dtype, const void *w, int64_t ldw, int64_t slot_stride, int32_t n_slots, int32_t n,
+                           int32_t k, void *q, int64_t ldq, int64_t q_stride, void *scales, void *cuda_stream);
+
+/* The grouped product of ew_grouped_mm with both operands in blocks:
+ *     y[r, :] = x[r, :] w[g]^T  for  offsets[g] <= r < offsets[g+1]     of the values that the blocks stand for
+ * x: blocks of rows, row_type EW_E4M3 or EW_E5M2; w: blocks of weights in EW_E4M3 (group_stride elements between matrices).  Every product
+ * is exact; sums are fp32, made in parts as there and with the same bound.  out_dtype: EW_BF16, EW_FP16 or EW_FP32.
+ * offsets: as there, and what is said there of rows outside them and of bad offsets; null: one group (groups = 1) of all rows.
+ * groups <= 2048.  rows = 0 is a no-op. */
+ew_status_t ew_scaled_mm(int32_t device, int32_t row_type, int32_t out_dtype, const void *x, int64_t ldx, const void *x_scales,
+                         int64_t ldxs, const void *w, int64_t ldw, int64_t group_stride, const void *w_scales, const int32_t *offsets,
+                         int32_t rows, int32_t groups, int32_t n, int32_t k, void *y, int64_t ldy, void *cuda_stream);
+
+/* Its gradient with respect to x's values:  dx[r, :] = dy[r, :] w[g],  dy blocks of rows of n values; all else as above.  (The
+ * weights' gradient sums over rows, along which nothing has blocks: ew_grouped_mm_dw on the 16-bit rows.) */
+ew_status_t ew_scaled_mm_dx(int32_t device, int32_t row_type, int32_t out_dtype, const void *dy, int64_t lddy, const void *dy_scales,
+                            int64_t lddys, const void *w, int64_t ldw, int64_t group_stride, const void *w_scales,
+                            const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k, void *dx, int64_t lddx,
+                            void *cuda_stream);
+
+/* ew_swiglu with its result as blocks of rows in EW_E4M3 (rounded once, from fp32). */
+ew_status_t ew_swiglu_scaled(int32_t device, int32_t dtype, const void *h, int64_t ldh, const float *row_weights, int32_t rows,
+                             int32_t inter, void *q, int64_t ldq, void *scales, int64_t ldscales, void *cuda_stream);
+
+/* RMS norm before a layer, with the residual's addition:
+ *     t = x + residual (fp32, rounded to dtype),   y = t / sqrt(mean(t^2) + eps) * weight      x [rows, width], weight [width]
+ * in fp32, rounded once.  residual null: t = x; otherwise t is written to sum [rows, width], which may be residual itself (same
+ * address and stride) but no other operand.  Results: y [rows, width] in dtype (null: not wanted), q and scales: blocks of rows in EW_E4M3 of
+ * the unrounded y (null: not wanted); one of them at least.  dtype: EW_BF16 or EW_FP16; any alignment is taken, rows on
+ * 16-byte boundaries are fastest.  A row's sum of squares has to fit fp32 (values up to 1e17).  width <= 16384. */
+ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,
+                        float eps, int32_t rows, int32_t width, void *sum, int64_t ldsum, void *y, int64_t ldy, void *q, int64_t ldq,
+                        void *scales, int64_t ldscales, void *cuda_stream);
+
+/* Its gradient: dt [rows, width] = the gradient with respect to t (and so to x and residual each) from dy and t, plus dt_in, the gradient that
+ * reaches t past the norm (null: none), and dweight fp32 [width], summed over the rows in a fixed order.  workspace: fp32
+ * [ew_rms_norm_grad_parts(rows, width), width], of this call alone while it runs. */
+ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight,
+                             const void *dt_in, int64_t lddt_in, float eps, int32_t rows, int32_t width, void *dt, int64_t lddt,
+                             float *dweight, float *workspace, void *cuda_stream);
+int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width);
 
 /* Read and clear the operators' error word of a device (waits for all work on it).  *code receives EW_OK,
  * EW_ERR_INVALID_ARG (an index in device memory was outside its range) or EW_ERR_TIMEOUT (a bounded wait expired).  Where both

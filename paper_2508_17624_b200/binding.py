@@ -24,7 +24,8 @@ EXPORTS = ["ew_pool_create", "ew_pool_destroy", "ew_load_base", "ew_load_adapter
            "ew_pool_trim", "ew_moe_forward", "ew_moe_forward_debug", "ew_moe_forward_host", "ew_profile_enable",
            "ew_profile_read", "ew_reroute", "ew_reroute_unfused", "ew_route_logits", "ew_route_noalloc", "ew_selftest_bounded_wait", "ew_get_expert_map",
            "ew_moe_forward_partial", "ew_ep_finish", "ew_moe_forward_scatter", "ew_ep_finish_gathered", "ew_pool_stats", "ew_last_device_error", "ew_slot_address", "ew_grouped_mm", "ew_grouped_mm_dx", "ew_grouped_mm_dw",
-           "ew_quant_mv", "ew_quant_pack", "ew_swiglu", "ew_swiglu_grad", "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
+           "ew_quant_mv", "ew_quant_pack", "ew_swiglu", "ew_swiglu_grad", "ew_scaled_rows", "ew_scaled_pack", "ew_scaled_mm", "ew_scaled_mm_dx",
+           "ew_swiglu_scaled", "ew_rms_norm", "ew_rms_norm_grad", "ew_rms_norm_grad_parts", "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
 
 
 class EwConfig(C.Structure):
@@ -77,6 +78,13 @@ def lib():
         _lib.ew_quant_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, i32, ptr, ptr, ptr]
         _lib.ew_swiglu.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr]
         _lib.ew_swiglu_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, ptr, i64, ptr, ptr]
+        _lib.ew_scaled_rows.argtypes = [i32, i32, i32, ptr, i64, i32, i32, ptr, i64, ptr, i64, ptr]
+        _lib.ew_scaled_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, ptr, i64, i64, ptr, ptr]
+        for name in ("ew_scaled_mm", "ew_scaled_mm_dx"):
+            getattr(_lib, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i64, i64, ptr, ptr, i32, i32, i32, i32, ptr, i64, ptr]
+        _lib.ew_swiglu_scaled.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr, i64, ptr]
+        _lib.ew_rms_norm.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, C.c_float, i32, i32, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
+        _lib.ew_rms_norm_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, ptr, ptr]
     return _lib
 
 
@@ -312,7 +320,9 @@ class _Torch:
     def load(cls):
         import torch
         cls.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-        cls.int32, cls.float32, cls.uint8 = torch.int32, torch.float32, torch.uint8
+        cls.int32, cls.float32, cls.uint8, cls.bfloat16 = torch.int32, torch.float32, torch.uint8, torch.bfloat16
+        cls.e4m3, cls.e5m2, cls.exponent = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
+        cls.eights = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
         cls.recording = torch.is_grad_enabled
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         cls.ready = True
@@ -586,6 +596,232 @@ def swiglu_grad(dact, h, row_weights=None, out=None):
     if rc:
         _check(rc, "ew_swiglu_grad")
     return out if dp is None else (out, dp)
+
+
+# 8-bit floating point in blocks of 128: q (float8_e4m3fn or float8_e5m2) and scales (float8_e8m0fnu, powers of two).  Rows of
+# q lie on 16-byte boundaries and rows of scales on 4-byte ones, as the products want them: results are views of padded tensors
+# where the width is no multiple of 16.
+def _eight(T, dtype, name) -> int:
+    code = T.eights.get(dtype)
+    if code is None:
+        raise ValueError(f"{name}: dtype {dtype} is not supported: float8_e4m3fn, float8_e5m2")
+    return code
+
+
+def _room(width, step):
+    return (width + step - 1) // step * step
+
+
+def _new_blocks(rows, width, dtype, T, like):
+    """(q, scales) of new blocks of rows."""
+    wide, blocks = _room(width, 16), (width + 127) // 128
+    room = _room(blocks, 4)
+    q, scales = like.new_empty((rows, wide), dtype=dtype), like.new_empty((rows, room), dtype=T.exponent)
+    return q if wide == width else q[:, :width], scales if room == blocks else scales[:, :blocks]
+
+
+def _row_blocks(out, rows, width, dtype, T, like):
+    """(q, scales, elements between q's rows, between the scales') of a result in blocks."""
+    if out is None:
+        q, scales = _new_blocks(rows, width, dtype, T, like)
+        return q, scales, _room(width, 16), _room((width + 127) // 128, 4)
+    q, scales = out
+    q, scales = _result(q, (rows, width), dtype, like, "q"), _result(scales, (rows, (width + 127) // 128), T.exponent, like, "scales")
+    return q, scales, q.stride(0) if rows > 1 else width, scales.stride(0) if rows > 1 else scales.shape[1]
+
+
+def scaled_rows(x, dtype=None, out=None):
+    """Rows x [rows, width] (bf16 or fp16) as 8-bit blocks for `scaled_mm`: (q [rows, width] of dtype, float8_e4m3fn by default, scales
+    [rows, ceil(width / 128)]).  The header has the form.  Not differentiable."""
+    T, dev = _torch(), x.get_device()
+    code = _code(T, x.dtype)
+    dtype = T.e4m3 if dtype is None else dtype
+    to = _eight(T, dtype, "scaled_rows")
+    rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
+    q, scales, ldq, lds = _row_blocks(out, rows, width, dtype, T, x)
+    rc = lib().ew_scaled_rows(dev, code, to, x.data_ptr(), ldx, rows, width, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    if rc:
+        _check(rc, "ew_scaled_rows")
+    return q, scales
+
+
+def scaled_pack(w, out=None):
+    """8-bit weights for `scaled_mm` from w [slots, n, k] (bf16 or fp16): (q float8_e4m3fn [slots, n, k], scales [slots, ceil(n / 128),
+    ceil(k / 128)]).  Not differentiable: w may be a parameter, the result is data."""
+    T, dev, dtype = _torch(), w.get_device(), w.dtype
+    code = _code(T, dtype)
+    slots, n, k, ld, stride = _matrices(w, dev, dtype, "w", None)
+    shape = (slots, (n + 127) // 128, (k + 127) // 128)
+    if out is None:
+        wide = _room(k, 16)
+        q, scales = w.new_empty((slots, n, wide), dtype=T.e4m3), w.new_empty(shape, dtype=T.exponent)
+        q = q if wide == k else q[:, :, :k]
+    else:
+        q, scales = _result(out[0], (slots, n, k), T.e4m3, w, "q"), _result(out[1], shape, T.exponent, w, "scales")
+        if not scales.is_contiguous():
+            raise ValueError("scales of weights are contiguous")
+    ldq = q.stride(1) if n > 1 else k
+    rc = lib().ew_scaled_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, q.data_ptr(), ldq, q.stride(0) if slots > 1 else n * ldq, scales.data_ptr(),
+                              T.stream(dev))
+    if rc:
+        _check(rc, "ew_scaled_pack")
+    return q, scales
+
+
+def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype, grad):
+    T, dev = _torch(), a.get_device()
+    row_type = _eight(T, a.dtype, "the rows' operand")
+    rows, width, lda = _matrix(a, dev, a.dtype, "the rows' operand", None)
+    groups, n, k, ldw, stride = _matrices(w, dev, T.e4m3, "w", a)
+    if width != (n if grad else k):
+        raise ValueError(f"rows of {width} do not match w of {tuple(w.shape)}")
+    if not _good(a_scales, dev, T.exponent, 2):
+        _on(a_scales, a, 2, "the rows' scales", T.exponent)
+    if not _good(w_scales, dev, T.exponent, 3):
+        _on(w_scales, a, 3, "w's scales", T.exponent)
+    blocks = (width + 127) // 128
+    if a_scales.shape[0] != rows or a_scales.shape[1] != blocks or (a_scales.stride(1) != 1 and blocks > 1 and rows):
+        raise ValueError(f"the rows' scales: ({rows}, {blocks}), a row's side by side, are wanted, got {tuple(a_scales.shape)}")
+    if tuple(w_scales.shape) != (groups, (n + 127) // 128, (k + 127) // 128) or not w_scales.is_contiguous():
+        raise ValueError(f"w's scales: contiguous ({groups}, {(n + 127) // 128}, {(k + 127) // 128}) are wanted, got {tuple(w_scales.shape)}")
+    if offsets is None:
+        if groups != 1:
+            raise ValueError(f"without offsets there is one matrix, got {groups}")
+    elif _offsets(offsets, dev, T, a) != groups:
+        raise ValueError(f"offsets has {offsets.shape[0]} entries for {groups} groups")
+    lds = a_scales.stride(0) if rows > 1 else _room(blocks, 4)
+    ldw = ldw if n > 1 else _room(k, 16)
+    stride = stride if groups > 1 else n * ldw
+    lda = lda if rows > 1 else _room(width, 16)
+    wide = k if grad else n
+    if out is None:
+        out_dtype = T.bfloat16 if out_dtype is None else out_dtype
+        code, out, ldo = _code(T, out_dtype), a.new_empty((rows, wide), dtype=out_dtype), wide
+    else:
+        out_dtype = out.dtype if out_dtype is None else out_dtype
+        code, out = _code(T, out_dtype), _result(out, (rows, wide), out_dtype, a)
+        ldo = out.stride(0) if rows > 1 else wide
+    rc = fn(dev, row_type, code, a.data_ptr(), lda, a_scales.data_ptr(), lds, w.data_ptr(), ldw, stride, w_scales.data_ptr(),
+            None if offsets is None else offsets.data_ptr(), rows, groups, n, k, out.data_ptr(), ldo, T.stream(dev))
+    if rc:
+        _check(rc, where)
+    return out
+
+
+def scaled_mm(x, x_scales, w, w_scales, offsets=None, out=None, out_dtype=None):
+    """y[r] = x[r] w[g]^T of the values that 8-bit blocks stand for, for the rows offsets[g] <= r < offsets[g+1] of each group: x, x_scales
+    from `scaled_rows`, `rms_norm_scaled` or `swiglu_scaled`, w, w_scales from `scaled_pack`.  offsets None: one matrix, all
+    rows.  out_dtype: bfloat16 (default), float16 or float32.  Rows outside the offsets as in `grouped_mm`."""
+    return _scaled_product(lib().ew_scaled_mm, "ew_scaled_mm", x, x_scales, w, w_scales, offsets, out, out_dtype, False)
+
+
+def scaled_mm_dx(dy, dy_scales, w, w_scales, offsets=None, out=None, out_dtype=None):
+    """The gradient of `scaled_mm` with respect to x's values: dx[r] = dy[r] w[g]; dy, dy_scales [rows, n] from `scaled_rows`, often in
+    float8_e5m2.  (The weights' gradient: `grouped_mm_dw` of the 16-bit rows.)"""
+    return _scaled_product(lib().ew_scaled_mm_dx, "ew_scaled_mm_dx", dy, dy_scales, w, w_scales, offsets, out, out_dtype, True)
+
+
+def swiglu_scaled(h, row_weights=None, out=None):
+    """`swiglu` with its result as 8-bit blocks of rows: (q float8_e4m3fn [rows, inter], scales [rows, ceil(inter / 128)])."""
+    T, dev, dtype = _torch(), h.get_device(), h.dtype
+    if (h.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
+        _recorded("ew_swiglu_scaled")
+    code = _code(T, dtype)
+    rows, two, ldh = _matrix(h, dev, dtype, "h", None)
+    if two < 2 or two % 2:
+        raise ValueError(f"h holds a gate and an up block side by side: an even width is wanted, got {two}")
+    p = _row_weights(row_weights, dev, T, rows, h)
+    q, scales, ldq, lds = _row_blocks(out, rows, two // 2, T.e4m3, T, h)
+    rc = lib().ew_swiglu_scaled(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, two // 2, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    if rc:
+        _check(rc, "ew_swiglu_scaled")
+    return q, scales
+
+
+def _norm_operands(x, weight, residual, T, dev, where):
+    if (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)) and T.recording():
+        _recorded(where)
+    code = _code(T, x.dtype)
+    rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
+    if not _good(weight, dev, x.dtype, 1) or weight.shape[0] != width or not weight.is_contiguous():
+        _on(weight, x, 1, "weight", x.dtype)
+        raise ValueError(f"weight: a contiguous tensor of {width} is wanted, got {tuple(weight.shape)}")
+    return code, rows, width, ldx
+
+
+def _like(t, shape, name, like):
+    """(tensor or None, address, elements between rows) of an operand that has x's shape and type."""
+    if t is None:
+        return None, 0
+    rows, width, ld = _matrix(t, like.get_device(), like.dtype, name, like)
+    if (rows, width) != shape:
+        raise ValueError(f"{name}: {shape} is wanted, got {tuple(t.shape)}")
+    return t.data_ptr(), ld
+
+
+def _norm(where, x, weight, residual, eps, y, with_y, blocks, with_blocks, sum_out):
+    T, dev = _torch(), x.get_device()
+    code, rows, width, ldx = _norm_operands(x, weight, residual, T, dev, where)
+    shape = (rows, width)
+    res, ldr = _like(residual, shape, "residual", x)
+    total, got = None, []
+    if residual is not None:
+        total = _result(sum_out, shape, x.dtype, x, "sum_out")
+    elif sum_out is not None:
+        raise ValueError("sum_out is for the sum with a residual")
+    q = scales = None
+    ldq = lds = 0
+    if with_blocks:
+        q, scales, ldq, lds = _row_blocks(blocks, rows, width, T.e4m3, T, x)
+        got += [q, scales]
+    if with_y:
+        y = _result(y, shape, x.dtype, x)
+        got.append(y)
+    if total is not None:
+        got.append(total)
+    many = rows > 1
+    rc = lib().ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width,
+                           None if total is None else total.data_ptr(), 0 if total is None else total.stride(0) if many else ldr,
+                           y.data_ptr() if with_y else None, (y.stride(0) if many else _room(width, 8)) if with_y else 0,
+                           None if q is None else q.data_ptr(), ldq, None if scales is None else scales.data_ptr(), lds, T.stream(dev))
+    if rc:
+        _check(rc, where)
+    return got[0] if len(got) == 1 else tuple(got)
+
+
+def rms_norm(x, weight, residual=None, eps=1e-6, out=None, sum_out=None):
+    """t / sqrt(mean(t^2) + eps) * weight of each row, t = x + residual rounded to their type (or x): y, or (y, t) with a residual.
+    x, residual [rows, width] and weight [width] bf16 or fp16.  sum_out: where t goes; it may be the residual itself."""
+    return _norm("ew_rms_norm", x, weight, residual, eps, out, True, None, False, sum_out)
+
+
+def rms_norm_scaled(x, weight, residual=None, eps=1e-6, with_y=False, out=None, sum_out=None):
+    """`rms_norm` with its result as 8-bit blocks of rows: (q float8_e4m3fn, scales), then y in 16 bits if asked for with_y (for a router,
+    say), then t with a residual.  out: (q, scales), or (q, scales, y)."""
+    if out is not None and len(out) != (3 if with_y else 2):
+        raise ValueError("out: (q, scales), and y if it is wanted")
+    return _norm("ew_rms_norm", x, weight, residual, eps, out[2] if out is not None and with_y else None, with_y, None if out is None else out[:2], True, sum_out)
+
+
+def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
+    """The gradient of `rms_norm` (and, for the blocks' values, of `rms_norm_scaled`) from dy and t, the normed stream (x, or its sum with
+    the residual): (dt [rows, width], the gradient of x and of the residual each, dweight float32 [width]).  dt: the
+    gradient that reaches t past the norm, added in."""
+    T, dev = _torch(), t.get_device()
+    if dy.requires_grad and T.recording() or (dt is not None and dt.requires_grad and T.recording()):
+        _recorded("ew_rms_norm_grad")
+    code, rows, width, ldt = _norm_operands(t, weight, None, T, dev, "ew_rms_norm_grad")
+    shape = (rows, width)
+    dy_at, lddy = _like(dy, shape, "dy", t)
+    dt_at, lddt = _like(dt, shape, "dt", t)
+    out = _result(out, shape, t.dtype, t)
+    dw = t.new_empty((width,), dtype=T.float32)
+    room = t.new_empty((lib().ew_rms_norm_grad_parts(rows, width), width), dtype=T.float32)
+    rc = lib().ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(),
+                                out.stride(0) if rows > 1 else _room(width, 8), dw.data_ptr(), room.data_ptr(), T.stream(dev))
+    if rc:
+        _check(rc, "ew_rms_norm_grad")
+    return out, dw
 
 
 def last_operator_error(device: int = 0) -> int:

@@ -1,0 +1,128 @@
+// 8-bit floating point in blocks of 128: the form that the scaled products read and the operators before them write.
+//
+// A block is 128 values q in e4m3 or e5m2 and one exponent byte c (e8m0), and stands for q 2^(c - 127).  c is the smallest, from 0
+// on, for which the block's largest finite value fits the type (448 or 57344, both 1.75 times a power of two):
+//     c = max(0, E - top + [mantissa of the largest above 1.75]),   E its biased exponent, top = 8 or 15
+// which is integer arithmetic on its bits.  A scale that is a power of two costs the values nothing but range: q is the value
+// rounded once, to nearest even, as if the type had no smallest exponent (but below 2^-9 of the block's largest, where e4m3 runs
+// out of exponents).  An infinity or NaN becomes the NaN of the type and takes no part in its block's scale.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <cstdint>
+
+#include "../../include/expertweave.h"
+
+namespace ew {
+namespace ops {
+namespace blocks {
+
+constexpr int kBlock = 128;
+constexpr int kSpan = 256;                             // values a warp works on at a time: eight a lane, two blocks
+constexpr unsigned kAll = 0xffffffffu;
+
+template <class T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <class T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
+
+template <class T> struct alignas(16) Eight { T v[8]; };
+
+template <bool E5M2> constexpr int kTop = E5M2 ? 15 : 8;
+__device__ __forceinline__ uint32_t scale_code(float most, int top) {
+    return (uint32_t)max((int)((__float_as_uint(most) + 0x1fffffu) >> 23) - top, 0);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t code) { return __uint_as_float((254u - code) << 23); }      // 2^(127 - code)
+
+template <bool E5M2>
+__device__ __forceinline__ uint32_t two_values(float lo, float hi) {
+    return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
+}
+__device__ __forceinline__ bool not_finite(float v) { return !(fabsf(v) <= 3.402823466e38f); }
+
+// Where a lane's eight values of a span lie.  VEC: side by side, so that they move in one access (rows on 16-byte boundaries);
+// otherwise 32 apart, so that a warp's accesses of single values are whole sectors all the same.
+template <bool VEC> __device__ __forceinline__ int place(int lane, int j) { return VEC ? lane * 8 + j : lane + 32 * j; }
+
+template <class T, bool VEC>
+__device__ __forceinline__ void load_span(Eight<T> &o, const T *row, int at, int lane, int width) {
+    if (VEC && at + lane * 8 + 8 <= width) {
+        o = *reinterpret_cast<const Eight<T> *>(row + at + lane * 8);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int i = at + place<VEC>(lane, j);
+        o.v[j] = i < width ? row[i] : from_f<T>(0.f);
+    }
+}
+template <class T, bool VEC>
+__device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, int lane, int width) {
+    if (VEC && at + lane * 8 + 8 <= width) {
+        *reinterpret_cast<Eight<T> *>(row + at + lane * 8) = o;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int i = at + place<VEC>(lane, j);
+        if (i < width) row[i] = o.v[j];
+    }
+}
+
+// Writes a span, whose values behind `width` are zeros, as two blocks.  The whole warp calls it.
+template <bool VEC, bool E5M2>
+__device__ __forceinline__ void put_span(float (&v)[8], uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
+    constexpr int kFirst = VEC ? 8 : 4;                // of the lane's values, those of its first block
+    float m0, m1;
+    auto most = [&] {
+        m0 = m1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < kFirst; ++j) m0 = fmaxf(m0, fabsf(v[j]));        // (a NaN is passed over)
+#pragma unroll
+        for (int j = kFirst; j < 8; ++j) m1 = fmaxf(m1, fabsf(v[j]));
+#pragma unroll
+        for (int d = VEC ? 8 : 16; d; d >>= 1) {
+            m0 = fmaxf(m0, __shfl_xor_sync(kAll, m0, d));
+            if (!VEC) m1 = fmaxf(m1, __shfl_xor_sync(kAll, m1, d));
+        }
+    };
+    most();
+    if (__any_sync(kAll, not_finite(m0) || not_finite(m1))) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (not_finite(v[j])) v[j] = __int_as_float(0x7fffffff);
+        most();
+    }
+    const uint32_t c0 = scale_code(m0, kTop<E5M2>), c1 = VEC ? c0 : scale_code(m1, kTop<E5M2>);
+    const float i0 = inverse_scale(c0), i1 = VEC ? i0 : inverse_scale(c1);
+    uint32_t pair[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float f = 2 * j < kFirst ? i0 : i1;
+        pair[j] = two_values<E5M2>(v[2 * j] * f, v[2 * j + 1] * f);
+    }
+    if (VEC && at + lane * 8 + 8 <= width) {
+        *reinterpret_cast<uint2 *>(q_row + at + lane * 8) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = at + place<VEC>(lane, j);
+            if (i < width) q_row[i] = (uint8_t)(pair[j >> 1] >> (8 * (j & 1)));
+        }
+    }
+    uint8_t *s = scale_row + at / kBlock;
+    if (VEC) {
+        if ((lane & 15) == 0 && at + lane * 8 < width) s[lane >> 4] = (uint8_t)c0;
+    } else if (lane == 0) {
+        s[0] = (uint8_t)c0;
+        if (at + kBlock < width) s[1] = (uint8_t)c1;
+    }
+}
+
+}  // namespace blocks
+}  // namespace ops
+}  // namespace ew

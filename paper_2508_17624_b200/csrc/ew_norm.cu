@@ -1,0 +1,310 @@
+// RMS norm with the residual's addition, its result in 16 bits, in 8-bit blocks or in both, and its gradient.
+//
+//   t = x + residual, rounded to their type (the stream as it is kept: the norm and its gradient are of that)
+//   y = t r w,   r = 1 / sqrt(mean(t^2) + eps)                                  of a row
+//   dt = r (g - u mean(g u)) + dt_in,   g = dy w, u = t r;     dw = sum over the rows of dy u
+//
+// Bound by HBM: forward 2 to 4 bytes of operands and 1 to 5 of results a value, backward 6 or 8, each read or written once: a row
+// stays in the registers of a warp (or of 8 or 16, for wide rows and few) between the sum and its use.  The weight's gradient
+// is summed in the registers of the threads that own its columns, over all rows that a CTA meets; a second kernel adds the
+// CTAs' sums up, in the same order every time.
+#include "ew_blocks.cuh"
+#include "ew_ops.h"
+#include "ew_tc.cuh"
+
+namespace ew {
+namespace ops {
+namespace {
+using namespace blocks;
+
+constexpr int kThreads = 256;
+constexpr int kMostWidth = 16384;                      // sixteen warps with four spans each
+template <int W> constexpr int kThreadsOf = W * 32 > kThreads ? W * 32 : kThreads;
+
+struct Args {
+    const void *x, *residual, *weight;
+    void *sum, *y;
+    uint8_t *q, *scales;
+    long long ldx, ldr, ldsum, ldy, ldq, lds, rows;
+    int width;
+    float inv_width, eps;
+};
+
+// The sum over the W warps of a row, in every thread of them.  `turn`: of the calls, so that one barrier a call is enough.
+template <int W, int N>
+__device__ __forceinline__ void add_up(float (&v)[N], int turn) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(kAll, v[i], d);
+    if (W == 1) return;
+    __shared__ float part[2][N][W];
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[turn & 1][i][threadIdx.x >> 5] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[i] += part[turn & 1][i][w];
+    }
+}
+
+// W warps a row, NV spans a warp
+template <class T, bool VEC, int W, int NV>
+__global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    constexpr int kRows = kThreadsOf<W> / 32 / W;
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W;
+    int turn = 0;
+    for (long long r = (long long)blockIdx.x * kRows + (threadIdx.x >> 5) / W; r < a.rows; r += (long long)gridDim.x * kRows) {
+        Eight<T> t[NV];
+        {
+            Eight<T> more[NV];
+            const T *x = reinterpret_cast<const T *>(a.x) + r * a.ldx, *res = reinterpret_cast<const T *>(a.residual) + r * a.ldr;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((i * W + w) * kSpan < a.width) {
+                    load_span<T, VEC>(t[i], x, (i * W + w) * kSpan, lane, a.width);
+                    if (a.residual) load_span<T, VEC>(more[i], res, (i * W + w) * kSpan, lane, a.width);
+                }
+            if (a.residual) {
+                T *sum = reinterpret_cast<T *>(a.sum) + r * a.ldsum;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if ((i * W + w) * kSpan < a.width) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) t[i].v[j] = from_f<T>(to_f(t[i].v[j]) + to_f(more[i].v[j]));
+                        store_span<T, VEC>(t[i], sum, (i * W + w) * kSpan, lane, a.width);
+                    }
+            }
+        }
+        float ss[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * W + w) * kSpan < a.width)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss[0] += to_f(t[i].v[j]) * to_f(t[i].v[j]);
+        add_up<W, 1>(ss, turn++);
+        const float norm = rsqrtf(ss[0] * a.inv_width + a.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = (i * W + w) * kSpan;
+            if (at < a.width) {
+                Eight<T> weight, y;
+                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), at, lane, a.width);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = to_f(t[i].v[j]) * norm * to_f(weight.v[j]);
+                    y.v[j] = from_f<T>(v[j]);
+                }
+                if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
+                if (a.q) put_span<VEC, false>(v, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
+            }
+        }
+    }
+}
+
+struct GradArgs {
+    const void *dy, *t, *weight, *more;
+    void *dt;
+    float *parts;                                      // [gridDim.x, width]: each CTA's sums for dw
+    long long lddy, ldt, ldmore, lddt, rows;
+    int width;
+    float inv_width, eps;
+};
+
+template <class T, bool VEC, int W, int NV>
+__global__ void __launch_bounds__(kThreadsOf<W>) grad_kernel(const GradArgs a) {
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    static_assert(W >= 8, "a row is a CTA's: a column has one thread");
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    float dw[NV][8] = {};
+    int turn = 0;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        Eight<T> dy[NV], t[NV], more[NV];
+        const T *dy_row = reinterpret_cast<const T *>(a.dy) + r * a.lddy, *t_row = reinterpret_cast<const T *>(a.t) + r * a.ldt;
+        const T *more_row = reinterpret_cast<const T *>(a.more) + r * a.ldmore;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * W + w) * kSpan < a.width) {
+                load_span<T, VEC>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
+                load_span<T, VEC>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
+                if (a.more) load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
+            }
+        float sums[2] = {0.f, 0.f};                    // of t^2 and of dy w t
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * W + w) * kSpan < a.width) {
+                Eight<T> weight;
+                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float tf = to_f(t[i].v[j]);
+                    sums[0] += tf * tf;
+                    sums[1] += to_f(dy[i].v[j]) * to_f(weight.v[j]) * tf;
+                }
+            }
+        add_up<W, 2>(sums, turn++);
+        const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);      // mean(g u) = norm mean(g t)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * W + w) * kSpan < a.width) {
+                Eight<T> weight, dt;
+                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float tf = to_f(t[i].v[j]), df = to_f(dy[i].v[j]);
+                    float v = norm * (df * to_f(weight.v[j]) - tf * along);
+                    if (a.more) v += to_f(more[i].v[j]);
+                    dt.v[j] = from_f<T>(v);
+                    dw[i][j] += df * (tf * norm);
+                }
+                store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
+            }
+    }
+    float *parts = a.parts + (long long)blockIdx.x * a.width;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = (i * W + w) * kSpan + place<VEC>(lane, j);
+            if (c < a.width) parts[c] = dw[i][j];
+        }
+}
+
+// dw[c] = the sum of parts[:, c]: 32 columns a CTA, 32 threads a column
+__global__ void __launch_bounds__(1024) parts_kernel(const float *parts, float *dw, int n_parts, int width) {
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float v = 0.f;
+    if (c < width)
+#pragma unroll 8
+        for (int p = warp; p < n_parts; p += 32) v += parts[(long long)p * width + c];
+    sums[warp][lane] = v;
+    __syncthreads();
+    v = sums[lane][warp];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
+    if (lane == 0 && blockIdx.x * 32 + warp < width) dw[blockIdx.x * 32 + warp] = v;
+}
+
+// Rows that a CTA meets are at most this much apart: the CTAs of the gradient, whose sums are the workspace.
+constexpr int kMostParts = 592;
+
+template <class T, bool VEC, int W, int NV>
+ew_status_t launch(const Args &a, cudaStream_t st) {
+    constexpr int kRows = kThreadsOf<W> / 32 / W;
+    const long long ctas = (a.rows + kRows - 1) / kRows, most = 0x7fffffff;
+    return launched(launch_pdl(norm_kernel<T, VEC, W, NV>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kThreadsOf<W>), 0, st, a), "RMS norm");
+}
+
+template <class T, bool VEC>
+ew_status_t pick(const Device &d, const Args &a, cudaStream_t st) {
+    if (a.width <= 2048 && a.rows >= (long long)d.sm_count * 8)
+        return a.width <= 512 ? launch<T, VEC, 1, 2>(a, st) : a.width <= 1024 ? launch<T, VEC, 1, 4>(a, st) : launch<T, VEC, 1, 8>(a, st);
+    if (a.width <= 2048) return launch<T, VEC, 8, 1>(a, st);
+    if (a.width <= 4096) return launch<T, VEC, 8, 2>(a, st);
+    if (a.width <= 8192) return launch<T, VEC, 8, 4>(a, st);
+    return launch<T, VEC, 16, 4>(a, st);
+}
+
+template <class T, bool VEC, int W, int NV>
+ew_status_t launch_grad(const GradArgs &a, int parts, float *dw, cudaStream_t st) {
+    const ew_status_t s = launched(launch_pdl(grad_kernel<T, VEC, W, NV>, dim3((unsigned)parts), dim3(kThreadsOf<W>), 0, st, a), "RMS norm gradient");
+    if (s != EW_OK) return s;
+    return launched(launch_pdl(parts_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(1024), 0, st, (const float *)a.parts, dw, parts, a.width), "RMS norm gradient");
+}
+
+template <class T, bool VEC>
+ew_status_t pick_grad(const GradArgs &a, int parts, float *dw, cudaStream_t st) {
+    if (a.width <= 2048) return launch_grad<T, VEC, 8, 1>(a, parts, dw, st);
+    if (a.width <= 4096) return launch_grad<T, VEC, 8, 2>(a, parts, dw, st);
+    if (a.width <= 8192) return launch_grad<T, VEC, 8, 4>(a, parts, dw, st);
+    return launch_grad<T, VEC, 16, 4>(a, parts, dw, st);
+}
+
+template <class T, bool VEC>
+int load_one() {
+    cudaFuncAttributes fa;
+    return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 4>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 8>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 1>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 1>) |
+           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 2>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 4>) |
+           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 16, 4>) | (int)cudaFuncGetAttributes(&fa, parts_kernel);
+}
+
+bool bad_eps(float eps) { return !(eps >= 0.f && eps <= 3.402823466e38f); }
+
+}  // namespace
+
+// Loads the kernels (a first launch inside a graph capture would have to).
+int norm_setup() {
+    return load_one<__nv_bfloat16, false>() | load_one<__nv_bfloat16, true>() | load_one<__half, false>() | load_one<__half, true>();
+}
+
+}  // namespace ops
+}  // namespace ew
+
+using namespace ew;
+using namespace ew::ops;
+
+extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight, float eps,
+                                   int32_t rows, int32_t width, void *sum, int64_t ldsum, void *y, int64_t ldy, void *q, int64_t ldq, void *scales,
+                                   int64_t ldscales, void *cuda_stream) {
+    if (!is_16bit(dtype)) return refuse("RMS norm: bf16 or fp16");
+    if (rows < 0 || width < 1 || width > kMostWidth || bad_eps(eps)) return refuse("RMS norm: size or eps out of range");
+    if (!y && !q && rows > 0) return refuse("RMS norm: no result is wanted");
+    if (ldx < width || (residual && (ldres < width || ldsum < width)) || (y && ldy < width) || (q && (ldq < width || ldscales < (width + blocks::kBlock - 1) / blocks::kBlock)))
+        return refuse("RMS norm: rows overlap");
+    if (rows > 0 && (!x || !weight || (residual && !sum) || (q && !scales) || (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)weight | (uintptr_t)sum | (uintptr_t)y) & 1)))
+        return refuse("RMS norm: null or misaligned pointer");
+    if (device < 0) return EW_ERR_NO_DEVICE;
+    if (rows == 0) return EW_OK;
+    DeviceGuard guard;
+    ew_status_t s = launched((int)guard.enter(device), "cudaSetDevice");
+    const Device *d;
+    if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
+    const Args a = {x, residual, weight, residual ? sum : nullptr, y, (uint8_t *)q, (uint8_t *)scales, ldx, residual ? ldres : 0, residual ? ldsum : 0, y ? ldy : 0, q ? ldq : 0,
+                    q ? ldscales : 0, rows, width, (float)(1.0 / width), eps};
+    const bool vec = !((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)weight | (uintptr_t)a.sum | (uintptr_t)y) & 15) | ((uintptr_t)q & 7) |
+                       ((a.ldx | a.ldr | a.ldsum | a.ldy | a.ldq) & 7));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == EW_BF16) return vec ? pick<__nv_bfloat16, true>(*d, a, st) : pick<__nv_bfloat16, false>(*d, a, st);
+    return vec ? pick<__half, true>(*d, a, st) : pick<__half, false>(*d, a, st);
+}
+
+extern "C" int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width) {
+    (void)width;
+    return rows < 1 ? 0 : rows < kMostParts ? rows : kMostParts;
+}
+
+extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight, const void *dt_in,
+                                        int64_t lddt_in, float eps, int32_t rows, int32_t width, void *dt, int64_t lddt, float *dweight, float *workspace,
+                                        void *cuda_stream) {
+    if (!is_16bit(dtype)) return refuse("RMS norm: bf16 or fp16");
+    if (rows < 0 || width < 1 || width > kMostWidth || bad_eps(eps)) return refuse("RMS norm: size or eps out of range");
+    if (lddy < width || ldt < width || (dt_in && lddt_in < width) || lddt < width) return refuse("RMS norm: rows overlap");
+    if (!dweight || ((uintptr_t)dweight & 3) ||
+        (rows > 0 && (!dy || !t || !weight || !dt || !workspace || ((uintptr_t)workspace & 3) || (((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 1))))
+        return refuse("RMS norm: null or misaligned pointer");
+    if (device < 0) return EW_ERR_NO_DEVICE;
+    DeviceGuard guard;
+    ew_status_t s = launched((int)guard.enter(device), "cudaSetDevice");
+    const Device *d;
+    if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (rows == 0) return launched((int)cudaMemsetAsync(dweight, 0, (size_t)width * 4, st), "cudaMemsetAsync");
+    const GradArgs a = {dy, t, weight, dt_in, dt, workspace, lddy, ldt, dt_in ? lddt_in : 0, lddt, rows, width, (float)(1.0 / width), eps};
+    const bool vec = !((((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 15) | ((a.lddy | a.ldt | a.ldmore | a.lddt) & 7));
+    const int parts = ew_rms_norm_grad_parts(rows, width);
+    if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(a, parts, dweight, st) : pick_grad<__nv_bfloat16, false>(a, parts, dweight, st);
+    return vec ? pick_grad<__half, true>(a, parts, dweight, st) : pick_grad<__half, false>(a, parts, dweight, st);
+}

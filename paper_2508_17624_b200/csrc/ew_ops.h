@@ -1,4 +1,4 @@
-// Shared host side of the stand-alone operators (grouped products, 4-bit matrix-vector products, SwiGLU): what they
+// Shared host side of the stand-alone operators (grouped products in 16 and 8 bits, 4-bit matrix-vector products, SwiGLU, RMS norm): what they
 // need to know of a device, argument checks, tensor maps.  These operators take no pool: everything they work on is
 // passed in, and they keep nothing between calls but the constants of a device.
 #pragma once
@@ -21,6 +21,8 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
 // was given (an offset, a slot) lies outside its range and was clamped or skipped.
 constexpr int kErrBadIndex = 4;
 
+constexpr int kMostSlots = 2048;                       // matrices of stacked weights: what the group tables in shared memory hold
+
 struct Device {
     int sm_count = 0;
     int *err = nullptr;              // device address of the error word
@@ -37,8 +39,12 @@ ew_status_t take_error(const Device &d, int *bits);
 int grouped_setup();
 int quant_setup();
 int swiglu_setup();
+int blocks_setup();
+int norm_setup();
+int scaled_setup();
 
 inline bool is_16bit(int dtype) { return dtype == EW_BF16 || dtype == EW_FP16; }
+inline bool is_8bit(int dtype) { return dtype == EW_E4M3 || dtype == EW_E5M2; }
 inline int elem_bytes(int dtype) { return dtype == EW_FP32 ? 4 : 2; }
 inline CUtensorMapDataType map_type(int dtype) {
     return dtype == EW_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
