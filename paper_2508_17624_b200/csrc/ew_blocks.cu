@@ -40,21 +40,20 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
             Eight<T> g[kAhead], u[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const int at = from + k * W * kSpan;
-                if (at < a.width) {
-                    load_span<T, VEC>(g[k], row, at, lane, a.width);
-                    if (ACT) load_span<T, VEC>(u[k], row + a.width, at, lane, a.width);
-                }
+                load_span<T, VEC>(g[k], row, from + k * W * kSpan, lane, a.width);
+                if (ACT) load_span<T, VEC>(u[k], row + a.width, from + k * W * kSpan, lane, a.width);
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int at = from + k * W * kSpan;
                 if (at < a.width) {
                     float v[8];
+                    span_values<T, VEC>(v, g[k], at, lane, a.width);
+                    if (ACT) {
+                        float up[8];
+                        span_values<T, VEC>(up, u[k], at, lane, a.width);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[j] = to_f(g[k].v[j]);
-                        if (ACT) v[j] = v[j] * __fdividef(1.f, 1.f + __expf(-v[j])) * to_f(u[k].v[j]) * p;
+                        for (int j = 0; j < 8; ++j) v[j] = v[j] * __fdividef(1.f, 1.f + __expf(-v[j])) * up[j] * p;
                     }
                     put_span<VEC, E5M2>(v, q, scales, at, lane, a.width);
                 }
@@ -84,16 +83,15 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
     // the row and column of a thread's value j of step i
     auto row_of = [&](int i, int j) { return bn * kBlock + (VEC ? i * 16 + (t >> 4) : (i * 8 + j) * 2 + (t >> 7)); };
     auto col_of = [&](int j) { return bk * kBlock + (VEC ? (t & 15) * 8 + j : t & 127); };
-    const bool whole = VEC && col_of(0) + 8 <= a.k;
-    Eight<T> raw[8];
+    const bool col_ok = col_of(0) < a.k;               // VEC: k is a multiple of eight
+    Eight<T> raw[8];                                   // (what lies behind the edges reads what lies before them, without a branch, and counts as zeros)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if (whole) {
-            if (row_of(i, 0) < a.n) raw[i] = *reinterpret_cast<const Eight<T> *>(w + row_of(i, 0) * a.ldw + col_of(0));
-            else raw[i] = {};
+        if constexpr (VEC) {
+            *reinterpret_cast<uint4 *>(&raw[i]) = *reinterpret_cast<const uint4 *>(w + min(row_of(i, 0), a.n - 1) * a.ldw + min(col_of(0), a.k - 8));
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) raw[i].v[j] = row_of(i, j) < a.n && col_of(j) < a.k ? w[row_of(i, j) * a.ldw + col_of(j)] : from_f<T>(0.f);
+            for (int j = 0; j < 8; ++j) raw[i].v[j] = w[min(row_of(i, j), a.n - 1) * a.ldw + min(col_of(j), a.k - 1)];
         }
     }
     auto find = [&] {
@@ -108,7 +106,7 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
         for (int i = 0; i < kThreads / 32; ++i) most = fmaxf(most, part[i]);
     };
 #pragma unroll
-    for (int i = 0; i < 64; ++i) v[i >> 3][i & 7] = to_f(raw[i >> 3].v[i & 7]);
+    for (int i = 0; i < 64; ++i) v[i >> 3][i & 7] = row_of(i >> 3, VEC ? 0 : i & 7) < a.n && col_of(VEC ? 0 : i & 7) < a.k ? to_f(raw[i >> 3].v[i & 7]) : 0.f;
     find();
     if (not_finite(most)) {                            // the same in every thread
 #pragma unroll
@@ -125,8 +123,8 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
         uint32_t pair[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) pair[j] = two_values<false>(v[i][2 * j] * f, v[i][2 * j + 1] * f);
-        if (whole) {
-            if (row_of(i, 0) < a.n) *reinterpret_cast<uint2 *>(q + row_of(i, 0) * a.ldq + col_of(0)) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+        if constexpr (VEC) {
+            if (col_ok && row_of(i, 0) < a.n) *reinterpret_cast<uint2 *>(q + row_of(i, 0) * a.ldq + col_of(0)) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -160,7 +158,7 @@ ew_status_t to_rows(bool act, int32_t device, int32_t dtype, int32_t q_type, con
     const Device *d;
     if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
     const RowArgs a = {x, p, (uint8_t *)q, (uint8_t *)scales, ldx, ldq, lds, rows, width};
-    const bool vec = !(((uintptr_t)x & 15) | ((uintptr_t)q & 7) | ((ldx | ldq | (act ? width : 0)) & 7));
+    const bool vec = !(((uintptr_t)x & 15) | ((uintptr_t)q & 7) | ((ldx | ldq | width) & 7));
     cudaStream_t st = (cudaStream_t)stream;
 #define EW_PICK(T, ACT, E5M2) (vec ? launch_rows<T, ACT, E5M2, true>(*d, a, st) : launch_rows<T, ACT, E5M2, false>(*d, a, st))
     if (act) return dtype == EW_BF16 ? EW_PICK(__nv_bfloat16, true, false) : EW_PICK(__half, true, false);
@@ -215,7 +213,7 @@ extern "C" ew_status_t ew_scaled_pack(int32_t device, int32_t dtype, const void 
     const Device *d;
     if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
     const WeightArgs a = {w, (uint8_t *)q, (uint8_t *)scales, ldw, n_slots > 1 ? slot_stride : 0, ldq, n_slots > 1 ? q_stride : 0, n, k, (int)nb, (int)kb};
-    const bool vec = !(((uintptr_t)w & 15) | ((uintptr_t)q & 7) | ((a.ldw | a.w_stride | a.ldq | a.q_stride) & 7));
+    const bool vec = !(((uintptr_t)w & 15) | ((uintptr_t)q & 7) | ((a.ldw | a.w_stride | a.ldq | a.q_stride | k) & 7));
     const dim3 grid((unsigned)(nb * kb), (unsigned)n_slots);
     cudaStream_t st = (cudaStream_t)cuda_stream;
 #define EW_PICK(T) (vec ? launch_pdl(weights_kernel<T, true>, grid, dim3(kThreads), 0, st, a) : launch_pdl(weights_kernel<T, false>, grid, dim3(kThreads), 0, st, a))

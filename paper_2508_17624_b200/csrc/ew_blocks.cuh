@@ -44,32 +44,36 @@ __device__ __forceinline__ uint32_t two_values(float lo, float hi) {
 }
 __device__ __forceinline__ bool not_finite(float v) { return !(fabsf(v) <= 3.402823466e38f); }
 
-// Where a lane's eight values of a span lie.  VEC: side by side, so that they move in one access (rows on 16-byte boundaries);
-// otherwise 32 apart, so that a warp's accesses of single values are whole sectors all the same.
+// Where a lane's eight values of a span lie.  VEC: side by side, so that they move in one access (rows on 16-byte boundaries, of a
+// multiple of eight values); otherwise 32 apart, so that a warp's accesses of single values are whole sectors all the same.
 template <bool VEC> __device__ __forceinline__ int place(int lane, int j) { return VEC ? lane * 8 + j : lane + 32 * j; }
 
+// Loading has no branch: a place behind the row's end reads its last values instead, and span_values() makes zeros of them.  (With a
+// branch around each access the compiler waits for one before it begins the next: the norm of 8192 rows took 90 us, SwiGLU of 49152 206.)
 template <class T, bool VEC>
 __device__ __forceinline__ void load_span(Eight<T> &o, const T *row, int at, int lane, int width) {
-    if (VEC && at + lane * 8 + 8 <= width) {
-        o = *reinterpret_cast<const Eight<T> *>(row + at + lane * 8);
-        return;
-    }
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4 *>(&o) = *reinterpret_cast<const uint4 *>(row + min(at + lane * 8, width - 8));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int i = at + place<VEC>(lane, j);
-        o.v[j] = i < width ? row[i] : from_f<T>(0.f);
+        for (int j = 0; j < 8; ++j) o.v[j] = row[min(at + lane + 32 * j, width - 1)];
     }
 }
 template <class T, bool VEC>
-__device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, int lane, int width) {
-    if (VEC && at + lane * 8 + 8 <= width) {
-        *reinterpret_cast<Eight<T> *>(row + at + lane * 8) = o;
-        return;
-    }
+__device__ __forceinline__ void span_values(float (&v)[8], const Eight<T> &o, int at, int lane, int width) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int i = at + place<VEC>(lane, j);
-        if (i < width) row[i] = o.v[j];
+    for (int j = 0; j < 8; ++j) v[j] = at + place<VEC>(lane, VEC ? 0 : j) < width ? to_f(o.v[j]) : 0.f;
+}
+template <class T, bool VEC>
+__device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, int lane, int width) {
+    if constexpr (VEC) {
+        if (at + lane * 8 < width) *reinterpret_cast<Eight<T> *>(row + at + lane * 8) = o;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = at + place<VEC>(lane, j);
+            if (i < width) row[i] = o.v[j];
+        }
     }
 }
 
@@ -105,8 +109,8 @@ __device__ __forceinline__ void put_span(float (&v)[8], uint8_t *q_row, uint8_t 
         const float f = 2 * j < kFirst ? i0 : i1;
         pair[j] = two_values<E5M2>(v[2 * j] * f, v[2 * j + 1] * f);
     }
-    if (VEC && at + lane * 8 + 8 <= width) {
-        *reinterpret_cast<uint2 *>(q_row + at + lane * 8) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+    if constexpr (VEC) {
+        if (at + lane * 8 < width) *reinterpret_cast<uint2 *>(q_row + at + lane * 8) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

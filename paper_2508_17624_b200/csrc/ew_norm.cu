@@ -63,47 +63,45 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
         Eight<T> t[NV];
         {
             Eight<T> more[NV];
-            const T *x = reinterpret_cast<const T *>(a.x) + r * a.ldx, *res = reinterpret_cast<const T *>(a.residual) + r * a.ldr;
+            const T *x = reinterpret_cast<const T *>(a.x) + r * a.ldx, *res = a.residual ? reinterpret_cast<const T *>(a.residual) + r * a.ldr : x;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if ((i * W + w) * kSpan < a.width) {
-                    load_span<T, VEC>(t[i], x, (i * W + w) * kSpan, lane, a.width);
-                    if (a.residual) load_span<T, VEC>(more[i], res, (i * W + w) * kSpan, lane, a.width);
-                }
+            for (int i = 0; i < NV; ++i) load_span<T, VEC>(t[i], x, (i * W + w) * kSpan, lane, a.width);
             if (a.residual) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) load_span<T, VEC>(more[i], res, (i * W + w) * kSpan, lane, a.width);
                 T *sum = reinterpret_cast<T *>(a.sum) + r * a.ldsum;
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if ((i * W + w) * kSpan < a.width) {
+                for (int i = 0; i < NV; ++i) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) t[i].v[j] = from_f<T>(to_f(t[i].v[j]) + to_f(more[i].v[j]));
-                        store_span<T, VEC>(t[i], sum, (i * W + w) * kSpan, lane, a.width);
-                    }
+                    for (int j = 0; j < 8; ++j) t[i].v[j] = from_f<T>(to_f(t[i].v[j]) + to_f(more[i].v[j]));
+                    store_span<T, VEC>(t[i], sum, (i * W + w) * kSpan, lane, a.width);
+                }
             }
         }
         float ss[1] = {0.f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((i * W + w) * kSpan < a.width)
+        for (int i = 0; i < NV; ++i) {
+            float v[8];
+            span_values<T, VEC>(v, t[i], (i * W + w) * kSpan, lane, a.width);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss[0] += to_f(t[i].v[j]) * to_f(t[i].v[j]);
+            for (int j = 0; j < 8; ++j) ss[0] += v[j] * v[j];
+        }
         add_up<W, 1>(ss, turn++);
         const float norm = rsqrtf(ss[0] * a.inv_width + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = (i * W + w) * kSpan;
-            if (at < a.width) {
-                Eight<T> weight, y;
-                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), at, lane, a.width);
-                float v[8];
+            Eight<T> weight, y;
+            load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), at, lane, a.width);
+            float v[8];
+            span_values<T, VEC>(v, t[i], at, lane, a.width);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[j] = to_f(t[i].v[j]) * norm * to_f(weight.v[j]);
-                    y.v[j] = from_f<T>(v[j]);
-                }
-                if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
-                if (a.q) put_span<VEC, false>(v, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
+            for (int j = 0; j < 8; ++j) {
+                v[j] = v[j] * norm * to_f(weight.v[j]);
+                y.v[j] = from_f<T>(v[j]);
             }
+            if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
+            if (a.q && at < a.width) put_span<VEC, false>(v, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
         }
     }
 }
@@ -130,42 +128,42 @@ __global__ void __launch_bounds__(kThreadsOf<W>) grad_kernel(const GradArgs a) {
         const T *dy_row = reinterpret_cast<const T *>(a.dy) + r * a.lddy, *t_row = reinterpret_cast<const T *>(a.t) + r * a.ldt;
         const T *more_row = reinterpret_cast<const T *>(a.more) + r * a.ldmore;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((i * W + w) * kSpan < a.width) {
-                load_span<T, VEC>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
-                load_span<T, VEC>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
-                if (a.more) load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
-            }
+        for (int i = 0; i < NV; ++i) {
+            load_span<T, VEC>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
+            load_span<T, VEC>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
+        }
+        if (a.more)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
         float sums[2] = {0.f, 0.f};                    // of t^2 and of dy w t
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((i * W + w) * kSpan < a.width) {
-                Eight<T> weight;
-                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+        for (int i = 0; i < NV; ++i) {
+            Eight<T> weight;
+            load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+            float v[8];
+            span_values<T, VEC>(v, t[i], (i * W + w) * kSpan, lane, a.width);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float tf = to_f(t[i].v[j]);
-                    sums[0] += tf * tf;
-                    sums[1] += to_f(dy[i].v[j]) * to_f(weight.v[j]) * tf;
-                }
+            for (int j = 0; j < 8; ++j) {
+                sums[0] += v[j] * v[j];
+                sums[1] += to_f(dy[i].v[j]) * to_f(weight.v[j]) * v[j];
             }
+        }
         add_up<W, 2>(sums, turn++);
         const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);      // mean(g u) = norm mean(g t)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((i * W + w) * kSpan < a.width) {
-                Eight<T> weight, dt;
-                load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+        for (int i = 0; i < NV; ++i) {
+            Eight<T> weight, dt;
+            load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float tf = to_f(t[i].v[j]), df = to_f(dy[i].v[j]);
-                    float v = norm * (df * to_f(weight.v[j]) - tf * along);
-                    if (a.more) v += to_f(more[i].v[j]);
-                    dt.v[j] = from_f<T>(v);
-                    dw[i][j] += df * (tf * norm);
-                }
-                store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
+            for (int j = 0; j < 8; ++j) {
+                const float tf = to_f(t[i].v[j]), df = to_f(dy[i].v[j]);
+                float v = norm * (df * to_f(weight.v[j]) - tf * along);
+                if (a.more) v += to_f(more[i].v[j]);
+                dt.v[j] = from_f<T>(v);
+                dw[i][j] += df * (tf * norm);
             }
+            store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
+        }
     }
     float *parts = a.parts + (long long)blockIdx.x * a.width;
 #pragma unroll
@@ -275,7 +273,7 @@ extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x,
     const Args a = {x, residual, weight, residual ? sum : nullptr, y, (uint8_t *)q, (uint8_t *)scales, ldx, residual ? ldres : 0, residual ? ldsum : 0, y ? ldy : 0, q ? ldq : 0,
                     q ? ldscales : 0, rows, width, (float)(1.0 / width), eps};
     const bool vec = !((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)weight | (uintptr_t)a.sum | (uintptr_t)y) & 15) | ((uintptr_t)q & 7) |
-                       ((a.ldx | a.ldr | a.ldsum | a.ldy | a.ldq) & 7));
+                       ((a.ldx | a.ldr | a.ldsum | a.ldy | a.ldq | width) & 7));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == EW_BF16) return vec ? pick<__nv_bfloat16, true>(*d, a, st) : pick<__nv_bfloat16, false>(*d, a, st);
     return vec ? pick<__half, true>(*d, a, st) : pick<__half, false>(*d, a, st);
@@ -303,7 +301,7 @@ extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const voi
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (rows == 0) return launched((int)cudaMemsetAsync(dweight, 0, (size_t)width * 4, st), "cudaMemsetAsync");
     const GradArgs a = {dy, t, weight, dt_in, dt, workspace, lddy, ldt, dt_in ? lddt_in : 0, lddt, rows, width, (float)(1.0 / width), eps};
-    const bool vec = !((((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 15) | ((a.lddy | a.ldt | a.ldmore | a.lddt) & 7));
+    const bool vec = !((((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 15) | ((a.lddy | a.ldt | a.ldmore | a.lddt | width) & 7));
     const int parts = ew_rms_norm_grad_parts(rows, width);
     if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(a, parts, dweight, st) : pick_grad<__nv_bfloat16, false>(a, parts, dweight, st);
     return vec ? pick_grad<__half, true>(a, parts, dweight, st) : pick_grad<__half, false>(a, parts, dweight, st);
