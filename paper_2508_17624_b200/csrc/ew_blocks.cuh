@@ -56,7 +56,10 @@ __device__ __forceinline__ void load_span(Eight<T> &o, const T *row, int at, int
         *reinterpret_cast<uint4 *>(&o) = *reinterpret_cast<const uint4 *>(row + min(at + lane * 8, width - 8));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o.v[j] = row[min(at + lane + 32 * j, width - 1)];
+        for (int j = 0; j < 8; ++j) {
+            const int i = at + lane + 32 * j;
+            o.v[j] = i < width ? row[i] : from_f<T>(0.f);
+        }
     }
 }
 template <class T, bool VEC>

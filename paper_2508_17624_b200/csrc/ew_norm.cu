@@ -19,7 +19,7 @@ using namespace blocks;
 
 constexpr int kThreads = 256;
 constexpr int kMostWidth = 16384;                      // sixteen warps with four spans each
-template <int W> constexpr int kThreadsOf = W * 32 > kThreads ? W * 32 : kThreads;
+template <int W> constexpr int kThreadsOf = W == 1 ? kThreads : W * 32;     // several warps a row: a CTA a row
 
 struct Args {
     const void *x, *residual, *weight;
@@ -119,7 +119,7 @@ template <class T, bool VEC, int W, int NV>
 __global__ void __launch_bounds__(kThreadsOf<W>) grad_kernel(const GradArgs a) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
-    static_assert(W >= 8, "a row is a CTA's: a column has one thread");
+    static_assert(W > 1, "a row is a CTA's: a column has one thread");
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     float dw[NV][8] = {};
     int turn = 0;
@@ -204,11 +204,11 @@ ew_status_t launch(const Args &a, cudaStream_t st) {
 }
 
 template <class T, bool VEC>
-ew_status_t pick(const Device &d, const Args &a, cudaStream_t st) {
-    if (a.width <= 2048 && a.rows >= (long long)d.sm_count * 8)
-        return a.width <= 512 ? launch<T, VEC, 1, 2>(a, st) : a.width <= 1024 ? launch<T, VEC, 1, 4>(a, st) : launch<T, VEC, 1, 8>(a, st);
-    if (a.width <= 2048) return launch<T, VEC, 8, 1>(a, st);
-    if (a.width <= 4096) return launch<T, VEC, 8, 2>(a, st);
+ew_status_t pick(const Args &a, cudaStream_t st) {
+    if (a.width <= 512) return launch<T, VEC, 1, 2>(a, st);
+    if (a.width <= 1024) return launch<T, VEC, 4, 1>(a, st);
+    if (a.width <= 2048) return launch<T, VEC, 4, 2>(a, st);
+    if (a.width <= 4096) return launch<T, VEC, 4, 4>(a, st);
     if (a.width <= 8192) return launch<T, VEC, 8, 4>(a, st);
     return launch<T, VEC, 16, 4>(a, st);
 }
@@ -231,12 +231,12 @@ ew_status_t pick_grad(const GradArgs &a, int parts, float *dw, cudaStream_t st) 
 template <class T, bool VEC>
 int load_one() {
     cudaFuncAttributes fa;
-    return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 4>) |
-           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 8>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 1>) |
-           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) |
-           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 1>) |
-           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 2>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 4>) |
-           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 16, 4>) | (int)cudaFuncGetAttributes(&fa, parts_kernel);
+    return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 1>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 4>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) |
+           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 1>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 2>) |
+           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 16, 4>) |
+           (int)cudaFuncGetAttributes(&fa, parts_kernel);
 }
 
 bool bad_eps(float eps) { return !(eps >= 0.f && eps <= 3.402823466e38f); }
@@ -275,8 +275,8 @@ extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x,
     const bool vec = !((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)weight | (uintptr_t)a.sum | (uintptr_t)y) & 15) | ((uintptr_t)q & 7) |
                        ((a.ldx | a.ldr | a.ldsum | a.ldy | a.ldq | width) & 7));
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == EW_BF16) return vec ? pick<__nv_bfloat16, true>(*d, a, st) : pick<__nv_bfloat16, false>(*d, a, st);
-    return vec ? pick<__half, true>(*d, a, st) : pick<__half, false>(*d, a, st);
+    if (dtype == EW_BF16) return vec ? pick<__nv_bfloat16, true>(a, st) : pick<__nv_bfloat16, false>(a, st);
+    return vec ? pick<__half, true>(a, st) : pick<__half, false>(a, st);
 }
 
 extern "C" int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width) {
