@@ -30,7 +30,7 @@ template <class T, bool ACT, bool E5M2, bool VEC, int W>
 __global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
-    constexpr int kRows = kThreads / 32 / W, kAhead = W > 1 ? 1 : ACT ? 3 : 4;
+    constexpr int kRows = kThreads / 32 / W, kAhead = W > 1 ? 1 : !VEC ? 2 : ACT ? 3 : 4;
     const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W;
     for (long long r = (long long)blockIdx.x * kRows + (threadIdx.x >> 5) / W; r < a.rows; r += (long long)gridDim.x * kRows) {
         const T *row = reinterpret_cast<const T *>(a.x) + r * a.ldx;
@@ -48,14 +48,12 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
                 const int at = from + k * W * kSpan;
                 if (at < a.width) {
                     float v[8];
-                    span_values<T, VEC>(v, g[k], at, lane, a.width);
-                    if (ACT) {
-                        float up[8];
-                        span_values<T, VEC>(up, u[k], at, lane, a.width);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = v[j] * __fdividef(1.f, 1.f + __expf(-v[j])) * up[j] * p;
+                    for (int j = 0; j < 8; ++j) {
+                        v[j] = to_f(g[k].v[j]);
+                        if (ACT) v[j] = v[j] * __fdividef(1.f, 1.f + __expf(-v[j])) * to_f(u[k].v[j]);
                     }
-                    put_span<VEC, E5M2>(v, q, scales, at, lane, a.width);
+                    put_span<VEC, E5M2>(v, p, q, scales, at, lane, a.width);
                 }
             }
         }
@@ -71,33 +69,34 @@ struct WeightArgs {
 
 // A CTA a block of 128 x 128.  VEC: sixteen lanes a row of the block; otherwise 128.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
+__global__ void __launch_bounds__(kThreads, VEC ? 3 : 2) weights_kernel(const WeightArgs a) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     __shared__ float part[kThreads / 32];
     const int t = threadIdx.x, bk = blockIdx.x % a.kb, bn = blockIdx.x / a.kb;
     const T *w = reinterpret_cast<const T *>(a.w) + blockIdx.y * a.w_stride;
     uint8_t *q = a.q + blockIdx.y * a.q_stride;
-    float v[8][8];
-    float most = 0.f;
     // the row and column of a thread's value j of step i
     auto row_of = [&](int i, int j) { return bn * kBlock + (VEC ? i * 16 + (t >> 4) : (i * 8 + j) * 2 + (t >> 7)); };
     auto col_of = [&](int j) { return bk * kBlock + (VEC ? (t & 15) * 8 + j : t & 127); };
-    const bool col_ok = col_of(0) < a.k;               // VEC: k is a multiple of eight
-    Eight<T> raw[8];                                   // (what lies behind the edges reads what lies before them, without a branch, and counts as zeros)
+    Eight<T> raw[8];                                   // what lies behind an edge reads the block's last values once more, without a branch
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if constexpr (VEC) {
+        if constexpr (VEC) {                           // (k is a multiple of eight)
             *reinterpret_cast<uint4 *>(&raw[i]) = *reinterpret_cast<const uint4 *>(w + min(row_of(i, 0), a.n - 1) * a.ldw + min(col_of(0), a.k - 8));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) raw[i].v[j] = w[min(row_of(i, j), a.n - 1) * a.ldw + min(col_of(j), a.k - 1)];
         }
     }
-    auto find = [&] {
+    float most;
+    auto find = [&](bool finite) {
         most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) most = fmaxf(most, fabsf(v[i >> 3][i & 7]));
+        for (int i = 0; i < 64; ++i) {
+            const float v = fabsf(to_f(raw[i >> 3].v[i & 7]));
+            most = fmaxf(most, finite && not_finite(v) ? 0.f : v);
+        }
 #pragma unroll
         for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, d));
         if ((t & 31) == 0) part[t >> 5] = most;
@@ -105,15 +104,11 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
 #pragma unroll
         for (int i = 0; i < kThreads / 32; ++i) most = fmaxf(most, part[i]);
     };
-#pragma unroll
-    for (int i = 0; i < 64; ++i) v[i >> 3][i & 7] = row_of(i >> 3, VEC ? 0 : i & 7) < a.n && col_of(VEC ? 0 : i & 7) < a.k ? to_f(raw[i >> 3].v[i & 7]) : 0.f;
-    find();
-    if (not_finite(most)) {                            // the same in every thread
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-            if (not_finite(v[i >> 3][i & 7])) v[i >> 3][i & 7] = __int_as_float(0x7fffffff);
+    find(false);
+    const bool bad = not_finite(most);                 // the same in every thread
+    if (bad) {
         __syncthreads();
-        find();
+        find(true);
     }
     const uint32_t code = scale_code(most, kTop<false>);
     const float f = inverse_scale(code);
@@ -122,9 +117,17 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(const WeightArgs a) {
     for (int i = 0; i < 8; ++i) {
         uint32_t pair[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pair[j] = two_values<false>(v[i][2 * j] * f, v[i][2 * j + 1] * f);
+        for (int j = 0; j < 4; ++j) {
+            float lo = to_f(raw[i].v[2 * j]), hi = to_f(raw[i].v[2 * j + 1]);
+            if (bad) {
+                if (not_finite(lo)) lo = __int_as_float(0x7fffffff);
+                if (not_finite(hi)) hi = __int_as_float(0x7fffffff);
+            }
+            pair[j] = two_values<false>(lo * f, hi * f);
+        }
         if constexpr (VEC) {
-            if (col_ok && row_of(i, 0) < a.n) *reinterpret_cast<uint2 *>(q + row_of(i, 0) * a.ldq + col_of(0)) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+            if (col_of(0) < a.k && row_of(i, 0) < a.n)
+                *reinterpret_cast<uint2 *>(q + row_of(i, 0) * a.ldq + col_of(0)) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)

@@ -44,12 +44,41 @@ __device__ __forceinline__ uint32_t two_values(float lo, float hi) {
 }
 __device__ __forceinline__ bool not_finite(float v) { return !(fabsf(v) <= 3.402823466e38f); }
 
+// Two fp32 numbers in one instruction: kernels that pass over memory at its full rate have some thirty issue slots a value.
+struct Two { unsigned long long v; };
+__device__ __forceinline__ Two two(float lo, float hi) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 parts_of(Two a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void to_pairs(Two (&p)[4], const Eight<T> &o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = two(to_f(o.v[2 * j]), to_f(o.v[2 * j + 1]));
+}
+
 // Where a lane's eight values of a span lie.  VEC: side by side, so that they move in one access (rows on 16-byte boundaries, of a
 // multiple of eight values); otherwise 32 apart, so that a warp's accesses of single values are whole sectors all the same.
 template <bool VEC> __device__ __forceinline__ int place(int lane, int j) { return VEC ? lane * 8 + j : lane + 32 * j; }
 
-// Loading has no branch: a place behind the row's end reads its last values instead, and span_values() makes zeros of them.  (With a
-// branch around each access the compiler waits for one before it begins the next: the norm of 8192 rows took 90 us, SwiGLU of 49152 206.)
+// Loading has no branch: a place behind the row's end reads its last values once more.  (With a branch around each access the
+// compiler waits for one before it begins the next: the norm of 8192 rows took 90 us, SwiGLU of 49152 206.)  They lie in the
+// row's last block or in one that is not written, so its largest is the same; sums have to leave them out.
 template <class T, bool VEC>
 __device__ __forceinline__ void load_span(Eight<T> &o, const T *row, int at, int lane, int width) {
     if constexpr (VEC) {
@@ -58,14 +87,22 @@ __device__ __forceinline__ void load_span(Eight<T> &o, const T *row, int at, int
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int i = at + lane + 32 * j;
-            o.v[j] = i < width ? row[i] : from_f<T>(0.f);
+            o.v[j] = row[min(i, width - 1)];
         }
     }
 }
+// What lies behind the row's end becomes zeros.
 template <class T, bool VEC>
-__device__ __forceinline__ void span_values(float (&v)[8], const Eight<T> &o, int at, int lane, int width) {
+__device__ __forceinline__ void clear_span(Eight<T> &o, int at, int lane, int width) {
+    if constexpr (VEC) {
+        uint4 &v = *reinterpret_cast<uint4 *>(&o);
+        const bool in = at + lane * 8 < width;
+        v = make_uint4(in ? v.x : 0, in ? v.y : 0, in ? v.z : 0, in ? v.w : 0);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = at + place<VEC>(lane, VEC ? 0 : j) < width ? to_f(o.v[j]) : 0.f;
+        for (int j = 0; j < 8; ++j)
+            if (at + lane + 32 * j >= width) o.v[j] = from_f<T>(0.f);
+    }
 }
 template <class T, bool VEC>
 __device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, int lane, int width) {
@@ -80,12 +117,12 @@ __device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, in
     }
 }
 
-// Writes a span, whose values behind `width` are zeros, as two blocks.  The whole warp calls it.
+// Writes the span p v as two blocks (p: the same for the whole row).  The whole warp calls it.
 template <bool VEC, bool E5M2>
-__device__ __forceinline__ void put_span(float (&v)[8], uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
+__device__ __forceinline__ void put_span(float (&v)[8], float p, uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
     constexpr int kFirst = VEC ? 8 : 4;                // of the lane's values, those of its first block
     float m0, m1;
-    auto most = [&] {
+    auto most = [&] {                                  // rounding keeps the order: the largest |p v| is |p| times the largest |v|
         m0 = m1 = 0.f;
 #pragma unroll
         for (int j = 0; j < kFirst; ++j) m0 = fmaxf(m0, fabsf(v[j]));        // (a NaN is passed over)
@@ -96,16 +133,21 @@ __device__ __forceinline__ void put_span(float (&v)[8], uint8_t *q_row, uint8_t 
             m0 = fmaxf(m0, __shfl_xor_sync(kAll, m0, d));
             if (!VEC) m1 = fmaxf(m1, __shfl_xor_sync(kAll, m1, d));
         }
+        m0 *= fabsf(p);
+        m1 *= fabsf(p);
     };
     most();
     if (__any_sync(kAll, not_finite(m0) || not_finite(m1))) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j) {
+            v[j] *= p;
             if (not_finite(v[j])) v[j] = __int_as_float(0x7fffffff);
+        }
+        p = 1.f;
         most();
     }
     const uint32_t c0 = scale_code(m0, kTop<E5M2>), c1 = VEC ? c0 : scale_code(m1, kTop<E5M2>);
-    const float i0 = inverse_scale(c0), i1 = VEC ? i0 : inverse_scale(c1);
+    const float i0 = p * inverse_scale(c0), i1 = VEC ? i0 : p * inverse_scale(c1);       // (a power of two: v (p f) is (v p) f)
     uint32_t pair[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

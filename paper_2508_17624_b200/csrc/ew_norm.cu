@@ -38,7 +38,7 @@ __device__ __forceinline__ void add_up(float (&v)[N], int turn) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(kAll, v[i], d);
     if (W == 1) return;
-    __shared__ float part[2][N][W];
+    __shared__ __align__(16) float part[2][N][W];
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) part[turn & 1][i][threadIdx.x >> 5] = v[i];
@@ -78,14 +78,16 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
                 }
             }
         }
-        float ss[1] = {0.f};
+        Two square = two(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float v[8];
-            span_values<T, VEC>(v, t[i], (i * W + w) * kSpan, lane, a.width);
+            Two v[4];
+            clear_span<T, VEC>(t[i], (i * W + w) * kSpan, lane, a.width);
+            to_pairs(v, t[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ss[0] += v[j] * v[j];
+            for (int j = 0; j < 4; ++j) square = fma2(v[j], v[j], square);
         }
+        float ss[1] = {parts_of(square).x + parts_of(square).y};
         add_up<W, 1>(ss, turn++);
         const float norm = rsqrtf(ss[0] * a.inv_width + a.eps);
 #pragma unroll
@@ -93,86 +95,157 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
             const int at = (i * W + w) * kSpan;
             Eight<T> weight, y;
             load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), at, lane, a.width);
+            Two tv[4], wv[4];
+            to_pairs(tv, t[i]);
+            to_pairs(wv, weight);
             float v[8];
-            span_values<T, VEC>(v, t[i], at, lane, a.width);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = v[j] * norm * to_f(weight.v[j]);
-                y.v[j] = from_f<T>(v[j]);
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = parts_of(mul2(mul2(tv[j], two(norm, norm)), wv[j]));
+                v[2 * j] = f.x;
+                v[2 * j + 1] = f.y;
+                y.v[2 * j] = from_f<T>(f.x);
+                y.v[2 * j + 1] = from_f<T>(f.y);
             }
             if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
-            if (a.q && at < a.width) put_span<VEC, false>(v, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
+            if (a.q && at < a.width) put_span<VEC, false>(v, 1.f, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
         }
     }
 }
+
+constexpr int kMostCtas = 444;                         // of the gradient, whose sums are the workspace
+constexpr int kMostStages = 3;
+constexpr int kRingBytes = 98304;                      // a CTA's rows on their way: at least one of the widest, of three operands
+static_assert(kMostWidth * 6 <= kRingBytes, "room for a row");
 
 struct GradArgs {
     const void *dy, *t, *weight, *more;
     void *dt;
     float *parts;                                      // [gridDim.x, width]: each CTA's sums for dw
     long long lddy, ldt, ldmore, lddt, rows;
-    int width;
+    int *err;
+    int width, stages;
     float inv_width, eps;
 };
 
-template <class T, bool VEC, int W, int NV>
-__global__ void __launch_bounds__(kThreadsOf<W>) grad_kernel(const GradArgs a) {
+// A row a CTA of W warps at a time, its columns' sums in the registers of the threads that own them.  BULK: rows come to shared memory by bulk
+// copies, kStages of them ahead of the one that is worked on; without it a CTA's loads wait for the row before (30 us for 8192
+// rows of 2048, with the copies TIME).  Needs rows on 16-byte boundaries of a multiple of eight values.
+template <class T, bool BULK, int W, int NV>
+__global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel(const GradArgs a) {
     tc::pdl_launch_dependents();
-    tc::pdl_wait();
-    static_assert(W > 1, "a row is a CTA's: a column has one thread");
+    extern __shared__ __align__(128) uint8_t ring[];   // [stages][t, dy, dt_in][width]
+    __shared__ uint64_t bars[kMostStages];
+    __shared__ int abort_word;
+    volatile int *abort_flag = &abort_word;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    float dw[NV][8] = {};
-    int turn = 0;
+    const uint32_t row_bytes = (uint32_t)a.width * 2, stage_bytes = row_bytes * (a.more ? 3 : 2), bar = tc::smem_u32(bars), ring_at = tc::smem_u32(ring);
+    auto fetch = [&](long long r, int stage) {         // by one thread
+        const uint32_t to = ring_at + stage * stage_bytes, full = bar + 8 * stage;
+        tc::mbar_expect_tx(full, stage_bytes);
+        tc::bulk_load(to, reinterpret_cast<const T *>(a.t) + r * a.ldt, row_bytes, full);
+        tc::bulk_load(to + row_bytes, reinterpret_cast<const T *>(a.dy) + r * a.lddy, row_bytes, full);
+        if (a.more) tc::bulk_load(to + 2 * row_bytes, reinterpret_cast<const T *>(a.more) + r * a.ldmore, row_bytes, full);
+    };
+    if (BULK) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < a.stages; ++i) tc::mbar_init(bar + 8 * i, 1);
+            abort_word = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+    }
+    tc::pdl_wait();
+    if (BULK && threadIdx.x == 0)
+        for (int i = 0; i < a.stages; ++i)
+            if (blockIdx.x + (long long)i * gridDim.x < a.rows) fetch(blockIdx.x + (long long)i * gridDim.x, i);
+    Two weight[NV][4], dw[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        Eight<T> x;
+        load_span<T, BULK>(x, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+        to_pairs(weight[i], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dw[i][j] = two(0.f, 0.f);
+    }
+    int turn = 0, stage = 0, phase = 0;
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         Eight<T> dy[NV], t[NV], more[NV];
-        const T *dy_row = reinterpret_cast<const T *>(a.dy) + r * a.lddy, *t_row = reinterpret_cast<const T *>(a.t) + r * a.ldt;
-        const T *more_row = reinterpret_cast<const T *>(a.more) + r * a.ldmore;
+        const T *t_row, *dy_row, *more_row;
+        if (BULK) {
+            tc::wait_warp(bar + 8 * stage, phase, abort_flag, a.err);        // (where it gives up, the rest is wrong and reported, but ends)
+            t_row = reinterpret_cast<const T *>(ring + stage * stage_bytes);
+            dy_row = t_row + a.width;
+            more_row = dy_row + a.width;
+        } else {
+            t_row = reinterpret_cast<const T *>(a.t) + r * a.ldt;
+            dy_row = reinterpret_cast<const T *>(a.dy) + r * a.lddy;
+            more_row = reinterpret_cast<const T *>(a.more) + r * a.ldmore;
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            load_span<T, VEC>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
-            load_span<T, VEC>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
+            load_span<T, BULK>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
+            load_span<T, BULK>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
         }
         if (a.more)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
-        float sums[2] = {0.f, 0.f};                    // of t^2 and of dy w t
+            for (int i = 0; i < NV; ++i) load_span<T, BULK>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
+        Two square = two(0.f, 0.f), along2 = square;   // sums of t^2 and of dy w t
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            Eight<T> weight;
-            load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
-            float v[8];
-            span_values<T, VEC>(v, t[i], (i * W + w) * kSpan, lane, a.width);
+            Two tv[4], dv[4];
+            clear_span<T, BULK>(t[i], (i * W + w) * kSpan, lane, a.width);
+            to_pairs(tv, t[i]);
+            to_pairs(dv, dy[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sums[0] += v[j] * v[j];
-                sums[1] += to_f(dy[i].v[j]) * to_f(weight.v[j]) * v[j];
+            for (int j = 0; j < 4; ++j) {
+                square = fma2(tv[j], tv[j], square);
+                along2 = fma2(mul2(dv[j], weight[i][j]), tv[j], along2);
             }
         }
+        float sums[2] = {parts_of(square).x + parts_of(square).y, parts_of(along2).x + parts_of(along2).y};
         add_up<W, 2>(sums, turn++);
+        if (BULK) {                                    // every thread has its part of the stage: the next row may come
+            if (threadIdx.x == 0 && r + (long long)a.stages * gridDim.x < a.rows) fetch(r + (long long)a.stages * gridDim.x, stage);
+            if (++stage == a.stages) { stage = 0; phase ^= 1; }
+        }
         const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);      // mean(g u) = norm mean(g t)
+        const Two norm2 = two(norm, norm), back = two(-norm * along, -norm * along);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            Eight<T> weight, dt;
-            load_span<T, VEC>(weight, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+            Eight<T> dt;
+            Two tv[4], dv[4], mv[4];
+            to_pairs(tv, t[i]);
+            to_pairs(dv, dy[i]);
+            if (a.more) to_pairs(mv, more[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float tf = to_f(t[i].v[j]), df = to_f(dy[i].v[j]);
-                float v = norm * (df * to_f(weight.v[j]) - tf * along);
-                if (a.more) v += to_f(more[i].v[j]);
-                dt.v[j] = from_f<T>(v);
-                dw[i][j] += df * (tf * norm);
+            for (int j = 0; j < 4; ++j) {
+                const Two scaled = mul2(dv[j], norm2);
+                Two v = a.more ? fma2(tv[j], back, mv[j]) : mul2(tv[j], back);
+                v = fma2(scaled, weight[i][j], v);
+                dw[i][j] = fma2(scaled, tv[j], dw[i][j]);
+                dt.v[2 * j] = from_f<T>(parts_of(v).x);
+                dt.v[2 * j + 1] = from_f<T>(parts_of(v).y);
             }
-            store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
+            store_span<T, BULK>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
         }
     }
-    float *parts = a.parts + (long long)blockIdx.x * a.width;
+    float *part = a.parts + (long long)blockIdx.x * a.width;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int c = (i * W + w) * kSpan + place<VEC>(lane, j);
-            if (c < a.width) parts[c] = dw[i][j];
+            const int c = (i * W + w) * kSpan + place<BULK>(lane, j);
+            const float2 f = parts_of(dw[i][j >> 1]);
+            if (c < a.width) part[c] = j & 1 ? f.y : f.x;
         }
+    if (BULK) {
+        __syncthreads();
+        if (*abort_flag) {                             // let copies in flight land before the CTA's memory is reused
+            const long long t0 = clock64();
+            while (clock64() - t0 < 2000000ll) {}
+        }
+    }
 }
 
 // dw[c] = the sum of parts[:, c]: 32 columns a CTA, 32 threads a column
@@ -181,10 +254,11 @@ __global__ void __launch_bounds__(1024) parts_kernel(const float *parts, float *
     tc::pdl_wait();
     __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    float v = 0.f;
-    if (c < width)
-#pragma unroll 8
-        for (int p = warp; p < n_parts; p += 32) v += parts[(long long)p * width + c];
+    float x[(kMostCtas + 31) / 32], v = 0.f;           // all of a thread's loads are on their way together
+#pragma unroll
+    for (int i = 0; i < (kMostCtas + 31) / 32; ++i) x[i] = c < width && warp + 32 * i < n_parts ? parts[(long long)(warp + 32 * i) * width + c] : 0.f;
+#pragma unroll
+    for (int i = 0; i < (kMostCtas + 31) / 32; ++i) v += x[i];
     sums[warp][lane] = v;
     __syncthreads();
     v = sums[lane][warp];
@@ -192,9 +266,6 @@ __global__ void __launch_bounds__(1024) parts_kernel(const float *parts, float *
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
     if (lane == 0 && blockIdx.x * 32 + warp < width) dw[blockIdx.x * 32 + warp] = v;
 }
-
-// Rows that a CTA meets are at most this much apart: the CTAs of the gradient, whose sums are the workspace.
-constexpr int kMostParts = 592;
 
 template <class T, bool VEC, int W, int NV>
 ew_status_t launch(const Args &a, cudaStream_t st) {
@@ -213,19 +284,30 @@ ew_status_t pick(const Args &a, cudaStream_t st) {
     return launch<T, VEC, 16, 4>(a, st);
 }
 
-template <class T, bool VEC, int W, int NV>
-ew_status_t launch_grad(const GradArgs &a, int parts, float *dw, cudaStream_t st) {
-    const ew_status_t s = launched(launch_pdl(grad_kernel<T, VEC, W, NV>, dim3((unsigned)parts), dim3(kThreadsOf<W>), 0, st, a), "RMS norm gradient");
-    if (s != EW_OK) return s;
-    return launched(launch_pdl(parts_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(1024), 0, st, (const float *)a.parts, dw, parts, a.width), "RMS norm gradient");
+int grad_ctas(long long rows) { return (int)(rows < kMostCtas ? rows : kMostCtas); }
+
+template <class T, bool BULK, int W, int NV>
+ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
+    const int ctas = grad_ctas(a.rows), stage_bytes = a.width * 2 * (a.more ? 3 : 2), fit = kRingBytes / stage_bytes;
+    a.stages = fit < 1 ? 1 : fit < kMostStages ? fit : kMostStages;
+    if (ctas == 1) a.parts = dw;
+    const ew_status_t s = launched(launch_pdl(grad_kernel<T, BULK, W, NV>, dim3((unsigned)ctas), dim3(W * 32), BULK ? a.stages * stage_bytes : 0, st, a), "RMS norm gradient");
+    if (s != EW_OK || ctas == 1) return s;
+    return launched(launch_pdl(parts_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(1024), 0, st, (const float *)a.parts, dw, ctas, a.width), "RMS norm gradient");
 }
 
-template <class T, bool VEC>
-ew_status_t pick_grad(const GradArgs &a, int parts, float *dw, cudaStream_t st) {
-    if (a.width <= 2048) return launch_grad<T, VEC, 8, 1>(a, parts, dw, st);
-    if (a.width <= 4096) return launch_grad<T, VEC, 8, 2>(a, parts, dw, st);
-    if (a.width <= 8192) return launch_grad<T, VEC, 8, 4>(a, parts, dw, st);
-    return launch_grad<T, VEC, 16, 4>(a, parts, dw, st);
+template <class T, bool BULK>
+ew_status_t pick_grad(const GradArgs &a, float *dw, cudaStream_t st) {
+    if (a.width <= 1024) return launch_grad<T, BULK, 4, 1>(a, dw, st);
+    if (a.width <= 2048) return launch_grad<T, BULK, 4, 2>(a, dw, st);
+    if (a.width <= 4096) return launch_grad<T, BULK, 8, 2>(a, dw, st);
+    if (a.width <= 8192) return launch_grad<T, BULK, 16, 2>(a, dw, st);
+    return launch_grad<T, BULK, 16, 4>(a, dw, st);
+}
+
+template <class T, bool BULK, int W, int NV>
+int load_grad() {
+    return (int)cudaFuncSetAttribute(grad_kernel<T, BULK, W, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
 }
 
 template <class T, bool VEC>
@@ -234,8 +316,7 @@ int load_one() {
     return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 1>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 4>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) |
-           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 1>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 2>) |
-           (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, grad_kernel<T, VEC, 16, 4>) |
+           load_grad<T, VEC, 4, 1>() | load_grad<T, VEC, 4, 2>() | load_grad<T, VEC, 8, 2>() | load_grad<T, VEC, 16, 2>() | load_grad<T, VEC, 16, 4>() |
            (int)cudaFuncGetAttributes(&fa, parts_kernel);
 }
 
@@ -281,7 +362,7 @@ extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x,
 
 extern "C" int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width) {
     (void)width;
-    return rows < 1 ? 0 : rows < kMostParts ? rows : kMostParts;
+    return rows < 1 ? 0 : grad_ctas(rows);
 }
 
 extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight, const void *dt_in,
@@ -300,9 +381,8 @@ extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const voi
     if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (rows == 0) return launched((int)cudaMemsetAsync(dweight, 0, (size_t)width * 4, st), "cudaMemsetAsync");
-    const GradArgs a = {dy, t, weight, dt_in, dt, workspace, lddy, ldt, dt_in ? lddt_in : 0, lddt, rows, width, (float)(1.0 / width), eps};
+    const GradArgs a = {dy, t, weight, dt_in, dt, workspace, lddy, ldt, dt_in ? lddt_in : 0, lddt, rows, d->err, width, 0, (float)(1.0 / width), eps};
     const bool vec = !((((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 15) | ((a.lddy | a.ldt | a.ldmore | a.lddt | width) & 7));
-    const int parts = ew_rms_norm_grad_parts(rows, width);
-    if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(a, parts, dweight, st) : pick_grad<__nv_bfloat16, false>(a, parts, dweight, st);
-    return vec ? pick_grad<__half, true>(a, parts, dweight, st) : pick_grad<__half, false>(a, parts, dweight, st);
+    if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(a, dweight, st) : pick_grad<__nv_bfloat16, false>(a, dweight, st);
+    return vec ? pick_grad<__half, true>(a, dweight, st) : pick_grad<__half, false>(a, dweight, st);
 }
