@@ -323,7 +323,7 @@ class _Torch:
         cls.int32, cls.float32, cls.uint8, cls.bfloat16 = torch.int32, torch.float32, torch.uint8, torch.bfloat16
         cls.e4m3, cls.e5m2, cls.exponent = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
         cls.eights = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
-        cls.recording = torch.is_grad_enabled
+        cls.recording, cls.empty_like = torch.is_grad_enabled, torch.empty_like
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         cls.ready = True
         return cls
@@ -612,19 +612,13 @@ def _room(width, step):
     return (width + step - 1) // step * step
 
 
-def _new_blocks(rows, width, dtype, T, like):
-    """(q, scales) of new blocks of rows."""
-    wide, blocks = _room(width, 16), (width + 127) // 128
-    room = _room(blocks, 4)
-    q, scales = like.new_empty((rows, wide), dtype=dtype), like.new_empty((rows, room), dtype=T.exponent)
-    return q if wide == width else q[:, :width], scales if room == blocks else scales[:, :blocks]
-
-
 def _row_blocks(out, rows, width, dtype, T, like):
     """(q, scales, elements between q's rows, between the scales') of a result in blocks."""
     if out is None:
-        q, scales = _new_blocks(rows, width, dtype, T, like)
-        return q, scales, _room(width, 16), _room((width + 127) // 128, 4)
+        wide, blocks = (width + 15) // 16 * 16, (width + 127) // 128
+        room = (blocks + 3) // 4 * 4
+        q, scales = like.new_empty((rows, wide), dtype=dtype), like.new_empty((rows, room), dtype=T.exponent)
+        return q if wide == width else q[:, :width], scales if room == blocks else scales[:, :blocks], wide, room
     q, scales = out
     q, scales = _result(q, (rows, width), dtype, like, "q"), _result(scales, (rows, (width + 127) // 128), T.exponent, like, "scales")
     return q, scales, q.stride(0) if rows > 1 else width, scales.stride(0) if rows > 1 else scales.shape[1]
@@ -635,7 +629,8 @@ def scaled_rows(x, dtype=None, out=None):
     [rows, ceil(width / 128)]).  The header has the form.  Not differentiable."""
     T, dev = _torch(), x.get_device()
     code = _code(T, x.dtype)
-    dtype = T.e4m3 if dtype is None else dtype
+    if dtype is None:
+        dtype = T.e4m3
     to = _eight(T, dtype, "scaled_rows")
     rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
     q, scales, ldq, lds = _row_blocks(out, rows, width, dtype, T, x)
@@ -675,34 +670,42 @@ def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype
     groups, n, k, ldw, stride = _matrices(w, dev, T.e4m3, "w", a)
     if width != (n if grad else k):
         raise ValueError(f"rows of {width} do not match w of {tuple(w.shape)}")
+    blocks, nb, kb = (width + 127) // 128, (n + 127) // 128, (k + 127) // 128
     if not _good(a_scales, dev, T.exponent, 2):
         _on(a_scales, a, 2, "the rows' scales", T.exponent)
     if not _good(w_scales, dev, T.exponent, 3):
         _on(w_scales, a, 3, "w's scales", T.exponent)
-    blocks = (width + 127) // 128
-    if a_scales.shape[0] != rows or a_scales.shape[1] != blocks or (a_scales.stride(1) != 1 and blocks > 1 and rows):
+    if a_scales.shape != (rows, blocks) or (blocks > 1 and rows and a_scales.stride(1) != 1):
         raise ValueError(f"the rows' scales: ({rows}, {blocks}), a row's side by side, are wanted, got {tuple(a_scales.shape)}")
-    if tuple(w_scales.shape) != (groups, (n + 127) // 128, (k + 127) // 128) or not w_scales.is_contiguous():
-        raise ValueError(f"w's scales: contiguous ({groups}, {(n + 127) // 128}, {(k + 127) // 128}) are wanted, got {tuple(w_scales.shape)}")
-    if offsets is None:
-        if groups != 1:
-            raise ValueError(f"without offsets there is one matrix, got {groups}")
-    elif _offsets(offsets, dev, T, a) != groups:
-        raise ValueError(f"offsets has {offsets.shape[0]} entries for {groups} groups")
-    lds = a_scales.stride(0) if rows > 1 else _room(blocks, 4)
-    ldw = ldw if n > 1 else _room(k, 16)
-    stride = stride if groups > 1 else n * ldw
-    lda = lda if rows > 1 else _room(width, 16)
-    wide = k if grad else n
-    if out is None:
-        out_dtype = T.bfloat16 if out_dtype is None else out_dtype
-        code, out, ldo = _code(T, out_dtype), a.new_empty((rows, wide), dtype=out_dtype), wide
+    if w_scales.shape != (groups, nb, kb) or not w_scales.is_contiguous():
+        raise ValueError(f"w's scales: contiguous ({groups}, {nb}, {kb}) are wanted, got {tuple(w_scales.shape)}")
+    offsets_at = None
+    if offsets is not None:
+        if _offsets(offsets, dev, T, a) != groups:
+            raise ValueError(f"offsets has {offsets.shape[0]} entries for {groups} groups")
+        offsets_at = offsets.data_ptr()
+    elif groups != 1:
+        raise ValueError(f"without offsets there is one matrix, got {groups}")
+    # a row, a matrix alone has no stride of its own
+    if rows > 1:
+        lds = a_scales.stride(0)
     else:
-        out_dtype = out.dtype if out_dtype is None else out_dtype
-        code, out = _code(T, out_dtype), _result(out, (rows, wide), out_dtype, a)
+        lda, lds = (width + 15) // 16 * 16, (blocks + 3) // 4 * 4
+    if n == 1:
+        ldw = (k + 15) // 16 * 16
+    if groups == 1:
+        stride = n * ldw
+    wide = k if grad else n
+    if out_dtype is None:
+        out_dtype = T.bfloat16 if out is None else out.dtype
+    code = _code(T, out_dtype)
+    if out is None:
+        out, ldo = a.new_empty((rows, wide), dtype=out_dtype), wide
+    else:
+        _result(out, (rows, wide), out_dtype, a)
         ldo = out.stride(0) if rows > 1 else wide
-    rc = fn(dev, row_type, code, a.data_ptr(), lda, a_scales.data_ptr(), lds, w.data_ptr(), ldw, stride, w_scales.data_ptr(),
-            None if offsets is None else offsets.data_ptr(), rows, groups, n, k, out.data_ptr(), ldo, T.stream(dev))
+    rc = fn(dev, row_type, code, a.data_ptr(), lda, a_scales.data_ptr(), lds, w.data_ptr(), ldw, stride, w_scales.data_ptr(), offsets_at, rows, groups, n, k,
+            out.data_ptr(), ldo, T.stream(dev))
     if rc:
         _check(rc, where)
     return out
@@ -738,61 +741,61 @@ def swiglu_scaled(h, row_weights=None, out=None):
     return q, scales
 
 
-def _norm_operands(x, weight, residual, T, dev, where):
-    if (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)) and T.recording():
-        _recorded(where)
+def _norm_operands(x, weight, T, dev):
     code = _code(T, x.dtype)
     rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
-    if not _good(weight, dev, x.dtype, 1) or weight.shape[0] != width or not weight.is_contiguous():
+    if weight.get_device() != dev or weight.dtype is not x.dtype or weight.dim() != 1 or weight.shape[0] != width or not weight.is_contiguous():
         _on(weight, x, 1, "weight", x.dtype)
         raise ValueError(f"weight: a contiguous tensor of {width} is wanted, got {tuple(weight.shape)}")
     return code, rows, width, ldx
 
 
-def _like(t, shape, name, like):
-    """(tensor or None, address, elements between rows) of an operand that has x's shape and type."""
-    if t is None:
-        return None, 0
-    rows, width, ld = _matrix(t, like.get_device(), like.dtype, name, like)
-    if (rows, width) != shape:
-        raise ValueError(f"{name}: {shape} is wanted, got {tuple(t.shape)}")
+def _beside(t, rows, width, name, like, dev):
+    """(address, elements between rows) of an operand that has x's shape and type."""
+    t_rows, t_width, ld = _matrix(t, dev, like.dtype, name, like)
+    if t_rows != rows or t_width != width:
+        raise ValueError(f"{name}: {(rows, width)} is wanted, got {tuple(t.shape)}")
     return t.data_ptr(), ld
 
 
-def _norm(where, x, weight, residual, eps, y, with_y, blocks, with_blocks, sum_out):
+def _like(out, rows, width, name, like, T):
+    """(tensor, elements between rows) of a result that has x's shape and type."""
+    if out is None:
+        return T.empty_like(like), width
+    _result(out, (rows, width), like.dtype, like, name)
+    return out, out.stride(0) if rows > 1 else width
+
+
+def _norm(x, weight, residual, eps, y, with_y, blocks, with_blocks, total):
     T, dev = _torch(), x.get_device()
-    code, rows, width, ldx = _norm_operands(x, weight, residual, T, dev, where)
-    shape = (rows, width)
-    res, ldr = _like(residual, shape, "residual", x)
-    total, got = None, []
-    if residual is not None:
-        total = _result(sum_out, shape, x.dtype, x, "sum_out")
-    elif sum_out is not None:
-        raise ValueError("sum_out is for the sum with a residual")
-    q = scales = None
-    ldq = lds = 0
+    if (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)) and T.recording():
+        _recorded("ew_rms_norm")
+    code, rows, width, ldx = _norm_operands(x, weight, T, dev)
+    res = total_at = y_at = q_at = scales_at = None
+    ldr = ldt = ldy = ldq = lds = 0
+    got = ()
     if with_blocks:
         q, scales, ldq, lds = _row_blocks(blocks, rows, width, T.e4m3, T, x)
-        got += [q, scales]
+        q_at, scales_at, got = q.data_ptr(), scales.data_ptr(), (q, scales)
     if with_y:
-        y = _result(y, shape, x.dtype, x)
-        got.append(y)
-    if total is not None:
-        got.append(total)
-    many = rows > 1
-    rc = lib().ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width,
-                           None if total is None else total.data_ptr(), 0 if total is None else total.stride(0) if many else ldr,
-                           y.data_ptr() if with_y else None, (y.stride(0) if many else _room(width, 8)) if with_y else 0,
-                           None if q is None else q.data_ptr(), ldq, None if scales is None else scales.data_ptr(), lds, T.stream(dev))
+        y, ldy = _like(y, rows, width, "out", x, T)
+        y_at, got = y.data_ptr(), got + (y,)
+    if residual is not None:
+        res, ldr = _beside(residual, rows, width, "residual", x, dev)
+        total, ldt = _like(total, rows, width, "sum_out", x, T)
+        total_at, got = total.data_ptr(), got + (total,)
+    elif total is not None:
+        raise ValueError("sum_out is for the sum with a residual")
+    rc = lib().ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width, total_at, ldt, y_at, ldy, q_at, ldq, scales_at, lds, T.stream(dev))
     if rc:
-        _check(rc, where)
-    return got[0] if len(got) == 1 else tuple(got)
+        _check(rc, "ew_rms_norm")
+    return got[0] if len(got) == 1 else got
 
 
 def rms_norm(x, weight, residual=None, eps=1e-6, out=None, sum_out=None):
     """t / sqrt(mean(t^2) + eps) * weight of each row, t = x + residual rounded to their type (or x): y, or (y, t) with a residual.
     x, residual [rows, width] and weight [width] bf16 or fp16.  sum_out: where t goes; it may be the residual itself."""
-    return _norm("ew_rms_norm", x, weight, residual, eps, out, True, None, False, sum_out)
+    return _norm(x, weight, residual, eps, out, True, None, False, sum_out)
 
 
 def rms_norm_scaled(x, weight, residual=None, eps=1e-6, with_y=False, out=None, sum_out=None):
@@ -800,7 +803,7 @@ def rms_norm_scaled(x, weight, residual=None, eps=1e-6, with_y=False, out=None, 
     say), then t with a residual.  out: (q, scales), or (q, scales, y)."""
     if out is not None and len(out) != (3 if with_y else 2):
         raise ValueError("out: (q, scales), and y if it is wanted")
-    return _norm("ew_rms_norm", x, weight, residual, eps, out[2] if out is not None and with_y else None, with_y, None if out is None else out[:2], True, sum_out)
+    return _norm(x, weight, residual, eps, out[2] if out is not None and with_y else None, with_y, None if out is None else out[:2], True, sum_out)
 
 
 def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
@@ -808,17 +811,17 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     the residual): (dt [rows, width], the gradient of x and of the residual each, dweight float32 [width]).  dt: the
     gradient that reaches t past the norm, added in."""
     T, dev = _torch(), t.get_device()
-    if dy.requires_grad and T.recording() or (dt is not None and dt.requires_grad and T.recording()):
+    if (dy.requires_grad or t.requires_grad or weight.requires_grad or (dt is not None and dt.requires_grad)) and T.recording():
         _recorded("ew_rms_norm_grad")
-    code, rows, width, ldt = _norm_operands(t, weight, None, T, dev, "ew_rms_norm_grad")
-    shape = (rows, width)
-    dy_at, lddy = _like(dy, shape, "dy", t)
-    dt_at, lddt = _like(dt, shape, "dt", t)
-    out = _result(out, shape, t.dtype, t)
-    dw = t.new_empty((width,), dtype=T.float32)
-    room = t.new_empty((lib().ew_rms_norm_grad_parts(rows, width), width), dtype=T.float32)
-    rc = lib().ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(),
-                                out.stride(0) if rows > 1 else _room(width, 8), dw.data_ptr(), room.data_ptr(), T.stream(dev))
+    code, rows, width, ldt = _norm_operands(t, weight, T, dev)
+    dy_at, lddy = _beside(dy, rows, width, "dy", t, dev)
+    dt_at, lddt = (None, 0) if dt is None else _beside(dt, rows, width, "dt", t, dev)
+    out, ldo = _like(out, rows, width, "out", t, T)
+    fn = lib()
+    parts = fn.ew_rms_norm_grad_parts(rows, width)
+    dw, room = weight.new_empty((width,), dtype=T.float32), weight.new_empty((parts, width), dtype=T.float32)
+    rc = fn.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
+                             T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm_grad")
     return out, dw

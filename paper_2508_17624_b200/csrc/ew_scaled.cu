@@ -186,7 +186,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     int *t_pre = reinterpret_cast<int *>(tmem_holder + 2), *t_lo = t_pre + a.groups + 1, *t_cnt = t_lo + a.groups;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
     const int unit = blockIdx.x / CG, units = gridDim.x / CG;
 
@@ -311,13 +311,13 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         bool ok = true;
         for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
             const Item it = next_item(i, turn);
-            if (lane == 0) {
-                const int n_cta = (it.cols + C::kStep - 1) / C::kStep * 16;  // c of this item that each CTA stages
-                const int f = it.f0 + (int)rank * 128, c = it.row0 + (int)rank * n_cta;
-                const CUtensorMap *mb = &map_b.m[n_cta / 16 - 1];
-                const uint32_t bytes = CG * (kATile + n_cta * kBlock);
-                for (int kb = 0; kb < it.kb; ++kb) {
-                    if (!(ok = wait_on<false>(bar_empty + 8 * stage, phase ^ 1, abort_flag, a.err))) break;
+            const int n_cta = (it.cols + C::kStep - 1) / C::kStep * 16;      // c of this item that each CTA stages
+            const int f = it.f0 + (int)rank * 128, c = it.row0 + (int)rank * n_cta;
+            const CUtensorMap *mb = &map_b.m[n_cta / 16 - 1];
+            const uint32_t bytes = CG * (kATile + n_cta * kBlock);
+            for (int kb = 0; kb < it.kb; ++kb) {
+                if (!(ok = wait_all<false>(bar_empty + 8 * stage, phase ^ 1, abort_flag, a.err))) break;
+                if (elect()) {
                     const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
                     const uint32_t bar = CG == 2 ? leader_addr(bar_full + 8 * stage) : bar_full + 8 * stage;
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
@@ -325,10 +325,9 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     if (WAY == kProduct) load_3d<CG>(sa, &map_a, t, f, it.g, bar);
                     else load_3d<CG>(sa, &map_a, f, t, it.g, bar);
                     load_2d<CG>(sb, mb, t, c, bar);
-                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
                 }
+                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
-            ok = __shfl_sync(0xffffffffu, ok, 0);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (the leader CTA's)
@@ -340,42 +339,43 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 const Item it = next_item(i, turn);
                 const int n = (it.cols + C::kStep - 1) / C::kStep * C::kStep;
                 const uint32_t idesc = base | ((uint32_t)(n >> 3) << 17);
-                for (int kb = 0; lane == 0 && kb < it.kb && ok;) {
-                    if (!(ok = wait_on<CG == 2>(bar_tempty + 8 * acc, (acc_phases >> acc & 1) ^ 1, abort_flag, a.err))) break;
+                for (int kb = 0; kb < it.kb && ok;) {
+                    if (!(ok = wait_all<CG == 2>(bar_tempty + 8 * acc, (acc_phases >> acc & 1) ^ 1, abort_flag, a.err))) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + acc * NT;
                     for (const int first = kb, end = min(it.kb, kb + it.chunk); kb < end; ++kb) {
                         const uint32_t t_sa = tmem_base + C::kScaleCol + slot * C::kSlotCols, t_sb = t_sa + 4;
                         if ((kb & 3) == 0) {           // the exponents of the next four k-blocks
-                            if (!(ok = wait_on<CG == 2>(bar_sfull + 8 * slot, slot_phase, abort_flag, a.err))) break;
+                            if (!(ok = wait_all<CG == 2>(bar_sfull + 8 * slot, slot_phase, abort_flag, a.err))) break;
                             tc_fence_after();
                             const uint64_t from = desc_scales(smem_u32(scales) + slot * C::kSlotBytes);
+                            if (elect())
 #pragma unroll
-                            for (int c = 0; c <= C::kBChunks; ++c)
-                                if (c < 2 || n > 128 * (c - 1)) copy_scales<CG>(t_sa + 4 * c, from + c * (512 >> 4));
+                                for (int c = 0; c <= C::kBChunks; ++c)
+                                    if (c < 2 || n > 128 * (c - 1)) copy_scales<CG>(t_sa + 4 * c, from + c * (512 >> 4));
                         }
-                        if (!(ok = wait_on<CG == 2>(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
+                        if (!(ok = wait_all<CG == 2>(bar_full + 8 * stage, phase, abort_flag, a.err))) break;
                         tc_fence_after();
-                        const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
-                        const uint64_t da = WAY == kProduct ? smem_desc_sw128(sa) : desc_mnmajor(sa), db = smem_desc_sw128(sb);
-                        const uint32_t id = idesc | (uint32_t)(kb & 3) << 4 | (uint32_t)(kb & 3) << 29;      // which byte of the exponents
-                        // 32 summed values a step: 32 bytes further along a K-major row, 32 rows of 128 bytes in an MN-major tile
-                        constexpr int kStepA = WAY == kProduct ? 2 : 256, kStepB = 2;
+                        const bool last = (kb & 3) == 3 || kb == it.kb - 1;
+                        if (elect()) {
+                            const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kATile;
+                            const uint64_t da = WAY == kProduct ? smem_desc_sw128(sa) : desc_mnmajor(sa), db = smem_desc_sw128(sb);
+                            const uint32_t id = idesc | (uint32_t)(kb & 3) << 4 | (uint32_t)(kb & 3) << 29;      // which byte of the exponents
+                            // 32 summed values a step: 32 bytes further along a K-major row, 32 rows of 128 bytes in an MN-major tile
+                            constexpr int kStepA = WAY == kProduct ? 2 : 256, kStepB = 2;
 #pragma unroll
-                        for (int ki = 0; ki < kBlock / 32; ++ki) mma<CG>(d, da + kStepA * ki, db + kStepB * ki, id, t_sa, t_sb, (kb != first || ki) ? 1u : 0u);
-                        commit<CG>(bar_empty + 8 * stage);
-                        if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
-                        if ((kb & 3) == 3 || kb == it.kb - 1) {
-                            commit<CG>(bar_sempty + 8 * slot);
-                            if (++slot == kSlots) { slot = 0; slot_phase ^= 1; }
+                            for (int ki = 0; ki < kBlock / 32; ++ki) mma<CG>(d, da + kStepA * ki, db + kStepB * ki, id, t_sa, t_sb, (kb != first || ki) ? 1u : 0u);
+                            commit<CG>(bar_empty + 8 * stage);
+                            if (last) commit<CG>(bar_sempty + 8 * slot);
                         }
+                        if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                        if (last && ++slot == kSlots) { slot = 0; slot_phase ^= 1; }
                     }
                     if (!ok) break;
-                    commit<CG>(bar_tfull + 8 * acc);
+                    if (elect()) commit<CG>(bar_tfull + 8 * acc);
                     acc_phases ^= 1u << acc;
                     if (!sums_here(it)) acc ^= 1;
                 }
-                ok = __shfl_sync(0xffffffffu, ok, 0);
             }
         }
     } else if (warp == kScaleWarp) {
@@ -571,7 +571,7 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     const uint32_t w_box[3] = {kBlock, 128, 1};
     if ((s = encode_map(*d, &ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, w, 3, wd, ws, w_box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
     const uint64_t xd[2] = {(uint64_t)t, (uint64_t)rows}, xs[1] = {(uint64_t)ldx};
-    for (int i = 0; i < kMaps; ++i) {
+    for (int i = 0; i < kMaps && 16 * i < rows; ++i) {                       // (an item has no more rows than there are)
         const uint32_t box[2] = {kBlock, 16u * (i + 1)};
         if ((s = encode_map(*d, &mb.m[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, x, 2, xd, xs, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
     }

@@ -251,5 +251,30 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
+// The same by a whole warp, in every lane: for the warps that issue copies and products.  Their loops are the same in all lanes and one
+// elected lane issues, which the compiler turns into uniform registers; with a loop in one lane alone every operand of every
+// product is first moved there (block-scaled products: 885 clocks a k-block of four, LATER).
+template <bool PEER>
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    if (__all_sync(0xffffffffu, try_nap<PEER>(bar, parity))) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        if (__all_sync(0xffffffffu, try_nap<PEER>(bar, parity))) return true;
+        const bool late = clock64() - t0 > kWaitLimitCycles;
+        if (__any_sync(0xffffffffu, late || *abort_flag)) {
+            if (late) {
+                *abort_flag = 1;
+                atomicOr(err, 2);
+            }
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 }  // namespace tc
 }  // namespace ew
