@@ -44,6 +44,7 @@ constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 7;
 constexpr int kSlots = 4;                              // places for the exponents of four k-blocks
 constexpr int kMaps = 8;                               // row boxes of 16, 32 .. 128 rows
+constexpr int kStaging = kEpilogueWarps * 2048;        // 32 x 32 16-bit results of each epilogue warp
 // Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 1024 terms for
 // fp32 results, 8192 for fp16, 65536 for bf16.
 constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 1024 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
@@ -61,6 +62,7 @@ struct Args {
     int out_kind;                                      // ew_dtype_t
     int sum_blocks;
     int e5m2;                                          // type of the rows
+    int wide;                                          // 16-bit results whose rows lie on 16-byte boundaries, f_size a multiple of eight
     int stages;
 };
 
@@ -154,6 +156,47 @@ __device__ __forceinline__ void store_columns(T *p, long long ldo, const uint32_
         q[j & 7] += step;
     }
 }
+// The same for 16-bit results in rows on 16-byte boundaries: the warp reads its 32 x 32 part of the accumulator in the order of the
+// small matrix instructions' results, turns it over on the way to shared memory (a row of 64 bytes a column, its four pieces of 16
+// bytes exchanged by the row so that neither side meets a bank twice), and stores 16 bytes a lane, eight rows at a time: a third of
+// the instructions, which at the power limit is time (prompt: 261 -> LATER us).
+template <bool BF16>
+__device__ __forceinline__ void store_wide(uint32_t taddr, uint8_t *stage, uint16_t *p, long long ldo, int lim, int lane, int f_left) {
+    uint32_t v[2][16];
+    tc_ld16x256(taddr, v[0]);
+    tc_ld16x256(taddr + (16u << 16), v[1]);
+    tc_wait_ld();
+    const uint32_t at = smem_u32(stage);
+    __syncwarp();                                      // (the last round has been read)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                      // eight columns a time: four 8 x 8 matrices, 8 f each
+        uint32_t m[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float lo = __uint_as_float(v[j >> 1][4 * i + 2 * (j & 1)]), hi = __uint_as_float(v[j >> 1][4 * i + 2 * (j & 1) + 1]);
+            if (BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                m[j] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __half2 h = __floats2half2_rn(lo, hi);
+                m[j] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+        const int row = 8 * i + (lane & 7), piece = lane >> 3;
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                     ::"r"(at + row * 64 + ((piece ^ (row >> 1 & 3)) << 4)), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3]) : "memory");
+    }
+    __syncwarp();
+    const int piece = lane & 3;
+    uint16_t *to = p + (long long)(lane >> 2) * ldo + piece * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 8 * i + (lane >> 2);
+        const uint4 x = *reinterpret_cast<const uint4 *>(stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4));
+        if (row < lim && piece * 8 < f_left) *reinterpret_cast<uint4 *>(to) = x;
+        to += 8 * ldo;
+    }
+}
 __device__ __forceinline__ void add_columns(float *p, long long ldo, const uint32_t (&v)[32], int lim) {
 #pragma unroll
     for (int j0 = 0; j0 < 32; j0 += 8) {
@@ -176,10 +219,11 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
-    // after the ring: the exponents; barriers full, empty [kMaxStages] each, exponents full, empty [kSlots] each, tmem full, empty [2]
+    // after the ring: the exponents; 16-bit results on their way out; barriers full, empty [kMaxStages] each, exponents full, empty [kSlots] each, tmem full, empty [2]
     // each; TMEM base, abort flag; then the group table: first block of each group, first row, rows
     uint8_t *scales = smem_al + a.stages * C::kStageBytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(scales + kSlots * C::kSlotBytes);
+    uint8_t *staging = scales + kSlots * C::kSlotBytes;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kStaging);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMaxStages, bar_sfull = bar_empty + 8 * kMaxStages, bar_sempty = bar_sfull + 8 * kSlots;
     const uint32_t bar_tfull = bar_sempty + 8 * kSlots, bar_tempty = bar_tfull + 16;
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 2 * kMaxStages + 2 * kSlots + 4);
@@ -453,21 +497,33 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     tc_wait_st();
                     if (!last) to_store = 0;
                 }
+                if (a.wide) {
+                    const int f_left = a.f_size - (f - lane);
+                    uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + at - lane;
+                    uint8_t *stage = staging + lg * 2048;
+                    if (f_left > 0)
 #pragma unroll 1
-                for (int c0 = 0; c0 < to_store; c0 += 32) {
-                    uint32_t v[32];
-                    tc_ld32(t0 + c0, v);               // columns behind the item's last are in the accumulator set, not stored
-                    tc_wait_ld();
-                    const int lim = min(32, it.cols - c0);
-                    const size_t to = at + (size_t)c0 * a.ldo;
-                    if (f_ok) {
-                        if (a.out_kind == EW_FP32) {
-                            if (kb > 0) add_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
-                            else store_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
-                        } else if (a.out_kind == EW_BF16) {
-                            store_columns(reinterpret_cast<__nv_bfloat16 *>(a.out) + to, a.ldo, v, lim);
-                        } else {
-                            store_columns(reinterpret_cast<__half *>(a.out) + to, a.ldo, v, lim);
+                        for (int c0 = 0; c0 < to_store; c0 += 32) {
+                            if (a.out_kind == EW_BF16) store_wide<true>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
+                            else store_wide<false>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
+                        }
+                } else {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < to_store; c0 += 32) {
+                        uint32_t v[32];
+                        tc_ld32(t0 + c0, v);           // columns behind the item's last are in the accumulator set, not stored
+                        tc_wait_ld();
+                        const int lim = min(32, it.cols - c0);
+                        const size_t to = at + (size_t)c0 * a.ldo;
+                        if (f_ok) {
+                            if (a.out_kind == EW_FP32) {
+                                if (kb > 0) add_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
+                                else store_columns(reinterpret_cast<float *>(a.out) + to, a.ldo, v, lim);
+                            } else if (a.out_kind == EW_BF16) {
+                                store_columns(reinterpret_cast<__nv_bfloat16 *>(a.out) + to, a.ldo, v, lim);
+                            } else {
+                                store_columns(reinterpret_cast<__half *>(a.out) + to, a.ldo, v, lim);
+                            }
                         }
                     }
                 }
@@ -504,7 +560,7 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     const long long live = a.groups < a.rows ? a.groups : a.rows;            // groups that can have rows
     const long long max_items = (live + a.rows / NT) * a.f_tiles;
     if (max_items > 0x7fff0000) return refuse("scaled product: too many output tiles");
-    const int rest = 1024 + kSlots * C::kSlotBytes + kBarBytes + (3 * a.groups + 1) * 4, fit = (kSmemLimit - rest) / C::kStageBytes;
+    const int rest = 1024 + kSlots * C::kSlotBytes + kStaging + kBarBytes + (3 * a.groups + 1) * 4, fit = (kSmemLimit - rest) / C::kStageBytes;
     a.stages = fit < kMaxStages ? fit : kMaxStages;
     cudaLaunchConfig_t cfg = {};
     const long long units = d.sm_count / CG;
@@ -591,6 +647,7 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     a.kb = (int)((k + (int64_t)kBlock - 1) / kBlock);
     a.out_kind = out_dtype;
     a.e5m2 = row_type == EW_E5M2;
+    a.wide = out_dtype != EW_FP32 && !(((uintptr_t)out & 15) | ((ldo | f) & 7));
     cudaStream_t st = (cudaStream_t)stream;
     if (rows <= 128ll * groups) return grad ? launch<1, 128, kInputGrad>(*d, ma, mb, a, st) : launch<1, 128, kProduct>(*d, ma, mb, a, st);
     return grad ? launch<2, 224, kInputGrad>(*d, ma, mb, a, st) : launch<2, 224, kProduct>(*d, ma, mb, a, st);
