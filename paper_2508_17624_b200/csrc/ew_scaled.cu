@@ -266,39 +266,42 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         // group table: first row and rows of each group, and the number of row blocks before it.  Offsets are clamped to
         // the matrix and to the largest one before them, so that whatever the call was given the groups lie inside the
         // matrix and apart from one another.
+        // The offsets of 128 groups are asked for together.
         auto offset = [&](int g) { return a.offsets ? *(const volatile int32_t *)(a.offsets + g) : g ? a.rows : 0; };
         int before = 0, raw = offset(0), end = min(max(raw, 0), a.rows);
         bool bad = raw != end;
-        for (int g0 = 0; g0 < a.groups; g0 += 32) {
-            const int g = g0 + lane;
-            int hi = end;
-            if (g < a.groups) {
-                raw = offset(g + 1);
-                hi = min(max(raw, 0), a.rows);
-            }
+        for (int g0 = 0; g0 < a.groups; g0 += 128) {
+            int next[4];
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, hi, d);
-                if (lane >= d) hi = max(hi, v);
-            }
-            hi = max(hi, end);
-            int lo = __shfl_up_sync(0xffffffffu, hi, 1);
-            if (lane == 0) lo = end;
-            const int nb = g >= a.groups ? 0 : (hi - lo + NT - 1) / NT;
-            int inc = nb;
+            for (int c = 0; c < 4; ++c) next[c] = offset(min(g0 + 32 * c + lane, a.groups - 1) + 1);
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, inc, d);
-                if (lane >= d) inc += v;
+            for (int c = 0; c < 4; ++c) {
+                const int g = g0 + 32 * c + lane;
+                int hi = g < a.groups ? min(max(next[c], 0), a.rows) : end;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, hi, d);
+                    if (lane >= d) hi = max(hi, v);
+                }
+                hi = max(hi, end);
+                int lo = __shfl_up_sync(0xffffffffu, hi, 1);
+                if (lane == 0) lo = end;
+                const int nb = g >= a.groups ? 0 : (hi - lo + NT - 1) / NT;
+                int inc = nb;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, inc, d);
+                    if (lane >= d) inc += v;
+                }
+                if (g < a.groups) {
+                    bad |= next[c] != hi;
+                    t_lo[g] = lo;
+                    t_cnt[g] = hi - lo;
+                    t_pre[g] = before + inc - nb;
+                }
+                before += __shfl_sync(0xffffffffu, inc, 31);
+                end = __shfl_sync(0xffffffffu, hi, 31);
             }
-            if (g < a.groups) {
-                bad |= raw != hi;
-                t_lo[g] = lo;
-                t_cnt[g] = hi - lo;
-                t_pre[g] = before + inc - nb;
-            }
-            before += __shfl_sync(0xffffffffu, inc, 31);
-            end = __shfl_sync(0xffffffffu, hi, 31);
         }
         if (lane == 0) t_pre[a.groups] = before;
         if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadIndex);
