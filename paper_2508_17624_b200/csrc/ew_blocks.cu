@@ -25,6 +25,19 @@ struct RowArgs {
     int width;                                         // of the result
 };
 
+// g / (1 + 2^(-g log2 e)) by the fast power of two and reciprocal: 2 + 1.2 |g| steps of 2^-23, and 0 where the power passes 2^126
+__device__ __forceinline__ Two silu(Two g) {
+    constexpr float kLog2e = 1.44269504f;
+    float2 e = parts_of(mul2(g, two(-kLog2e, -kLog2e)));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    const Two one = two(1.f, 1.f);
+    e = parts_of(fma2(two(e.x, e.y), one, one));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    return mul2(g, two(e.x, e.y));
+}
+
 // W warps share a row; each asks for AHEAD spans before it works on the first.
 template <class T, bool ACT, bool E5M2, bool VEC, int W>
 __global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
@@ -47,11 +60,13 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
             for (int k = 0; k < kAhead; ++k) {
                 const int at = from + k * W * kSpan;
                 if (at < a.width) {
-                    float v[8];
+                    Two v[4];
+                    to_pairs(v, g[k]);
+                    if (ACT) {
+                        Two up[4];
+                        to_pairs(up, u[k]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[j] = to_f(g[k].v[j]);
-                        if (ACT) v[j] = v[j] * __fdividef(1.f, 1.f + __expf(-v[j])) * to_f(u[k].v[j]);
+                        for (int j = 0; j < 4; ++j) v[j] = mul2(silu(v[j]), up[j]);
                     }
                     put_span<VEC, E5M2>(v, p, q, scales, at, lane, a.width);
                 }

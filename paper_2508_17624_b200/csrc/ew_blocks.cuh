@@ -66,6 +66,12 @@ __device__ __forceinline__ Two mul2(Two a, Two b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
+// max(m, |a.lo|, |a.hi|); a NaN is passed over
+__device__ __forceinline__ float max_abs(float m, Two a) {
+    const float2 v = parts_of(a);
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(fabsf(v.x)), "f"(fabsf(v.y)), "f"(m));
+    return m;
+}
 template <class T>
 __device__ __forceinline__ void to_pairs(Two (&p)[4], const Eight<T> &o) {
 #pragma unroll
@@ -119,15 +125,15 @@ __device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, in
 
 // Writes the span p v as two blocks (p: the same for the whole row).  The whole warp calls it.
 template <bool VEC, bool E5M2>
-__device__ __forceinline__ void put_span(float (&v)[8], float p, uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
-    constexpr int kFirst = VEC ? 8 : 4;                // of the lane's values, those of its first block
+__device__ __forceinline__ void put_span(Two (&v)[4], float p, uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
+    constexpr int kFirst = VEC ? 4 : 2;                // of the lane's pairs, those of its first block
     float m0, m1;
     auto most = [&] {                                  // rounding keeps the order: the largest |p v| is |p| times the largest |v|
         m0 = m1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < kFirst; ++j) m0 = fmaxf(m0, fabsf(v[j]));        // (a NaN is passed over)
+        for (int j = 0; j < kFirst; ++j) m0 = max_abs(m0, v[j]);
 #pragma unroll
-        for (int j = kFirst; j < 8; ++j) m1 = fmaxf(m1, fabsf(v[j]));
+        for (int j = kFirst; j < 4; ++j) m1 = max_abs(m1, v[j]);
 #pragma unroll
         for (int d = VEC ? 8 : 16; d; d >>= 1) {
             m0 = fmaxf(m0, __shfl_xor_sync(kAll, m0, d));
@@ -139,9 +145,11 @@ __device__ __forceinline__ void put_span(float (&v)[8], float p, uint8_t *q_row,
     most();
     if (__any_sync(kAll, not_finite(m0) || not_finite(m1))) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] *= p;
-            if (not_finite(v[j])) v[j] = __int_as_float(0x7fffffff);
+        for (int j = 0; j < 4; ++j) {
+            float2 f = parts_of(mul2(v[j], two(p, p)));
+            if (not_finite(f.x)) f.x = __int_as_float(0x7fffffff);
+            if (not_finite(f.y)) f.y = __int_as_float(0x7fffffff);
+            v[j] = two(f.x, f.y);
         }
         p = 1.f;
         most();
@@ -151,8 +159,9 @@ __device__ __forceinline__ void put_span(float (&v)[8], float p, uint8_t *q_row,
     uint32_t pair[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float f = 2 * j < kFirst ? i0 : i1;
-        pair[j] = two_values<E5M2>(v[2 * j] * f, v[2 * j + 1] * f);
+        const float f = j < kFirst ? i0 : i1;
+        const float2 x = parts_of(mul2(v[j], two(f, f)));
+        pair[j] = two_values<E5M2>(x.x, x.y);
     }
     if constexpr (VEC) {
         if (at + lane * 8 < width) *reinterpret_cast<uint2 *>(q_row + at + lane * 8) = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);

@@ -98,17 +98,15 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
             Two tv[4], wv[4];
             to_pairs(tv, t[i]);
             to_pairs(wv, weight);
-            float v[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 f = parts_of(mul2(mul2(tv[j], two(norm, norm)), wv[j]));
-                v[2 * j] = f.x;
-                v[2 * j + 1] = f.y;
+                tv[j] = mul2(mul2(tv[j], two(norm, norm)), wv[j]);
+                const float2 f = parts_of(tv[j]);
                 y.v[2 * j] = from_f<T>(f.x);
                 y.v[2 * j + 1] = from_f<T>(f.y);
             }
             if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
-            if (a.q && at < a.width) put_span<VEC, false>(v, 1.f, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
+            if (a.q && at < a.width) put_span<VEC, false>(tv, 1.f, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
         }
     }
 }
