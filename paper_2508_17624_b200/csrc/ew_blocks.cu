@@ -40,7 +40,7 @@ __device__ __forceinline__ Two silu(Two g) {
 
 // W warps share a row; each asks for AHEAD spans before it works on the first.
 template <class T, bool ACT, bool E5M2, bool VEC, int W>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
+__global__ void __launch_bounds__(kThreads, VEC && W == 1 ? 5 : 1) rows_kernel(const RowArgs a) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     constexpr int kRows = kThreads / 32 / W, kAhead = W > 1 ? 1 : !VEC ? 2 : ACT ? 3 : 4;
