@@ -403,8 +403,9 @@ ew_status_t ew_swiglu_grad(int32_t device, int32_t dtype, const void *dact, int6
  *   rows     q [rows, width] with ldq elements between rows, scales [rows, ceil(width / 128)] with ldscales bytes between
  *            rows: a scale for 128 neighbouring values of a row (the last of a row may be shorter)
  *   weights  q [n_slots, n, k], scales [n_slots, ceil(n / 128), ceil(k / 128)] without gaps: a scale for 128 x 128 values
- * The products below read q from 16-byte aligned rows (ldq and strides multiples of 16) and the rows' scales from 4-byte aligned ones (ldscales
- * a multiple of 4); the operators that write them take any strides.  Bytes behind a row's end are neither read nor written. */
+ * The products below read q from 16-byte aligned rows (ldq and strides multiples of 16) and take scales at any address, those of rows
+ * fastest from 4-byte boundaries; the operators that write blocks take any strides.  Bytes behind a row's end are neither
+ * read nor written. */
 
 /* Rows x [rows, width] (bf16 or fp16) as blocks of q_type. */
 ew_status_t ew_scaled_rows(int32_t device, int32_t dtype, int32_t q_type, const void *x, int64_t ldx, int32_t rows, int32_t width,
@@ -447,7 +448,7 @@ ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x, int64_t ld
                         void *scales, int64_t ldscales, void *cuda_stream);
 
 /* Its gradient: dt [rows, width] = the gradient with respect to t (and so to x and residual each) from dy and t, plus dt_in, the gradient that
- * reaches t past the norm (null: none), and dweight fp32 [width], summed over the rows in a fixed order.  workspace: fp32
+ * reaches t past the norm (null: none; it may be dt itself, same address and stride), and dweight fp32 [width], summed over the rows in a fixed order.  workspace: fp32
  * [ew_rms_norm_grad_parts(rows, width), width], of this call alone while it runs. */
 ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight,
                              const void *dt_in, int64_t lddt_in, float eps, int32_t rows, int32_t width, void *dt, int64_t lddt,

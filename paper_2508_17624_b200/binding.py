@@ -599,8 +599,8 @@ def swiglu_grad(dact, h, row_weights=None, out=None):
 
 
 # 8-bit floating point in blocks of 128: q (float8_e4m3fn or float8_e5m2) and scales (float8_e8m0fnu, powers of two).  Rows of
-# q lie on 16-byte boundaries and rows of scales on 4-byte ones, as the products want them: results are views of padded tensors
-# where the width is no multiple of 16.
+# q lie on 16-byte boundaries, as the products want them, and rows of scales on 4-byte ones, as they like them: results are views of
+# padded tensors where the width is no multiple of 16 or 512.
 def _eight(T, dtype, name) -> int:
     code = T.eights.get(dtype)
     if code is None:
@@ -626,8 +626,10 @@ def _row_blocks(out, rows, width, dtype, T, like):
 
 def scaled_rows(x, dtype=None, out=None):
     """Rows x [rows, width] (bf16 or fp16) as 8-bit blocks for `scaled_mm`: (q [rows, width] of dtype, float8_e4m3fn by default, scales
-    [rows, ceil(width / 128)]).  The header has the form.  Not differentiable."""
+    [rows, ceil(width / 128)]).  The header has the form."""
     T, dev = _torch(), x.get_device()
+    if x.requires_grad and T.recording():
+        _recorded("ew_scaled_rows")
     code = _code(T, x.dtype)
     if dtype is None:
         dtype = T.e4m3
@@ -665,6 +667,8 @@ def scaled_pack(w, out=None):
 
 def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype, grad):
     T, dev = _torch(), a.get_device()
+    if (a.requires_grad or w.requires_grad) and T.recording():
+        _recorded(where)
     row_type = _eight(T, a.dtype, "the rows' operand")
     rows, width, lda = _matrix(a, dev, a.dtype, "the rows' operand", None)
     groups, n, k, ldw, stride = _matrices(w, dev, T.e4m3, "w", a)
@@ -809,7 +813,7 @@ def rms_norm_scaled(x, weight, residual=None, eps=1e-6, with_y=False, out=None, 
 def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     """The gradient of `rms_norm` (and, for the blocks' values, of `rms_norm_scaled`) from dy and t, the normed stream (x, or its sum with
     the residual): (dt [rows, width], the gradient of x and of the residual each, dweight float32 [width]).  dt: the
-    gradient that reaches t past the norm, added in."""
+    gradient that reaches t past the norm, added in; it may be `out`."""
     T, dev = _torch(), t.get_device()
     if (dy.requires_grad or t.requires_grad or weight.requires_grad or (dt is not None and dt.requires_grad)) and T.recording():
         _recorded("ew_rms_norm_grad")

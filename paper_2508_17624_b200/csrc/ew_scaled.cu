@@ -62,6 +62,7 @@ struct Args {
     int out_kind;                                      // ew_dtype_t
     int sum_blocks;
     int e5m2;                                          // type of the rows
+    int words;                                         // the rows' scales start on 4-byte boundaries
     int wide;                                          // 16-bit results whose rows lie on 16-byte boundaries, f_size a multiple of eight
     int stages;
 };
@@ -446,9 +447,12 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     const uint8_t *p = a.row_scales + (long long)(it.row0 + min(lane + 32 * j, it.cols - 1)) * a.lds + kb;
                     word[j] = 0;
                     if (32 * j < it.cols) {
-                        if (left == 4) word[j] = *reinterpret_cast<const uint32_t *>(p);
-                        else
-                            for (int b = 0; b < left; ++b) word[j] |= (uint32_t)p[b] << (8 * b);
+                        if (a.words && left == 4) {
+                            word[j] = *reinterpret_cast<const uint32_t *>(p);
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) word[j] |= (uint32_t)p[min(b, left - 1)] << (8 * b);
+                        }
                     }
                 }
             };
@@ -616,8 +620,7 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     if ((rows > 0 && bad_matrix(x, ldx, t)) || bad_matrix(w, ldw, k) || ldo < f || !rows_apart(groups, group_stride, n, ldw, k) ||
         (groups > 1 && ((group_stride & 15) || group_stride >= (1ll << 39))))
         return refuse("scaled product: operands need 16-byte aligned rows that do not overlap");
-    if (rows > 0 && (!x_scales || ((uintptr_t)x_scales & 3) || (lds & 3) || lds < (t + (int64_t)kBlock - 1) / kBlock))
-        return refuse("scaled product: the rows' scales start on 4-byte boundaries");
+    if (rows > 0 && (!x_scales || lds < (t + (int64_t)kBlock - 1) / kBlock)) return refuse("scaled product: the rows' scales are missing or overlap");
     if (device < 0) return EW_ERR_NO_DEVICE;
     if (rows == 0) return EW_OK;
     DeviceGuard guard;
@@ -650,6 +653,7 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     a.kb = (int)((k + (int64_t)kBlock - 1) / kBlock);
     a.out_kind = out_dtype;
     a.e5m2 = row_type == EW_E5M2;
+    a.words = !(((uintptr_t)x_scales | lds) & 3);
     a.wide = out_dtype != EW_FP32 && !(((uintptr_t)out & 15) | ((ldo | f) & 7));
     cudaStream_t st = (cudaStream_t)stream;
     if (rows <= 128ll * groups) return grad ? launch<1, 128, kInputGrad>(*d, ma, mb, a, st) : launch<1, 128, kProduct>(*d, ma, mb, a, st);

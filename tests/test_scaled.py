@@ -23,13 +23,13 @@ def test_scaled_mm_refuses(lib, fn):
     def mm(device=-1, dtype=E4M3, out_dtype=BF16, x=X, ldx=128, sx=SX, lds=4, w=W, ldw=128, gs=128 * 128, sw=SW, off=OFF, rows=8, groups=2, n=128, k=128, out=OUT, ldo=128):
         return getattr(lib, fn)(device, dtype, out_dtype, x, ldx, sx, lds, w, ldw, gs, sw, off, rows, groups, n, k, out, ldo, None)
 
-    good = [dict(), dict(dtype=E5M2, out_dtype=FP32), dict(out_dtype=FP16), dict(rows=0, x=None, sx=None, out=None), dict(groups=1, gs=0, off=None), dict(sw=SW + 1),
+    good = [dict(), dict(dtype=E5M2, out_dtype=FP32), dict(out_dtype=FP16), dict(rows=0, x=None, sx=None, out=None), dict(groups=1, gs=0, off=None), dict(sw=SW + 1), dict(sx=SX + 1, lds=5),
             dict(n=100, k=100, ldo=100), dict(gs=128, ldw=256)]
     for change in good:
         assert mm(**change) == NO_DEVICE, change
     bad = [dict(dtype=BF16), dict(dtype=FP32), dict(dtype=7), dict(out_dtype=E4M3), dict(out_dtype=-1), dict(rows=-1), dict(groups=0), dict(groups=2049), dict(n=0), dict(k=0),
            dict(off=None), dict(off=OFF + 2), dict(out=None), dict(out=OUT + 1), dict(out_dtype=FP32, out=OUT + 2), dict(x=None), dict(x=X + 8), dict(ldx=120), dict(ldx=136),
-           dict(sx=None), dict(sx=SX + 2), dict(lds=0), dict(lds=5), dict(w=None), dict(w=W + 8), dict(ldw=112), dict(ldw=130), dict(gs=128 * 127), dict(gs=128 * 128 + 8), dict(sw=None),
+           dict(sx=None), dict(lds=0), dict(w=None), dict(w=W + 8), dict(ldw=112), dict(ldw=130), dict(gs=128 * 127), dict(gs=128 * 128 + 8), dict(sw=None),
            dict(ldo=127)]
     for change in bad:
         assert mm(**change) == INVALID, change
