@@ -325,11 +325,13 @@ class _Torch:
         cls.eights = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
         cls.recording, cls.empty_like = torch.is_grad_enabled, torch.empty_like
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        lib()
         cls.ready = True
         return cls
 
 
 def _torch():
+    """Torch's constants; the library is loaded when they are."""
     return _Torch if _Torch.ready else _Torch.load()
 
 
@@ -617,7 +619,8 @@ def _row_blocks(out, rows, width, dtype, T, like):
     if out is None:
         wide, blocks = (width + 15) // 16 * 16, (width + 127) // 128
         room = (blocks + 3) // 4 * 4
-        q, scales = like.new_empty((rows, wide), dtype=dtype), like.new_empty((rows, room), dtype=T.exponent)
+        scales = like.new_empty((rows, room), dtype=T.exponent)
+        q = T.empty_like(like, dtype=dtype) if like.shape == (rows, wide) else like.new_empty((rows, wide), dtype=dtype)
         return q if wide == width else q[:, :width], scales if room == blocks else scales[:, :blocks], wide, room
     q, scales = out
     q, scales = _result(q, (rows, width), dtype, like, "q"), _result(scales, (rows, (width + 127) // 128), T.exponent, like, "scales")
@@ -636,7 +639,7 @@ def scaled_rows(x, dtype=None, out=None):
     to = _eight(T, dtype, "scaled_rows")
     rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
     q, scales, ldq, lds = _row_blocks(out, rows, width, dtype, T, x)
-    rc = lib().ew_scaled_rows(dev, code, to, x.data_ptr(), ldx, rows, width, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    rc = _lib.ew_scaled_rows(dev, code, to, x.data_ptr(), ldx, rows, width, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
     if rc:
         _check(rc, "ew_scaled_rows")
     return q, scales
@@ -658,14 +661,14 @@ def scaled_pack(w, out=None):
         if not scales.is_contiguous():
             raise ValueError("scales of weights are contiguous")
     ldq = q.stride(1) if n > 1 else k
-    rc = lib().ew_scaled_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, q.data_ptr(), ldq, q.stride(0) if slots > 1 else n * ldq, scales.data_ptr(),
+    rc = _lib.ew_scaled_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, q.data_ptr(), ldq, q.stride(0) if slots > 1 else n * ldq, scales.data_ptr(),
                               T.stream(dev))
     if rc:
         _check(rc, "ew_scaled_pack")
     return q, scales
 
 
-def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype, grad):
+def _scaled_product(where, a, a_scales, w, w_scales, offsets, out, out_dtype, grad):
     T, dev = _torch(), a.get_device()
     if (a.requires_grad or w.requires_grad) and T.recording():
         _recorded(where)
@@ -675,9 +678,9 @@ def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype
     if width != (n if grad else k):
         raise ValueError(f"rows of {width} do not match w of {tuple(w.shape)}")
     blocks, nb, kb = (width + 127) // 128, (n + 127) // 128, (k + 127) // 128
-    if not _good(a_scales, dev, T.exponent, 2):
+    if a_scales.get_device() != dev or a_scales.dtype is not T.exponent:
         _on(a_scales, a, 2, "the rows' scales", T.exponent)
-    if not _good(w_scales, dev, T.exponent, 3):
+    if w_scales.get_device() != dev or w_scales.dtype is not T.exponent:
         _on(w_scales, a, 3, "w's scales", T.exponent)
     if a_scales.shape != (rows, blocks) or (blocks > 1 and rows and a_scales.stride(1) != 1):
         raise ValueError(f"the rows' scales: ({rows}, {blocks}), a row's side by side, are wanted, got {tuple(a_scales.shape)}")
@@ -708,6 +711,7 @@ def _scaled_product(fn, where, a, a_scales, w, w_scales, offsets, out, out_dtype
     else:
         _result(out, (rows, wide), out_dtype, a)
         ldo = out.stride(0) if rows > 1 else wide
+    fn = _lib.ew_scaled_mm_dx if grad else _lib.ew_scaled_mm
     rc = fn(dev, row_type, code, a.data_ptr(), lda, a_scales.data_ptr(), lds, w.data_ptr(), ldw, stride, w_scales.data_ptr(), offsets_at, rows, groups, n, k,
             out.data_ptr(), ldo, T.stream(dev))
     if rc:
@@ -719,13 +723,13 @@ def scaled_mm(x, x_scales, w, w_scales, offsets=None, out=None, out_dtype=None):
     """y[r] = x[r] w[g]^T of the values that 8-bit blocks stand for, for the rows offsets[g] <= r < offsets[g+1] of each group: x, x_scales
     from `scaled_rows`, `rms_norm_scaled` or `swiglu_scaled`, w, w_scales from `scaled_pack`.  offsets None: one matrix, all
     rows.  out_dtype: bfloat16 (default), float16 or float32.  Rows outside the offsets as in `grouped_mm`."""
-    return _scaled_product(lib().ew_scaled_mm, "ew_scaled_mm", x, x_scales, w, w_scales, offsets, out, out_dtype, False)
+    return _scaled_product("ew_scaled_mm", x, x_scales, w, w_scales, offsets, out, out_dtype, False)
 
 
 def scaled_mm_dx(dy, dy_scales, w, w_scales, offsets=None, out=None, out_dtype=None):
     """The gradient of `scaled_mm` with respect to x's values: dx[r] = dy[r] w[g]; dy, dy_scales [rows, n] from `scaled_rows`, often in
     float8_e5m2.  (The weights' gradient: `grouped_mm_dw` of the 16-bit rows.)"""
-    return _scaled_product(lib().ew_scaled_mm_dx, "ew_scaled_mm_dx", dy, dy_scales, w, w_scales, offsets, out, out_dtype, True)
+    return _scaled_product("ew_scaled_mm_dx", dy, dy_scales, w, w_scales, offsets, out, out_dtype, True)
 
 
 def swiglu_scaled(h, row_weights=None, out=None):
@@ -739,17 +743,20 @@ def swiglu_scaled(h, row_weights=None, out=None):
         raise ValueError(f"h holds a gate and an up block side by side: an even width is wanted, got {two}")
     p = _row_weights(row_weights, dev, T, rows, h)
     q, scales, ldq, lds = _row_blocks(out, rows, two // 2, T.e4m3, T, h)
-    rc = lib().ew_swiglu_scaled(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, two // 2, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    rc = _lib.ew_swiglu_scaled(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, two // 2, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
     if rc:
         _check(rc, "ew_swiglu_scaled")
     return q, scales
 
 
 def _norm_operands(x, weight, T, dev):
-    code = _code(T, x.dtype)
-    rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
-    if weight.get_device() != dev or weight.dtype is not x.dtype or weight.dim() != 1 or weight.shape[0] != width or not weight.is_contiguous():
-        _on(weight, x, 1, "weight", x.dtype)
+    dtype = x.dtype
+    code = T.codes.get(dtype)
+    if code is None:
+        _code(T, dtype)
+    rows, width, ldx = _matrix(x, dev, dtype, "x", None)
+    if weight.get_device() != dev or weight.dtype is not dtype or weight.shape != (width,) or not weight.is_contiguous():
+        _on(weight, x, 1, "weight", dtype)
         raise ValueError(f"weight: a contiguous tensor of {width} is wanted, got {tuple(weight.shape)}")
     return code, rows, width, ldx
 
@@ -762,10 +769,10 @@ def _beside(t, rows, width, name, like, dev):
     return t.data_ptr(), ld
 
 
-def _like(out, rows, width, name, like, T):
+def _like(out, rows, width, name, like):
     """(tensor, elements between rows) of a result that has x's shape and type."""
     if out is None:
-        return T.empty_like(like), width
+        return _Torch.empty_like(like), width
     _result(out, (rows, width), like.dtype, like, name)
     return out, out.stride(0) if rows > 1 else width
 
@@ -782,15 +789,15 @@ def _norm(x, weight, residual, eps, y, with_y, blocks, with_blocks, total):
         q, scales, ldq, lds = _row_blocks(blocks, rows, width, T.e4m3, T, x)
         q_at, scales_at, got = q.data_ptr(), scales.data_ptr(), (q, scales)
     if with_y:
-        y, ldy = _like(y, rows, width, "out", x, T)
+        y, ldy = _like(y, rows, width, "out", x)
         y_at, got = y.data_ptr(), got + (y,)
     if residual is not None:
         res, ldr = _beside(residual, rows, width, "residual", x, dev)
-        total, ldt = _like(total, rows, width, "sum_out", x, T)
+        total, ldt = _like(total, rows, width, "sum_out", x)
         total_at, got = total.data_ptr(), got + (total,)
     elif total is not None:
         raise ValueError("sum_out is for the sum with a residual")
-    rc = lib().ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width, total_at, ldt, y_at, ldy, q_at, ldq, scales_at, lds, T.stream(dev))
+    rc = _lib.ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width, total_at, ldt, y_at, ldy, q_at, ldq, scales_at, lds, T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm")
     return got[0] if len(got) == 1 else got
@@ -820,11 +827,10 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     code, rows, width, ldt = _norm_operands(t, weight, T, dev)
     dy_at, lddy = _beside(dy, rows, width, "dy", t, dev)
     dt_at, lddt = (None, 0) if dt is None else _beside(dt, rows, width, "dt", t, dev)
-    out, ldo = _like(out, rows, width, "out", t, T)
-    fn = lib()
-    parts = fn.ew_rms_norm_grad_parts(rows, width)
+    out, ldo = _like(out, rows, width, "out", t)
+    parts = _lib.ew_rms_norm_grad_parts(rows, width)
     dw, room = weight.new_empty((width,), dtype=T.float32), weight.new_empty((parts, width), dtype=T.float32)
-    rc = fn.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
+    rc = _lib.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
                              T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm_grad")
