@@ -2,6 +2,8 @@
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -28,12 +30,19 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
-    cmd = [_nvcc(), "-shared", "-Xcompiler", "-fPIC", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
-           "-std=c++17", "-cudart", "static", "-o", LIB + ".tmp"]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    compile_ = [_nvcc(), "-c", "-Xcompiler", "-fPIC", *arch, "-lineinfo", "-O3", "-std=c++17", "-cudart", "static"]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.run(cmd, check=True)
+        compile_ += ["-Xptxas", "-v"]
+    with tempfile.TemporaryDirectory() as objects:
+        def one(source):
+            target = os.path.join(objects, source + ".o")
+            subprocess.run([*compile_, "-o", target, os.path.join(CSRC, source)], check=True)
+            return target
+
+        with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as pool:    # a file each
+            targets = list(pool.map(one, SOURCES))
+        subprocess.run([_nvcc(), "-shared", "-Xcompiler", "-fPIC", *arch, "-cudart", "static", "-o", LIB + ".tmp", *targets], check=True)
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

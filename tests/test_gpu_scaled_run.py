@@ -142,6 +142,33 @@ def test_backward_captured_while_an_eager_graph_lives():
     assert leaves[0].grad.isfinite().all()
 
 
+def test_training_step_captured():
+    """Forward and backward through autograd in a graph: replays give the eager step's gradients."""
+    leaves, offsets, g_out, g_t = training_leaves()
+
+    def step():
+        for v in leaves:
+            v.grad = None
+        torch.autograd.backward(Experts.apply(*leaves, offsets), (g_out, g_t))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    eager = [v.grad.clone() for v in leaves]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for v in leaves:
+        v.grad.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(v.grad, e) for v, e in zip(leaves, eager))
+
+
 def every_operator(seed=0):
     """One call of each, and their results as bits."""
     x, r, w = uneven((300, 512), BF16, seed + 1), uneven((300, 512), BF16, seed + 2), randn((512,), BF16, seed + 3)
