@@ -66,9 +66,9 @@ __global__ void __launch_bounds__(kThreads, VEC && W == 1 ? 5 : 1) rows_kernel(c
                         Two up[4];
                         to_pairs(up, u[k]);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] = mul2(silu(v[j]), up[j]);
+                        for (int j = 0; j < 4; ++j) v[j] = mul2(mul2(silu(v[j]), up[j]), two(p, p));
                     }
-                    put_span<VEC, E5M2>(v, p, q, scales, at, lane, a.width);
+                    put_span<VEC, E5M2>(v, q, scales, at, lane, a.width);
                 }
             }
         }

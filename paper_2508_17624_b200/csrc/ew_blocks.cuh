@@ -123,12 +123,12 @@ __device__ __forceinline__ void store_span(const Eight<T> &o, T *row, int at, in
     }
 }
 
-// Writes the span p v as two blocks (p: the same for the whole row).  The whole warp calls it.
+// Writes a span as two blocks.  The whole warp calls it.
 template <bool VEC, bool E5M2>
-__device__ __forceinline__ void put_span(Two (&v)[4], float p, uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
+__device__ __forceinline__ void put_span(Two (&v)[4], uint8_t *q_row, uint8_t *scale_row, int at, int lane, int width) {
     constexpr int kFirst = VEC ? 4 : 2;                // of the lane's pairs, those of its first block
     float m0, m1;
-    auto most = [&] {                                  // rounding keeps the order: the largest |p v| is |p| times the largest |v|
+    auto most = [&] {
         m0 = m1 = 0.f;
 #pragma unroll
         for (int j = 0; j < kFirst; ++j) m0 = max_abs(m0, v[j]);
@@ -139,23 +139,20 @@ __device__ __forceinline__ void put_span(Two (&v)[4], float p, uint8_t *q_row, u
             m0 = fmaxf(m0, __shfl_xor_sync(kAll, m0, d));
             if (!VEC) m1 = fmaxf(m1, __shfl_xor_sync(kAll, m1, d));
         }
-        m0 *= fabsf(p);
-        m1 *= fabsf(p);
     };
     most();
     if (__any_sync(kAll, not_finite(m0) || not_finite(m1))) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float2 f = parts_of(mul2(v[j], two(p, p)));
+            float2 f = parts_of(v[j]);
             if (not_finite(f.x)) f.x = __int_as_float(0x7fffffff);
             if (not_finite(f.y)) f.y = __int_as_float(0x7fffffff);
             v[j] = two(f.x, f.y);
         }
-        p = 1.f;
         most();
     }
     const uint32_t c0 = scale_code(m0, kTop<E5M2>), c1 = VEC ? c0 : scale_code(m1, kTop<E5M2>);
-    const float i0 = p * inverse_scale(c0), i1 = VEC ? i0 : p * inverse_scale(c1);       // (a power of two: v (p f) is (v p) f)
+    const float i0 = inverse_scale(c0), i1 = VEC ? i0 : inverse_scale(c1);
     uint32_t pair[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
                 y.v[2 * j + 1] = from_f<T>(f.y);
             }
             if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
-            if (a.q && at < a.width) put_span<VEC, false>(tv, 1.f, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
+            if (a.q && at < a.width) put_span<VEC, false>(tv, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
         }
     }
 }
@@ -127,8 +127,8 @@ struct GradArgs {
 };
 
 // A row a CTA of W warps at a time, its columns' sums in the registers of the threads that own them.  BULK: rows come to shared memory by bulk
-// copies, kStages of them ahead of the one that is worked on; without it a CTA's loads wait for the row before (30 us for 8192
-// rows of 2048, with the copies TIME).  Needs rows on 16-byte boundaries of a multiple of eight values.
+// copies, up to kMostStages of them ahead of the one that is worked on; without them a CTA's loads wait for the row before.  Needs rows on
+// 16-byte boundaries of a multiple of eight values.
 template <class T, bool BULK, int W, int NV>
 __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel(const GradArgs a) {
     tc::pdl_launch_dependents();

@@ -349,3 +349,18 @@ def test_swiglu(rows, inter, pad, weights, dtype):
     q, s = binding.swiglu_scaled(h, p)
     # the fast exponential and division: 2 + 1.2 |g| steps of 2^-23, two more for the division and a handful of products: 20 for |g| < 8
     blocks_near(q, s, ref, 20 * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("inter", [256, 200, 131])
+def test_swiglu_large_weights_and_zeros(inter):
+    """Row weights above one beside blocks of zeros and of the smallest numbers, weights of zero beside infinities."""
+    h = randn((7, 2 * inter), BF16, 1).clamp_(-7.9, 7.9)
+    p = torch.tensor([3.0, 100.0, 1e30, 2.5, 0.0, -4.0, 1e-30], device="cuda")
+    h[0], h[1, :128], h[2, inter:] = 0, 0, 1e-37
+    q, s = binding.swiglu_scaled(h, p)
+    g, u = h.double().chunk(2, dim=1)
+    ref = g * torch.sigmoid(g) * u * p.double()[:, None]
+    blocks_near(q, s, ref, 20 * 2.0 ** -23)
+    h[4, 5] = float("inf")                              # times a weight of zero
+    q, s = binding.swiglu_scaled(h, p)
+    assert q[4, 5].float().isnan() and q[4, 6:].float().isfinite().all() and not q[4, 6:].float().any()
