@@ -404,8 +404,8 @@ ew_status_t ew_swiglu_grad(int32_t device, int32_t dtype, const void *dact, int6
  *            rows: a scale for 128 neighbouring values of a row (the last of a row may be shorter)
  *   weights  q [n_slots, n, k], scales [n_slots, ceil(n / 128), ceil(k / 128)] without gaps: a scale for 128 x 128 values
  * The products below read q from 16-byte aligned rows (ldq and strides multiples of 16) and take scales at any address, those of rows
- * fastest from 4-byte boundaries; the operators that write blocks take any strides.  Bytes behind a row's end are neither
- * read nor written. */
+ * fastest from 4-byte boundaries; the operators that write blocks take any strides.  Nothing behind a row's end is written, and
+ * nothing used: of scales on 4-byte boundaries the whole of a row's last word is read. */
 
 /* Rows x [rows, width] (bf16 or fp16) as blocks of q_type. */
 ew_status_t ew_scaled_rows(int32_t device, int32_t dtype, int32_t q_type, const void *x, int64_t ldx, int32_t rows, int32_t width,

@@ -447,7 +447,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     const uint8_t *p = a.row_scales + (long long)(it.row0 + min(lane + 32 * j, it.cols - 1)) * a.lds + kb;
                     word[j] = 0;
                     if (32 * j < it.cols) {
-                        if (a.words && left == 4) {
+                        if (a.words) {                 // (what a row's last word holds behind its end is not used)
                             word[j] = *reinterpret_cast<const uint32_t *>(p);
                         } else {
 #pragma unroll
@@ -472,7 +472,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ epilogue (both CTAs)
-        const int lg = warp & 3;                       // the TMEM lanes this warp may read
+        const int lg = warp & 3, half = (warp - 2) >> 2;     // the TMEM lanes this warp may read; its columns
         uint32_t acc = 0, acc_phases = 0;
         bool ok = true;
         for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
@@ -491,7 +491,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     const bool last = kb + it.chunk >= it.kb;
                     const uint32_t t_sum = lanes + (acc ^ 1) * NT;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < it.cols; c0 += 32) {
+                    for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * kEpilogueWarps) {
                         uint32_t v[32], sum[32];
                         tc_ld32(t0 + c0, v);
                         tc_ld32(t_sum + c0, sum);
@@ -507,16 +507,16 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 if (a.wide) {
                     const int f_left = a.f_size - (f - lane);
                     uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + at - lane;
-                    uint8_t *stage = staging + lg * 2048;
+                    uint8_t *stage = staging + (warp - 2) * 2048;
                     if (f_left > 0)
 #pragma unroll 1
-                        for (int c0 = 0; c0 < to_store; c0 += 32) {
+                        for (int c0 = 32 * half; c0 < to_store; c0 += 8 * kEpilogueWarps) {
                             if (a.out_kind == EW_BF16) store_wide<true>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
                             else store_wide<false>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
                         }
                 } else {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < to_store; c0 += 32) {
+                    for (int c0 = 32 * half; c0 < to_store; c0 += 8 * kEpilogueWarps) {
                         uint32_t v[32];
                         tc_ld32(t0 + c0, v);           // columns behind the item's last are in the accumulator set, not stored
                         tc_wait_ld();
