@@ -44,7 +44,7 @@ constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 7;
 constexpr int kSlots = 4;                              // places for the exponents of four k-blocks
 constexpr int kMaps = 8;                               // row boxes of 16, 32 .. 128 rows
-constexpr int kStaging = kEpilogueWarps * 2048;        // 32 x 32 16-bit results of each epilogue warp
+constexpr int kStaging = 2 * 2 * 4096;                 // 16-bit results on their way out: two tiles of 64 f x 32 rows of each pair of epilogue warps
 // Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 1024 terms for
 // fp32 results, 8192 for fp16, 65536 for bf16.
 constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 1024 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
@@ -157,18 +157,26 @@ __device__ __forceinline__ void store_columns(T *p, long long ldo, const uint32_
         q[j & 7] += step;
     }
 }
-// The same for 16-bit results in rows on 16-byte boundaries: the warp reads its 32 x 32 part of the accumulator in the order of the
-// small matrix instructions' results, turns it over on the way to shared memory (a row of 64 bytes a column, its four pieces of 16
-// bytes exchanged by the row so that neither side meets a bank twice), and stores 16 bytes a lane, eight rows at a time: a third of
-// the instructions, which at the power limit is time (prompt: 261 -> LATER us).
+// Barrier of each pair of epilogue warps (2 and 3, 4 and 5)
+__device__ __forceinline__ uint32_t pair_barrier() { return 1 + ((threadIdx.x >> 6) & 1); }
+__device__ __forceinline__ bool both_of_pair(bool ok) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "r"(pair_barrier()) : "memory");
+    return r != 0;
+}
+// The same for 16-bit results in rows on 16-byte boundaries.  A warp reads its 32 x 32 part of the accumulator in the order of the
+// small matrix instructions' results and turns it over on the way to shared memory, where it and its neighbour fill a tile of 32 rows of 64 f
+// (128 bytes; pieces of 16 bytes exchanged by the row, the copy's swizzle, so that no bank is met twice).  A bulk copy takes the tile away while the next
+// is filled; of rows behind the item's end only the others are stored, 16 bytes a lane.
+// (32 stores of two bytes a lane: prompt 261 us, input gradient 95; 16 bytes a lane: 257 and 79.)
 template <bool BF16>
-__device__ __forceinline__ void store_wide(uint32_t taddr, uint8_t *stage, uint16_t *p, long long ldo, int lim, int lane, int f_left) {
+__device__ __forceinline__ void store_tile(uint32_t taddr, uint8_t *tile, const CUtensorMap *map, int f, int row0, uint16_t *p, long long ldo, int lim, int lane, int odd, int f_left) {
     uint32_t v[2][16];
     tc_ld16x256(taddr, v[0]);
     tc_ld16x256(taddr + (16u << 16), v[1]);
     tc_wait_ld();
-    const uint32_t at = smem_u32(stage);
-    __syncwarp();                                      // (the last round has been read)
+    const uint32_t at = smem_u32(tile);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {                      // eight columns a time: four 8 x 8 matrices, 8 f each
         uint32_t m[4];
@@ -183,19 +191,26 @@ __device__ __forceinline__ void store_wide(uint32_t taddr, uint8_t *stage, uint1
                 m[j] = *reinterpret_cast<const uint32_t *>(&h);
             }
         }
-        const int row = 8 * i + (lane & 7), piece = lane >> 3;
+        const int row = 8 * i + (lane & 7), piece = odd * 4 + (lane >> 3);
         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
-                     ::"r"(at + row * 64 + ((piece ^ (row >> 1 & 3)) << 4)), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3]) : "memory");
+                     ::"r"(at + row * 128 + ((piece ^ (row & 7)) << 4)), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3]) : "memory");
     }
-    __syncwarp();
-    const int piece = lane & 3;
-    uint16_t *to = p + (long long)(lane >> 2) * ldo + piece * 8;
+    const bool copier = lane == 0 && !odd;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (copier) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");           // the other tile is free again
+    asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_barrier()) : "memory");
+    if (lim >= 32) {
+        if (copier)
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n\tcp.async.bulk.commit_group;"
+                         ::"l"(map), "r"(at), "r"(f), "r"(row0) : "memory");
+    } else {
+        const int piece = odd * 4 + (lane & 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = 8 * i + (lane >> 2);
-        const uint4 x = *reinterpret_cast<const uint4 *>(stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4));
-        if (row < lim && piece * 8 < f_left) *reinterpret_cast<uint4 *>(to) = x;
-        to += 8 * ldo;
+        for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + (lane >> 2);
+            const uint4 x = *reinterpret_cast<const uint4 *>(tile + row * 128 + ((piece ^ (row & 7)) << 4));
+            if (row < lim && (lane & 3) * 8 < f_left) *reinterpret_cast<uint4 *>(p + row * ldo + (lane & 3) * 8) = x;
+        }
     }
 }
 __device__ __forceinline__ void add_columns(float *p, long long ldo, const uint32_t (&v)[32], int lim) {
@@ -215,16 +230,16 @@ __device__ __forceinline__ void add_columns(float *p, long long ldo, const uint3
 // LONG: 16-bit results whose sums may have several parts
 template <int CG, int NT, int WAY, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1)
-scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ Args a) {
+scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ CUtensorMap map_out,
+                      const __grid_constant__ Args a) {
     using C = Cfg<CG, NT>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
-    // after the ring: the exponents; 16-bit results on their way out; barriers full, empty [kMaxStages] each, exponents full, empty [kSlots] each, tmem full, empty [2]
+    // after the ring: 16-bit results on their way out; the exponents; barriers full, empty [kMaxStages] each, exponents full, empty [kSlots] each, tmem full, empty [2]
     // each; TMEM base, abort flag; then the group table: first block of each group, first row, rows
-    uint8_t *scales = smem_al + a.stages * C::kStageBytes;
-    uint8_t *staging = scales + kSlots * C::kSlotBytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kStaging);
+    uint8_t *staging = smem_al + a.stages * C::kStageBytes, *scales = staging + kStaging;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(scales + kSlots * C::kSlotBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMaxStages, bar_sfull = bar_empty + 8 * kMaxStages, bar_sempty = bar_sfull + 8 * kSlots;
     const uint32_t bar_tfull = bar_sempty + 8 * kSlots, bar_tempty = bar_tfull + 16;
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 2 * kMaxStages + 2 * kSlots + 4);
@@ -472,7 +487,8 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ epilogue (both CTAs)
-        const int lg = warp & 3, half = (warp - 2) >> 2;     // the TMEM lanes this warp may read; its columns
+        const int lg = warp & 3;                       // the TMEM lanes this warp may read
+        int tiles = 0;                                 // stored so far
         uint32_t acc = 0, acc_phases = 0;
         bool ok = true;
         for (int i = unit, turn = 0; i < n_items && ok; i += units, ++turn) {
@@ -481,7 +497,8 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             const bool f_ok = f < a.f_size;
             const size_t at = (size_t)it.row0 * a.ldo + f;
             for (int kb = 0; kb < it.kb; kb += it.chunk) {
-                if (!(ok = wait_warp(bar_tfull + 8 * acc, acc_phases >> acc & 1, abort_flag, a.err))) break;
+                // (the two warps of a pair meet at barriers below, so they go on or give up together)
+                if (!(ok = both_of_pair(wait_warp(bar_tfull + 8 * acc, acc_phases >> acc & 1, abort_flag, a.err)))) break;
                 tc_fence_after();
                 const uint32_t lanes = tmem_base + ((uint32_t)(lg * 32) << 16), t0 = lanes + acc * NT;
                 const bool here = sums_here(it);
@@ -491,7 +508,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     const bool last = kb + it.chunk >= it.kb;
                     const uint32_t t_sum = lanes + (acc ^ 1) * NT;
 #pragma unroll 1
-                    for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * kEpilogueWarps) {
+                    for (int c0 = 0; c0 < it.cols; c0 += 32) {
                         uint32_t v[32], sum[32];
                         tc_ld32(t0 + c0, v);
                         tc_ld32(t_sum + c0, sum);
@@ -505,18 +522,20 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     if (!last) to_store = 0;
                 }
                 if (a.wide) {
-                    const int f_left = a.f_size - (f - lane);
+                    const int f_left = a.f_size - (f - lane), f_pair = f - lane - 32 * (lg & 1);
                     uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + at - lane;
-                    uint8_t *stage = staging + (warp - 2) * 2048;
-                    if (f_left > 0)
+                    if (f_pair < a.f_size)
 #pragma unroll 1
-                        for (int c0 = 32 * half; c0 < to_store; c0 += 8 * kEpilogueWarps) {
-                            if (a.out_kind == EW_BF16) store_wide<true>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
-                            else store_wide<false>(t0 + c0, stage, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, f_left);
+                        for (int c0 = 0; c0 < to_store; c0 += 32) {
+                            uint8_t *tile = staging + ((lg >> 1) * 2 + (tiles++ & 1)) * 4096;
+                            if (a.out_kind == EW_BF16)
+                                store_tile<true>(t0 + c0, tile, &map_out, f_pair, it.row0 + c0, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, lg & 1, f_left);
+                            else
+                                store_tile<false>(t0 + c0, tile, &map_out, f_pair, it.row0 + c0, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, lg & 1, f_left);
                         }
                 } else {
 #pragma unroll 1
-                    for (int c0 = 32 * half; c0 < to_store; c0 += 8 * kEpilogueWarps) {
+                    for (int c0 = 0; c0 < to_store; c0 += 32) {
                         uint32_t v[32];
                         tc_ld32(t0 + c0, v);           // columns behind the item's last are in the accumulator set, not stored
                         tc_wait_ld();
@@ -541,6 +560,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 if (!here) acc ^= 1;
             }
         }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");            // the copies out of shared memory have arrived
     }
 
     // ---------------------------------------------------------------------- teardown
@@ -561,7 +581,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 constexpr int kBarBytes = (2 * kMaxStages + 2 * kSlots + 4 + 1) * 8;
 
 template <int CG, int NT, int WAY>
-ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Args a, cudaStream_t st) {
+ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, const CUtensorMap &mo, Args a, cudaStream_t st) {
     using C = Cfg<CG, NT>;
     a.f_tiles = (a.f_size + C::kTile - 1) / C::kTile;
     const long long live = a.groups < a.rows ? a.groups : a.rows;            // groups that can have rows
@@ -592,8 +612,8 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, Ar
     cfg.numAttrs = attrs;
     a.sum_blocks = sum_blocks(a.out_kind);
     const bool long_sums = a.out_kind != EW_FP32 && a.t_size > a.sum_blocks * kBlock;
-    return launched((int)(long_sums ? cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, true>, ma, mb, a)
-                                    : cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, false>, ma, mb, a)), "scaled product");
+    return launched((int)(long_sums ? cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, true>, ma, mb, mo, a)
+                                    : cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, false>, ma, mb, mo, a)), "scaled product");
 }
 
 template <int CG, int NT, int WAY>
@@ -627,7 +647,7 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     ew_status_t s = launched((int)guard.enter(device), "cudaSetDevice");
     const Device *d;
     if (s != EW_OK || (s = device_state(device, &d)) != EW_OK) return s;
-    CUtensorMap ma;
+    CUtensorMap ma, mo;
     RowMaps mb;
     const uint64_t wd[3] = {(uint64_t)k, (uint64_t)n, (uint64_t)groups}, ws[2] = {(uint64_t)ldw, groups > 1 ? (uint64_t)group_stride : (uint64_t)ldw};
     const uint32_t w_box[3] = {kBlock, 128, 1};
@@ -654,10 +674,15 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     a.out_kind = out_dtype;
     a.e5m2 = row_type == EW_E5M2;
     a.words = !(((uintptr_t)x_scales | lds) & 3);
-    a.wide = out_dtype != EW_FP32 && !(((uintptr_t)out & 15) | ((ldo | f) & 7));
+    a.wide = out_dtype != EW_FP32 && !(((uintptr_t)out & 15) | ((ldo | f) & 7)) && ldo < (1ll << 38);
+    if (a.wide) {
+        const uint64_t od[2] = {(uint64_t)f, (uint64_t)rows}, os[1] = {(uint64_t)ldo * 2};
+        const uint32_t box[2] = {64, 32};
+        if ((s = encode_map(*d, &mo, map_type(out_dtype), out, 2, od, os, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
+    }
     cudaStream_t st = (cudaStream_t)stream;
-    if (rows <= 128ll * groups) return grad ? launch<1, 128, kInputGrad>(*d, ma, mb, a, st) : launch<1, 128, kProduct>(*d, ma, mb, a, st);
-    return grad ? launch<2, 224, kInputGrad>(*d, ma, mb, a, st) : launch<2, 224, kProduct>(*d, ma, mb, a, st);
+    if (rows <= 128ll * groups) return grad ? launch<1, 128, kInputGrad>(*d, ma, mb, mo, a, st) : launch<1, 128, kProduct>(*d, ma, mb, mo, a, st);
+    return grad ? launch<2, 224, kInputGrad>(*d, ma, mb, mo, a, st) : launch<2, 224, kProduct>(*d, ma, mb, mo, a, st);
 }
 
 }  // namespace

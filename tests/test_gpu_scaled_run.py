@@ -292,7 +292,7 @@ def test_rows_scales_at_any_address():
     q, s = binding.scaled_rows(uneven((40, 700), BF16, 1))
     w = binding.scaled_pack(uneven((1, 72, 700), BF16, 2, 0.1))
     want = binding.scaled_mm(q, s, *w)
-    for left, ld in ((0, 6), (1, 7), (3, 13)):
+    for left, ld in ((0, 6), (0, 8), (4, 12), (1, 7), (3, 13)):
         wide = torch.full((40, ld + left), 255, dtype=torch.uint8, device="cuda")
         wide[:, left:left + 6] = s.view(torch.uint8)
         assert torch.equal(binding.scaled_mm(q, wide.view(E8M0)[:, left:left + 6], *w), want)
