@@ -36,15 +36,13 @@ using namespace tc;
 enum Way { kProduct = 0, kInputGrad = 1 };
 
 constexpr int kBlock = 128;                            // values a scale; bytes of a stage's row
-constexpr int kEpilogueWarps = 4;
-constexpr int kThreads = (3 + kEpilogueWarps) * 32;    // TMA, MMA, epilogue, scales
-constexpr int kScaleWarp = 2 + kEpilogueWarps;
+constexpr int threads_of(int epilogue_warps) { return (3 + epilogue_warps) * 32; }       // TMA, MMA, epilogue, scales
 constexpr int kATile = 128 * kBlock;                   // 16 KiB: 128 f of one stage
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 7;
 constexpr int kSlots = 4;                              // places for the exponents of four k-blocks
 constexpr int kMaps = 8;                               // row boxes of 16, 32 .. 128 rows
-constexpr int kStaging = 2 * 2 * 4096;                 // 16-bit results on their way out: two tiles of 64 f x 32 rows of each pair of epilogue warps
+constexpr int kTiles = 2;                              // 16-bit results on their way out: tiles of 64 f x 32 rows of each pair of epilogue warps
 // Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 1024 terms for
 // fp32 results, 8192 for fp16, 65536 for bf16.
 constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 1024 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
@@ -67,8 +65,11 @@ struct Args {
     int stages;
 };
 
-template <int CG, int NT>
+// CG: CTAs that share one MMA tile (1, or 2 = a pair with 256 f); NT: columns of an accumulator set; EW: epilogue warps, four or
+// eight (two to each quarter of the TMEM lanes, taking turns at the columns)
+template <int CG, int NT, int EW>
 struct Cfg {
+    static constexpr int kThreads = (3 + EW) * 32, kScaleWarp = 2 + EW, kStaging = EW / 2 * kTiles * 4096;
     static constexpr int kBRows = NT / CG;             // c staged by each CTA
     static constexpr int kStageBytes = kATile + kBRows * kBlock;
     static constexpr int kTile = 128 * CG;             // f of an item
@@ -157,8 +158,9 @@ __device__ __forceinline__ void store_columns(T *p, long long ldo, const uint32_
         q[j & 7] += step;
     }
 }
-// Barrier of each pair of epilogue warps (2 and 3, 4 and 5)
-__device__ __forceinline__ uint32_t pair_barrier() { return 1 + ((threadIdx.x >> 6) & 1); }
+// Pairs of epilogue warps: 2 and 3, 4 and 5 ..., and their barriers
+__device__ __forceinline__ uint32_t pair_index() { return (threadIdx.x >> 6) - 1; }
+__device__ __forceinline__ uint32_t pair_barrier() { return 1 + pair_index(); }
 __device__ __forceinline__ bool both_of_pair(bool ok) {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
@@ -197,7 +199,7 @@ __device__ __forceinline__ void store_tile(uint32_t taddr, uint8_t *tile, const 
     }
     const bool copier = lane == 0 && !odd;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    if (copier) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");           // the other tile is free again
+    if (copier) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kTiles - 2) : "memory");      // the next tile is free again
     asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_barrier()) : "memory");
     if (lim >= 32) {
         if (copier)
@@ -227,18 +229,18 @@ __device__ __forceinline__ void add_columns(float *p, long long ldo, const uint3
     }
 }
 
-// LONG: 16-bit results whose sums may have several parts
-template <int CG, int NT, int WAY, bool LONG>
-__global__ void __launch_bounds__(kThreads, 1)
+// LONG: 16-bit results whose sums may have several parts (more than 8192 terms: four epilogue warps)
+template <int CG, int NT, int EW, int WAY, bool LONG>
+__global__ void __launch_bounds__(threads_of(EW), 1)
 scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ RowMaps map_b, const __grid_constant__ CUtensorMap map_out,
                       const __grid_constant__ Args a) {
-    using C = Cfg<CG, NT>;
+    using C = Cfg<CG, NT, EW>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
     // after the ring: 16-bit results on their way out; the exponents; barriers full, empty [kMaxStages] each, exponents full, empty [kSlots] each, tmem full, empty [2]
     // each; TMEM base, abort flag; then the group table: first block of each group, first row, rows
-    uint8_t *staging = smem_al + a.stages * C::kStageBytes, *scales = staging + kStaging;
+    uint8_t *staging = smem_al + a.stages * C::kStageBytes, *scales = staging + C::kStaging;
     uint64_t *bars = reinterpret_cast<uint64_t *>(scales + kSlots * C::kSlotBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMaxStages, bar_sfull = bar_empty + 8 * kMaxStages, bar_sempty = bar_sfull + 8 * kSlots;
     const uint32_t bar_tfull = bar_sempty + 8 * kSlots, bar_tempty = bar_tfull + 16;
@@ -261,7 +263,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_tfull + 8 * i, 1);
-            mbar_init(bar_tempty + 8 * i, kEpilogueWarps * CG);
+            mbar_init(bar_tempty + 8 * i, EW * CG);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -441,7 +443,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 }
             }
         }
-    } else if (warp == kScaleWarp) {
+    } else if (warp == C::kScaleWarp) {
         // ------------------------------------------------------------------ exponents (both CTAs)
         uint32_t slot = 0, phase = 0;
         bool ok = true;
@@ -487,7 +489,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ epilogue (both CTAs)
-        const int lg = warp & 3;                       // the TMEM lanes this warp may read
+        const int lg = warp & 3, half = (warp - 2) >> 2;     // the TMEM lanes this warp may read; its columns
         int tiles = 0;                                 // stored so far
         uint32_t acc = 0, acc_phases = 0;
         bool ok = true;
@@ -508,7 +510,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     const bool last = kb + it.chunk >= it.kb;
                     const uint32_t t_sum = lanes + (acc ^ 1) * NT;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < it.cols; c0 += 32) {
+                    for (int c0 = 32 * half; c0 < it.cols; c0 += 8 * EW) {
                         uint32_t v[32], sum[32];
                         tc_ld32(t0 + c0, v);
                         tc_ld32(t_sum + c0, sum);
@@ -526,8 +528,8 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + at - lane;
                     if (f_pair < a.f_size)
 #pragma unroll 1
-                        for (int c0 = 0; c0 < to_store; c0 += 32) {
-                            uint8_t *tile = staging + ((lg >> 1) * 2 + (tiles++ & 1)) * 4096;
+                        for (int c0 = 32 * half; c0 < to_store; c0 += 8 * EW) {
+                            uint8_t *tile = staging + (pair_index() * kTiles + tiles++ % kTiles) * 4096;
                             if (a.out_kind == EW_BF16)
                                 store_tile<true>(t0 + c0, tile, &map_out, f_pair, it.row0 + c0, out + (size_t)c0 * a.ldo, a.ldo, it.cols - c0, lane, lg & 1, f_left);
                             else
@@ -535,7 +537,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                         }
                 } else {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < to_store; c0 += 32) {
+                    for (int c0 = 32 * half; c0 < to_store; c0 += 8 * EW) {
                         uint32_t v[32];
                         tc_ld32(t0 + c0, v);           // columns behind the item's last are in the accumulator set, not stored
                         tc_wait_ld();
@@ -580,19 +582,19 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 
 constexpr int kBarBytes = (2 * kMaxStages + 2 * kSlots + 4 + 1) * 8;
 
-template <int CG, int NT, int WAY>
+template <int CG, int NT, int EW, int WAY>
 ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, const CUtensorMap &mo, Args a, cudaStream_t st) {
-    using C = Cfg<CG, NT>;
+    using C = Cfg<CG, NT, EW>;
     a.f_tiles = (a.f_size + C::kTile - 1) / C::kTile;
     const long long live = a.groups < a.rows ? a.groups : a.rows;            // groups that can have rows
     const long long max_items = (live + a.rows / NT) * a.f_tiles;
     if (max_items > 0x7fff0000) return refuse("scaled product: too many output tiles");
-    const int rest = 1024 + kSlots * C::kSlotBytes + kStaging + kBarBytes + (3 * a.groups + 1) * 4, fit = (kSmemLimit - rest) / C::kStageBytes;
+    const int rest = 1024 + kSlots * C::kSlotBytes + C::kStaging + kBarBytes + (3 * a.groups + 1) * 4, fit = (kSmemLimit - rest) / C::kStageBytes;
     a.stages = fit < kMaxStages ? fit : kMaxStages;
     cudaLaunchConfig_t cfg = {};
     const long long units = d.sm_count / CG;
     cfg.gridDim = dim3((unsigned)(CG * (max_items < units ? max_items : units)));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(C::kThreads);
     cfg.dynamicSmemBytes = (size_t)a.stages * C::kStageBytes + rest;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -612,14 +614,14 @@ ew_status_t launch(const Device &d, const CUtensorMap &ma, const RowMaps &mb, co
     cfg.numAttrs = attrs;
     a.sum_blocks = sum_blocks(a.out_kind);
     const bool long_sums = a.out_kind != EW_FP32 && a.t_size > a.sum_blocks * kBlock;
-    return launched((int)(long_sums ? cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, true>, ma, mb, mo, a)
-                                    : cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, WAY, false>, ma, mb, mo, a)), "scaled product");
+    return launched((int)(EW == 4 && long_sums ? cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, EW, WAY, EW == 4>, ma, mb, mo, a)
+                                    : cudaLaunchKernelEx(&cfg, scaled_product_kernel<CG, NT, EW, WAY, false>, ma, mb, mo, a)), "scaled product");
 }
 
-template <int CG, int NT, int WAY>
+template <int CG, int NT, int EW, int WAY>
 int setup_one() {
-    return (int)cudaFuncSetAttribute(scaled_product_kernel<CG, NT, WAY, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
-           (int)cudaFuncSetAttribute(scaled_product_kernel<CG, NT, WAY, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    return (int)cudaFuncSetAttribute(scaled_product_kernel<CG, NT, EW, WAY, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) |
+           (int)cudaFuncSetAttribute(scaled_product_kernel<CG, NT, EW, WAY, EW == 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
 }
 
 // A row-major matrix of bytes whose rows keep every TMA copy on a 16-byte boundary
@@ -681,14 +683,24 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
         if ((s = encode_map(*d, &mo, map_type(out_dtype), out, 2, od, os, box, CU_TENSOR_MAP_SWIZZLE_128B)) != EW_OK) return s;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (rows <= 128ll * groups) return grad ? launch<1, 128, kInputGrad>(*d, ma, mb, mo, a, st) : launch<1, 128, kProduct>(*d, ma, mb, mo, a, st);
-    return grad ? launch<2, 224, kInputGrad>(*d, ma, mb, mo, a, st) : launch<2, 224, kProduct>(*d, ma, mb, mo, a, st);
+#define EW_LAUNCH(CG, NT, EW) (grad ? launch<CG, NT, EW, kInputGrad>(*d, ma, mb, mo, a, st) : launch<CG, NT, EW, kProduct>(*d, ma, mb, mo, a, st))
+    // One CTA with 128 columns against the pair: 64 groups of 2816 x 2048 with 96 rows each 69.4 and 69.8 us, 128 rows 73.0 and 72.7, 144 rows 95.7
+    // and 75.7; where the pairs' tiles would not fill the GPU (8 groups of 1024 x 512, 160 rows each) 6.7 and 7.5.  (The host
+    // knows only how many groups there are, not which have rows: over many empty ones the one-CTA form may be taken where the pair would
+    // be faster.)
+    const long long live = groups < rows ? groups : rows, pair_tiles = (live + rows / 224) * ((f + 255) / 256);
+    if (rows <= 128ll * groups || pair_tiles <= d->sm_count / 2) return EW_LAUNCH(1, 128, 4);
+    // Short sums: the results' way out is what counts, and eight warps walk it (20000 rows, 16 groups, n = 1408; k = 256: 19.6 us
+    // against 23.8, 512: 22.4 and 25.8, 1024: 31.5 and 32.3); long ones: at the power limit four cost less (2048, 49152 rows: 285 and 289).
+    return t <= 1024 ? EW_LAUNCH(2, 224, 8) : EW_LAUNCH(2, 224, 4);
+#undef EW_LAUNCH
 }
 
 }  // namespace
 
 int scaled_setup() {
-    return setup_one<1, 128, kProduct>() | setup_one<1, 128, kInputGrad>() | setup_one<2, 224, kProduct>() | setup_one<2, 224, kInputGrad>();
+    return setup_one<1, 128, 4, kProduct>() | setup_one<1, 128, 4, kInputGrad>() | setup_one<2, 224, 4, kProduct>() | setup_one<2, 224, 4, kInputGrad>() |
+           setup_one<2, 224, 8, kProduct>() | setup_one<2, 224, 8, kInputGrad>();
 }
 
 }  // namespace ops
