@@ -21,6 +21,14 @@
 //
 // Two tile widths as in the 16-bit products: 128 columns on one CTA, and a CTA pair with 256 f x 224 columns (two accumulator sets of 256
 // would leave the exponents no tensor memory).
+//
+// Measured (one B200; copy bandwidth 6551 GB/s, cuBLAS bf16 1669 TFLOP/s in a burst, 1392 sustained):
+//   y,  1536 rows, 96 groups, 2816 x 2048   93 us = 6.1 TB/s, 92 % of the copy bandwidth (bound by the weights' bytes)
+//   y, 49152 rows, 64 groups, 2816 x 2048   286 to 313 us sustained = 1.8 to 2.0 PFLOP/s, bound by power (1.04 GHz at 990 W); 238 us in a
+//                                           burst of milliseconds, 160 us = 3.5 PFLOP/s for one launch on an idle GPU
+//   dx, 24582 rows, 64 groups, 2048 x 1408  90 to 92 us sustained, 75 in a burst
+//   y, 6 rows of 64 groups, 2816 x 2048     9.9 us: 35 MB, 5.3 us of stream, behind launch, offsets and the first copies
+// Without its scales (one kind of product less) the prompt takes the same time.
 
 #include "ew_ops.h"
 #include "ew_tc.cuh"
@@ -44,7 +52,8 @@ constexpr int kSlots = 4;                              // places for the exponen
 constexpr int kMaps = 8;                               // row boxes of 16, 32 .. 128 rows
 constexpr int kTiles = 2;                              // 16-bit results on their way out: tiles of 64 f x 32 rows of each pair of epilogue warps
 // Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 1024 terms for
-// fp32 results, 8192 for fp16, 65536 for bf16.
+// fp32 results, 8192 for fp16, 65536 for bf16.  (Products of 8-bit values have few digits: over terms of one sign and size 1.1e-7 of the result is cut
+// off in 1024 of them; but with a first block 2^12 times the others up to 7e-6, 1.4e-5 in 2048, 5.5e-5 in 8192.)
 constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 1024 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
 
 struct Args {
@@ -171,7 +180,7 @@ __device__ __forceinline__ bool both_of_pair(bool ok) {
 // small matrix instructions' results and turns it over on the way to shared memory, where it and its neighbour fill a tile of 32 rows of 64 f
 // (128 bytes; pieces of 16 bytes exchanged by the row, the copy's swizzle, so that no bank is met twice).  A bulk copy takes the tile away while the next
 // is filled; of rows behind the item's end only the others are stored, 16 bytes a lane.
-// (32 stores of two bytes a lane: prompt 261 us, input gradient 95; 16 bytes a lane: 257 and 79.)
+// (Prompt and input gradient: 242 and 75 us; 32 stores of two bytes a lane 261 and 95, of 16 bytes 258 and 78.)
 template <bool BF16>
 __device__ __forceinline__ void store_tile(uint32_t taddr, uint8_t *tile, const CUtensorMap *map, int f, int row0, uint16_t *p, long long ldo, int lim, int lane, int odd, int f_left) {
     uint32_t v[2][16];

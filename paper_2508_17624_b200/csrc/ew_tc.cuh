@@ -264,7 +264,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
 
 // The same by a whole warp, in every lane: for the warps that issue copies and products.  Their loops are the same in all lanes and one
 // elected lane issues, which the compiler turns into uniform registers; with a loop in one lane alone every operand of every
-// product is first moved there (block-scaled products: 885 clocks a k-block of four, LATER).
+// product is first moved there (block-scaled products, a k-block of four: 885 clocks in one lane, 330 so).
 template <bool PEER>
 __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
     if (__all_sync(0xffffffffu, try_nap<PEER>(bar, parity))) return true;
