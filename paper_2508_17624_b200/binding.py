@@ -64,27 +64,28 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_2508_17624_b200.build` "
                                "(the CUDA extension is required; there is no CPU fallback)")
-        _lib = C.CDLL(LIB_PATH)
-        _lib.ew_status_str.restype = C.c_char_p
-        _lib.ew_last_error_string.restype = C.c_char_p
+        loaded = C.CDLL(LIB_PATH)
+        loaded.ew_status_str.restype = C.c_char_p
+        loaded.ew_last_error_string.restype = C.c_char_p
         for name in EXPORTS:
-            getattr(_lib, name)
+            getattr(loaded, name)
         # the stand-alone operators are called with plain integers (addresses among them)
         i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
         for name in ("ew_grouped_mm", "ew_grouped_mm_dx"):
-            getattr(_lib, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, i64, ptr, i32, i32, i32, i32, ptr, i64, ptr]
-        _lib.ew_grouped_mm_dw.argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, i64, i64, ptr]
-        _lib.ew_quant_mv.argtypes = [i32, i32, i32, ptr, i64, ptr, ptr, ptr, i32, i32, i32, i32, i32, i32, ptr, i64, ptr]
-        _lib.ew_quant_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, i32, ptr, ptr, ptr]
-        _lib.ew_swiglu.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr]
-        _lib.ew_swiglu_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, ptr, i64, ptr, ptr]
-        _lib.ew_scaled_rows.argtypes = [i32, i32, i32, ptr, i64, i32, i32, ptr, i64, ptr, i64, ptr]
-        _lib.ew_scaled_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, ptr, i64, i64, ptr, ptr]
+            getattr(loaded, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, i64, ptr, i32, i32, i32, i32, ptr, i64, ptr]
+        loaded.ew_grouped_mm_dw.argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, i64, i64, ptr]
+        loaded.ew_quant_mv.argtypes = [i32, i32, i32, ptr, i64, ptr, ptr, ptr, i32, i32, i32, i32, i32, i32, ptr, i64, ptr]
+        loaded.ew_quant_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, i32, ptr, ptr, ptr]
+        loaded.ew_swiglu.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr]
+        loaded.ew_swiglu_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, i32, i32, ptr, i64, ptr, ptr]
+        loaded.ew_scaled_rows.argtypes = [i32, i32, i32, ptr, i64, i32, i32, ptr, i64, ptr, i64, ptr]
+        loaded.ew_scaled_pack.argtypes = [i32, i32, ptr, i64, i64, i32, i32, i32, ptr, i64, i64, ptr, ptr]
         for name in ("ew_scaled_mm", "ew_scaled_mm_dx"):
-            getattr(_lib, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i64, i64, ptr, ptr, i32, i32, i32, i32, ptr, i64, ptr]
-        _lib.ew_swiglu_scaled.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr, i64, ptr]
-        _lib.ew_rms_norm.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, C.c_float, i32, i32, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
-        _lib.ew_rms_norm_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, ptr, ptr]
+            getattr(loaded, name).argtypes = [i32, i32, i32, ptr, i64, ptr, i64, ptr, i64, i64, ptr, ptr, i32, i32, i32, i32, ptr, i64, ptr]
+        loaded.ew_swiglu_scaled.argtypes = [i32, i32, ptr, i64, ptr, i32, i32, ptr, i64, ptr, i64, ptr]
+        loaded.ew_rms_norm.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, C.c_float, i32, i32, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
+        loaded.ew_rms_norm_grad.argtypes = [i32, i32, ptr, i64, ptr, i64, ptr, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, ptr, ptr]
+        _lib = loaded                                      # (complete: another thread may be waiting for it to be there)
     return _lib
 
 
@@ -325,13 +326,11 @@ class _Torch:
         cls.eights = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
         cls.recording, cls.empty_like = torch.is_grad_enabled, torch.empty_like
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
-        lib()
         cls.ready = True
         return cls
 
 
 def _torch():
-    """Torch's constants; the library is loaded when they are."""
     return _Torch if _Torch.ready else _Torch.load()
 
 
@@ -639,7 +638,7 @@ def scaled_rows(x, dtype=None, out=None):
     to = _eight(T, dtype, "scaled_rows")
     rows, width, ldx = _matrix(x, dev, x.dtype, "x", None)
     q, scales, ldq, lds = _row_blocks(out, rows, width, dtype, T, x)
-    rc = _lib.ew_scaled_rows(dev, code, to, x.data_ptr(), ldx, rows, width, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    rc = lib().ew_scaled_rows(dev, code, to, x.data_ptr(), ldx, rows, width, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
     if rc:
         _check(rc, "ew_scaled_rows")
     return q, scales
@@ -661,7 +660,7 @@ def scaled_pack(w, out=None):
         if not scales.is_contiguous():
             raise ValueError("scales of weights are contiguous")
     ldq = q.stride(1) if n > 1 else k
-    rc = _lib.ew_scaled_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, q.data_ptr(), ldq, q.stride(0) if slots > 1 else n * ldq, scales.data_ptr(),
+    rc = lib().ew_scaled_pack(dev, code, w.data_ptr(), ld, stride, slots, n, k, q.data_ptr(), ldq, q.stride(0) if slots > 1 else n * ldq, scales.data_ptr(),
                               T.stream(dev))
     if rc:
         _check(rc, "ew_scaled_pack")
@@ -711,7 +710,7 @@ def _scaled_product(where, a, a_scales, w, w_scales, offsets, out, out_dtype, gr
     else:
         _result(out, (rows, wide), out_dtype, a)
         ldo = out.stride(0) if rows > 1 else wide
-    fn = _lib.ew_scaled_mm_dx if grad else _lib.ew_scaled_mm
+    fn = lib().ew_scaled_mm_dx if grad else lib().ew_scaled_mm
     rc = fn(dev, row_type, code, a.data_ptr(), lda, a_scales.data_ptr(), lds, w.data_ptr(), ldw, stride, w_scales.data_ptr(), offsets_at, rows, groups, n, k,
             out.data_ptr(), ldo, T.stream(dev))
     if rc:
@@ -743,7 +742,7 @@ def swiglu_scaled(h, row_weights=None, out=None):
         raise ValueError(f"h holds a gate and an up block side by side: an even width is wanted, got {two}")
     p = _row_weights(row_weights, dev, T, rows, h)
     q, scales, ldq, lds = _row_blocks(out, rows, two // 2, T.e4m3, T, h)
-    rc = _lib.ew_swiglu_scaled(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, two // 2, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
+    rc = lib().ew_swiglu_scaled(dev, code, h.data_ptr(), ldh if rows > 1 else two, p, rows, two // 2, q.data_ptr(), ldq, scales.data_ptr(), lds, T.stream(dev))
     if rc:
         _check(rc, "ew_swiglu_scaled")
     return q, scales
@@ -797,7 +796,7 @@ def _norm(x, weight, residual, eps, y, with_y, blocks, with_blocks, total):
         total_at, got = total.data_ptr(), got + (total,)
     elif total is not None:
         raise ValueError("sum_out is for the sum with a residual")
-    rc = _lib.ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width, total_at, ldt, y_at, ldy, q_at, ldq, scales_at, lds, T.stream(dev))
+    rc = lib().ew_rms_norm(dev, code, x.data_ptr(), ldx, res, ldr, weight.data_ptr(), eps, rows, width, total_at, ldt, y_at, ldy, q_at, ldq, scales_at, lds, T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm")
     return got[0] if len(got) == 1 else got
@@ -828,9 +827,9 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     dy_at, lddy = _beside(dy, rows, width, "dy", t, dev)
     dt_at, lddt = (None, 0) if dt is None else _beside(dt, rows, width, "dt", t, dev)
     out, ldo = _like(out, rows, width, "out", t)
-    parts = _lib.ew_rms_norm_grad_parts(rows, width)
+    parts = lib().ew_rms_norm_grad_parts(rows, width)
     dw, room = weight.new_empty((width,), dtype=T.float32), weight.new_empty((parts, width), dtype=T.float32)
-    rc = _lib.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
+    rc = lib().ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
                              T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm_grad")

@@ -210,6 +210,28 @@ def test_products_long_sums_in_parts(counts, n, k, out_dtype):
     check_both(counts, n, k, E4M3, out_dtype, seed=11)
 
 
+@pytest.mark.parametrize("rows", [3000, 300000])
+def test_products_most_groups(rows):
+    check_both(make_counts(rows, 2048, 4, empty=range(0, 2048, 3)), 24, 32, out_dtype=FP32, seed=6)
+
+
+def test_products_groups_that_take_turns():
+    """Weights whose matrices interleave their rows, results in the middle of a larger tensor."""
+    w = uneven((3, 72, 256), BF16, 1, 0.1)
+    packed = binding.scaled_pack(w)
+    turns = torch.zeros((72, 3, 272), dtype=torch.uint8, device="cuda").view(E4M3).transpose(0, 1)[:, :, :256]
+    turned = binding.scaled_pack(w, out=(turns, torch.empty_like(packed[1])))
+    assert torch.equal(as_bits(turned[0]), as_bits(packed[0])) and turned[0] is turns
+    offsets = torch.tensor([0, 30, 31, 50], dtype=torch.int32, device="cuda")
+    for call, width, wide in ((binding.scaled_mm, 256, 72), (binding.scaled_mm_dx, 72, 256)):
+        q, s = binding.scaled_rows(uneven((50, width), BF16, 2))
+        want = call(q, s, *packed, offsets)
+        for left, room_ in ((8, 96 if wide == 72 else 280), (3, wide + 8), (0, wide + 1)):
+            out = torch.full((50, room_), 7.0, dtype=BF16, device="cuda")
+            call(q, s, *turned, offsets, out=out[:, left:left + wide])
+            assert torch.equal(out[:, left:left + wide], want) and (out[:, :left] == 7).all() and (out[:, left + wide:] == 7).all()
+
+
 def test_products_without_offsets():
     w, ws = binding.scaled_pack(uneven((1, 200, 300), BF16, 1, 0.1))
     q, s = binding.scaled_rows(uneven((37, 300), FP16, 2))
@@ -297,7 +319,7 @@ def grad_ref(dy, t, w, dt, eps):
 
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
 @pytest.mark.parametrize("with_dt", [True, False])
-@pytest.mark.parametrize("rows,width,pad", [(1, 1, 0), (1, 2048, 0), (3, 129, 0), (70, 264, 8), (593, 300, 4), (2500, 512, 0), (1300, 1333, 0), (3, 4000, 0), (700, 8192, 0), (2, 16384, 0),
+@pytest.mark.parametrize("rows,width,pad", [(1, 1, 0), (1, 2048, 0), (3, 129, 0), (70, 264, 8), (593, 300, 4), (2500, 512, 0), (1300, 1333, 0), (3, 4000, 0), (700, 8192, 0), (900, 16384, 0),
                                             (2, 12345, 1)])
 def test_norm_grad(rows, width, pad, with_dt, dtype):
     t, dy = uneven((rows, width), dtype, 1, 0.5, pad), randn((rows, width), dtype, 2, 0.1, pad)
