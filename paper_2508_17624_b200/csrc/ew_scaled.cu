@@ -51,10 +51,11 @@ constexpr int kMaxStages = 7;
 constexpr int kSlots = 4;                              // places for the exponents of four k-blocks
 constexpr int kMaps = 8;                               // row boxes of 16, 32 .. 128 rows
 constexpr int kTiles = 2;                              // 16-bit results on their way out: tiles of 64 f x 32 rows of each pair of epilogue warps
-// Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 1024 terms for
+// Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 2048 terms for
 // fp32 results, 8192 for fp16, 65536 for bf16.  (Products of 8-bit values have few digits: over terms of one sign and size 1.1e-7 of the result is cut
-// off in 1024 of them; but with a first block 2^12 times the others up to 7e-6, 1.4e-5 in 2048, 5.5e-5 in 8192.)
-constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 1024 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
+// off in 1024 of them; but with a first block 2^12 times the others up to 7e-6, 1.4e-5 in 2048, 5.5e-5 in 8192: two steps of 2^-23 an
+// instruction.)
+constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 2048 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
 
 struct Args {
     const int32_t *offsets;                            // null: one group, all rows

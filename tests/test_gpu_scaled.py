@@ -210,6 +210,19 @@ def test_products_long_sums_in_parts(counts, n, k, out_dtype):
     check_both(counts, n, k, E4M3, out_dtype, seed=11)
 
 
+@pytest.mark.parametrize("rows", [40, 700])
+@pytest.mark.parametrize("n,k", [(264, 2048), (2048, 520), (136, 5000)])
+def test_products_of_one_sign_in_the_2_norm(n, k, rows):
+    """fp32 results of positive operands: off by at most 1.5e-5 (two steps of 2^-23 of the sum an instruction of 32 terms, 2048 terms a part), which
+    neither a 16-bit rounding on the way (1.4e-4 for fp16) nor a summed element left out (1/k) would pass."""
+    w, ws = binding.scaled_pack(uneven((1, n, k), BF16, 1).abs_())
+    for call, width in ((binding.scaled_mm, k), (binding.scaled_mm_dx, n)):
+        q, s = binding.scaled_rows(uneven((rows, width), BF16, 2).abs_())
+        got, wd = call(q, s, w, ws, out_dtype=FP32).double(), values(w, ws)[0]
+        ref = values(q, s) @ (wd.t() if call is binding.scaled_mm else wd)
+        assert (got - ref).norm() / ref.norm() <= 1.5e-5 and ((got - ref).abs() <= 1.5e-5 * ref).all()
+
+
 @pytest.mark.parametrize("rows", [3000, 300000])
 def test_products_most_groups(rows):
     check_both(make_counts(rows, 2048, 4, empty=range(0, 2048, 3)), 24, 32, out_dtype=FP32, seed=6)
