@@ -24,9 +24,10 @@
 //
 // Measured (one B200; copy bandwidth 6551 GB/s, cuBLAS bf16 1669 TFLOP/s in a burst, 1392 sustained):
 //   y,  1536 rows, 96 groups, 2816 x 2048   93 us = 6.1 TB/s, 92 % of the copy bandwidth (bound by the weights' bytes)
-//   y, 49152 rows, 64 groups, 2816 x 2048   286 to 313 us sustained = 1.8 to 2.0 PFLOP/s, bound by power (1.04 GHz at 990 W); 238 us in a
-//                                           burst of milliseconds, 160 us = 3.5 PFLOP/s for one launch on an idle GPU
-//   dx, 24582 rows, 64 groups, 2048 x 1408  90 to 92 us sustained, 75 in a burst
+//   y, 49152 rows, 64 groups, 2816 x 2048   286 to 313 us sustained = 1.8 to 2.0 PFLOP/s, bound by power (1.04 GHz at 990 W); 235 us in a
+//                                           burst of milliseconds, 211 us = 2.7 PFLOP/s for one launch on an idle GPU
+//   y, 49152 rows, one group, 2816 x 2048   240 us sustained = 2.4 PFLOP/s (cuBLAS, 8 bits: 238 with a scale for 32 values, 258 with one in all)
+//   dx, 24582 rows, 64 groups, 2048 x 1408  90 to 92 us sustained, 75 in a burst, 72 for one launch
 //   y, 6 rows of 64 groups, 2816 x 2048     9.9 us: 35 MB, 5.3 us of stream, behind launch, offsets and the first copies
 // Without its scales (one kind of product less) the prompt takes the same time.
 
