@@ -449,7 +449,7 @@ ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x, int64_t ld
 
 /* Its gradient: dt [rows, width] = the gradient with respect to t (and so to x and residual each) from dy and t, plus dt_in, the gradient that
  * reaches t past the norm (null: none; it may be dt itself, same address and stride), and dweight fp32 [width], summed over the rows in a fixed order.  workspace: fp32
- * [ew_rms_norm_grad_parts(rows, width), width], of this call alone while it runs. */
+ * [ew_rms_norm_grad_parts(rows, width), width], of this call alone while it runs (null where that is 0: few rows need none). */
 ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight,
                              const void *dt_in, int64_t lddt_in, float eps, int32_t rows, int32_t width, void *dt, int64_t lddt,
                              float *dweight, float *workspace, void *cuda_stream);

@@ -827,9 +827,13 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     dy_at, lddy = _beside(dy, rows, width, "dy", t, dev)
     dt_at, lddt = (None, 0) if dt is None else _beside(dt, rows, width, "dt", t, dev)
     out, ldo = _like(out, rows, width, "out", t)
-    parts = lib().ew_rms_norm_grad_parts(rows, width)
-    dw, room = weight.new_empty((width,), dtype=T.float32), weight.new_empty((parts, width), dtype=T.float32)
-    rc = lib().ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room.data_ptr(),
+    fn = lib()
+    parts, room, room_at = fn.ew_rms_norm_grad_parts(rows, width), None, None
+    dw = t.new_empty((width,), dtype=T.float32)
+    if parts:
+        room = t.new_empty((parts, width), dtype=T.float32)
+        room_at = room.data_ptr()
+    rc = fn.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room_at,
                              T.stream(dev))
     if rc:
         _check(rc, "ew_rms_norm_grad")

@@ -7,7 +7,7 @@
 // Bound by HBM: forward 2 to 4 bytes of operands and 1 to 5 of results a value, backward 6 or 8, each read or written once: a row
 // stays in the registers of a warp (or of 8 or 16, for wide rows and few) between the sum and its use.  The weight's gradient
 // is summed in the registers of the threads that own its columns, over all rows that a CTA meets; a second kernel adds the
-// CTAs' sums up, in the same order every time.  Measured: 8192 x 2048 with a
+// CTAs' sums up, in the same order every time (few rows: one cluster of CTAs, one kernel).  Measured: 8192 x 2048 with a
 // residual and both results 25.6 us = 5.9 TB/s (90 % of the measured copy bandwidth); its gradient 27 us = 4.9 TB/s, 23 of them the first
 // kernel's stream.
 #include "ew_blocks.cuh"
@@ -248,6 +248,130 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
     }
 }
 
+// The gradient of few rows in one launch: a cluster of sixteen CTAs, four teams of four warps in each, a row a team at a time, the next one
+// asked for before this one is worked on.  The teams' and then the CTAs' sums for dw are added up through shared memory, in their
+// order.  One launch and no workspace take the host 4 us less, which is what a call of few rows waits for: 2048 columns, alone and called from
+// Python, 128 rows 6.7 and 11.9 us, with the two kernels above 7.7 and 16; 333 rows 10.5 and 12 against 9.3 and 16; 512 rows 13.5 and 13.9 against
+// 9.0 and 16.  (Clusters of eight, the portable size: 333 rows 16 us.)
+constexpr int kCluster = 16, kTeams = 4, kTeamWarps = 4;
+constexpr int kFewRows = 384, kFewWidth = 2048;
+
+__device__ __forceinline__ float peer_value(const float *p, uint32_t rank) {
+    float v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(tc::smem_u32(p)), "r"(rank) : "memory");
+    return v;
+}
+
+template <class T, bool VEC, int NV>
+__global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(const GradArgs a) {
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    constexpr int W = kTeamWarps;
+    extern __shared__ float columns[];                 // [kTeams][width]
+    __shared__ __align__(16) float part[kTeams][2][2][W];
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W, team = (threadIdx.x >> 5) / W, step = kCluster * kTeams;
+    const int rank = (int)tc::cluster_ctarank();
+    Eight<T> dy[NV], t[NV], more[NV];
+    auto load = [&](int r) {
+        r = min(r, (int)a.rows - 1);
+        const T *dy_row = reinterpret_cast<const T *>(a.dy) + r * a.lddy, *t_row = reinterpret_cast<const T *>(a.t) + r * a.ldt;
+        const T *more_row = a.more ? reinterpret_cast<const T *>(a.more) + r * a.ldmore : t_row;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            load_span<T, VEC>(t[i], t_row, (i * W + w) * kSpan, lane, a.width);
+            load_span<T, VEC>(dy[i], dy_row, (i * W + w) * kSpan, lane, a.width);
+            load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
+        }
+    };
+    const int first = rank + kCluster * team;          // (one row a CTA before two)
+    load(first);
+    Two weight[NV][4], dw[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        Eight<T> x;
+        load_span<T, VEC>(x, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
+        to_pairs(weight[i], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dw[i][j] = two(0.f, 0.f);
+    }
+    int turn = 0;
+    for (int r = first; r < (int)a.rows; r += step, turn ^= 1) {
+        Two tv[NV][4], dv[NV][4], mv[NV][4], square = two(0.f, 0.f), along2 = square;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            clear_span<T, VEC>(t[i], (i * W + w) * kSpan, lane, a.width);
+            to_pairs(tv[i], t[i]);
+            to_pairs(dv[i], dy[i]);
+            to_pairs(mv[i], more[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                square = fma2(tv[i][j], tv[i][j], square);
+                along2 = fma2(mul2(dv[i][j], weight[i][j]), tv[i][j], along2);
+            }
+        }
+        load(r + step);
+        float sums[2] = {parts_of(square).x + parts_of(square).y, parts_of(along2).x + parts_of(along2).y};
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            sums[0] += __shfl_xor_sync(kAll, sums[0], d);
+            sums[1] += __shfl_xor_sync(kAll, sums[1], d);
+        }
+        if (lane == 0) {
+            part[team][turn][0][w] = sums[0];
+            part[team][turn][1][w] = sums[1];
+        }
+        asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + team), "n"(W * 32) : "memory");
+        sums[0] = sums[1] = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            sums[0] += part[team][turn][0][k];
+            sums[1] += part[team][turn][1][k];
+        }
+        const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);
+        const Two norm2 = two(norm, norm), back = two(-norm * along, -norm * along);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            Eight<T> dt;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Two scaled = mul2(dv[i][j], norm2);
+                Two v = a.more ? fma2(tv[i][j], back, mv[i][j]) : mul2(tv[i][j], back);
+                v = fma2(scaled, weight[i][j], v);
+                dw[i][j] = fma2(scaled, tv[i][j], dw[i][j]);
+                dt.v[2 * j] = from_f<T>(parts_of(v).x);
+                dt.v[2 * j + 1] = from_f<T>(parts_of(v).y);
+            }
+            store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = (i * W + w) * kSpan + place<VEC>(lane, j);
+            const float2 f = parts_of(dw[i][j >> 1]);
+            if (c < a.width) columns[team * a.width + c] = j & 1 ? f.y : f.x;
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.width; c += kTeams * W * 32) {
+        float v = columns[c];
+#pragma unroll
+        for (int k = 1; k < kTeams; ++k) v += columns[k * a.width + c];
+        columns[c] = v;
+    }
+    tc::cluster_sync_all();
+    const int share = (a.width + kCluster - 1) / kCluster, from = rank * share, to = min(from + share, a.width);
+    for (int c = from + threadIdx.x; c < to; c += kTeams * W * 32) {
+        float x[kCluster], v = 0.f;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) x[k] = peer_value(columns + c, k);
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) v += x[k];
+        a.parts[c] = v;
+    }
+    tc::cluster_sync_all();                            // until then the others read this CTA's sums
+}
+
 // dw[c] = the sum of parts[:, c]: 32 columns a CTA, 32 threads a column
 __global__ void __launch_bounds__(1024) parts_kernel(const float *parts, float *dw, int n_parts, int width) {
     tc::pdl_launch_dependents();
@@ -286,19 +410,39 @@ ew_status_t pick(const Args &a, cudaStream_t st) {
 }
 
 int grad_ctas(long long rows) { return (int)(rows < kMostCtas ? rows : kMostCtas); }
+bool few_rows(long long rows, int width) { return rows <= kFewRows && width <= kFewWidth; }
+
+template <class T, bool VEC, int NV>
+ew_status_t launch_few(GradArgs a, float *dw, cudaStream_t st) {
+    a.parts = dw;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kCluster);
+    cfg.blockDim = dim3(kTeams * kTeamWarps * 32);
+    cfg.dynamicSmemBytes = (size_t)kTeams * a.width * 4;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    return launched((int)cudaLaunchKernelEx(&cfg, few_rows_kernel<T, VEC, NV>, a), "RMS norm gradient");
+}
 
 template <class T, bool BULK, int W, int NV>
 ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
     const int ctas = grad_ctas(a.rows), stage_bytes = a.width * 2 * (a.more ? 3 : 2), fit = kRingBytes / stage_bytes;
     a.stages = fit < 1 ? 1 : fit < kMostStages ? fit : kMostStages;
-    if (ctas == 1) a.parts = dw;
     const ew_status_t s = launched(launch_pdl(grad_kernel<T, BULK, W, NV>, dim3((unsigned)ctas), dim3(W * 32), BULK ? a.stages * stage_bytes : 0, st, a), "RMS norm gradient");
-    if (s != EW_OK || ctas == 1) return s;
+    if (s != EW_OK) return s;
     return launched(launch_pdl(parts_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(1024), 0, st, (const float *)a.parts, dw, ctas, a.width), "RMS norm gradient");
 }
 
 template <class T, bool BULK>
 ew_status_t pick_grad(const GradArgs &a, float *dw, cudaStream_t st) {
+    if (few_rows(a.rows, a.width)) return a.width <= 1024 ? launch_few<T, BULK, 1>(a, dw, st) : launch_few<T, BULK, 2>(a, dw, st);
     if (a.width <= 1024) return launch_grad<T, BULK, 4, 1>(a, dw, st);
     if (a.width <= 2048) return launch_grad<T, BULK, 4, 2>(a, dw, st);
     if (a.width <= 4096) return launch_grad<T, BULK, 8, 2>(a, dw, st);
@@ -318,6 +462,8 @@ int load_one() {
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 4>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) |
            load_grad<T, VEC, 4, 1>() | load_grad<T, VEC, 4, 2>() | load_grad<T, VEC, 8, 2>() | load_grad<T, VEC, 16, 2>() | load_grad<T, VEC, 16, 4>() |
+           (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
+           (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 2>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
            (int)cudaFuncGetAttributes(&fa, parts_kernel);
 }
 
@@ -362,8 +508,7 @@ extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x,
 }
 
 extern "C" int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width) {
-    (void)width;
-    return rows < 1 ? 0 : grad_ctas(rows);
+    return rows < 1 || few_rows(rows, width) ? 0 : grad_ctas(rows);
 }
 
 extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight, const void *dt_in,
@@ -373,7 +518,7 @@ extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const voi
     if (rows < 0 || width < 1 || width > kMostWidth || bad_eps(eps)) return refuse("RMS norm: size or eps out of range");
     if (lddy < width || ldt < width || (dt_in && lddt_in < width) || lddt < width) return refuse("RMS norm: rows overlap");
     if (!dweight || ((uintptr_t)dweight & 3) ||
-        (rows > 0 && (!dy || !t || !weight || !dt || !workspace || ((uintptr_t)workspace & 3) || (((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 1))))
+        (rows > 0 && (!dy || !t || !weight || !dt || (!workspace && !few_rows(rows, width)) || ((uintptr_t)workspace & 3) || (((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 1))))
         return refuse("RMS norm: null or misaligned pointer");
     if (device < 0) return EW_ERR_NO_DEVICE;
     DeviceGuard guard;

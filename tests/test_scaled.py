@@ -80,11 +80,12 @@ def test_rms_norm_grad_refuses(lib):
     def grad(device=-1, dtype=BF16, dy=X, lddy=64, t=W, ldt=64, w=OFF, more=SX, ldm=64, eps=1e-6, rows=4, width=64, dt=OUT, lddt=64, dw=SW, room=0x7000):
         return lib.ew_rms_norm_grad(device, dtype, dy, lddy, t, ldt, w, more, ldm, eps, rows, width, dt, lddt, dw, room, None)
 
-    assert grad() == grad(more=None) == grad(rows=0, dy=None, t=None, dt=None, room=None) == NO_DEVICE
+    assert grad() == grad(more=None) == grad(rows=0, dy=None, t=None, dt=None, room=None) == grad(room=None) == grad(rows=10 ** 6) == NO_DEVICE
     for change in [dict(dtype=FP32), dict(dy=None), dict(dy=X + 1), dict(lddy=63), dict(t=None), dict(ldt=63), dict(w=None), dict(more=SX + 1), dict(ldm=63), dict(eps=-1e-6), dict(rows=-1),
-                   dict(width=0), dict(width=16385), dict(dt=None), dict(dt=OUT + 1), dict(lddt=63), dict(dw=None), dict(dw=SW + 2), dict(room=None), dict(room=0x7002)]:
+                   dict(width=0), dict(width=16385), dict(dt=None), dict(dt=OUT + 1), dict(lddt=63), dict(dw=None), dict(dw=SW + 2), dict(rows=10 ** 6, room=None), dict(room=0x7002)]:
         assert grad(**change) == INVALID, change
-    assert lib.ew_rms_norm_grad_parts(0, 64) == 0 and lib.ew_rms_norm_grad_parts(1, 64) == 1 and 1 < lib.ew_rms_norm_grad_parts(1 << 30, 64) <= 4096
+    assert lib.ew_rms_norm_grad_parts(0, 64) == lib.ew_rms_norm_grad_parts(1, 64) == 0 and 1 < lib.ew_rms_norm_grad_parts(1 << 30, 64) <= 4096
+    assert lib.ew_rms_norm_grad_parts(1, 16384) == 1
 
 
 def test_python_checks_before_the_library():
