@@ -288,8 +288,8 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512u) : "memory");
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
         }
+        pdl_launch_dependents();                       // (once the tensor memory is held: a kernel that found room beside this one and took some of it would wait for this one's end)
     }
-    pdl_launch_dependents();
     pdl_wait();                                        // the operands and the offsets may come from the kernel before
     if (warp == 0) {
         // group table: first row and rows of each group, and the number of row blocks before it.  Offsets are clamped to
@@ -466,7 +466,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             uint32_t word[4 * C::kBChunks], w_word;
             auto gather = [&](int kb) {                // of the k-blocks kb .. kb + 3
                 const int left = min(4, it.kb - kb);
-                uint32_t byte = lane < left ? w_scales[(long long)(kb + lane) * w_step] << (8 * lane) : 0;
+                uint32_t byte = lane < left ? (uint32_t)w_scales[(long long)(kb + lane) * w_step] << (8 * lane) : 0;
                 byte |= __shfl_xor_sync(0xffffffffu, byte, 1);
                 byte |= __shfl_xor_sync(0xffffffffu, byte, 2);
                 w_word = __shfl_sync(0xffffffffu, byte, 0);
