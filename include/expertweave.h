@@ -442,7 +442,7 @@ ew_status_t ew_swiglu_scaled(int32_t device, int32_t dtype, const void *h, int64
  * in fp32, rounded once.  residual null: t = x; otherwise t is written to sum [rows, width], which may be residual itself (same
  * address and stride) but no other operand.  Results: y [rows, width] in dtype (null: not wanted), q and scales: blocks of rows in EW_E4M3 of
  * the unrounded y (null: not wanted); one of them at least.  dtype: EW_BF16 or EW_FP16; any alignment is taken, rows on
- * 16-byte boundaries are fastest.  A row's sum of squares has to fit fp32 (values up to 1e17).  width <= 16384. */
+ * 16-byte boundaries are fastest.  A row's sum of squares has to fit fp32 (values up to 1e17; with eps = 0 not all below 1e-18).  width <= 16384. */
 ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,
                         float eps, int32_t rows, int32_t width, void *sum, int64_t ldsum, void *y, int64_t ldy, void *q, int64_t ldq,
                         void *scales, int64_t ldscales, void *cuda_stream);

@@ -245,6 +245,22 @@ def test_products_groups_that_take_turns():
             assert torch.equal(out[:, left:left + wide], want) and (out[:, :left] == 7).all() and (out[:, left + wide:] == 7).all()
 
 
+def test_input_gradient_by_differences():
+    """Whole numbers that e4m3 holds, so that every sum is exact: <dy, y(x + v) - y(x - v)> = 2 <dx, v>, to the last bit."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def whole(shape, most):
+        return torch.randint(-most, most + 1, shape, device="cuda", generator=g).to(BF16)
+
+    offsets = torch.tensor([0, 3, 3, 40, 300], dtype=torch.int32, device="cuda")
+    x, v, dy, w = whole((300, 200), 6), whole((300, 200), 1), whole((300, 136), 4), whole((4, 136, 200), 4)
+    packed = binding.scaled_pack(w)
+    plus, minus = (binding.scaled_mm(*binding.scaled_rows(t), *packed, offsets, out_dtype=FP32).double() for t in (x + v, x - v))
+    dx = binding.scaled_mm_dx(*binding.scaled_rows(dy, E5M2), *packed, offsets, out_dtype=FP32).double()
+    assert torch.equal(values(*binding.scaled_rows(x + v)), (x + v).double()) and torch.equal(values(*binding.scaled_rows(dy, E5M2)), dy.double())
+    assert float((dy.double() * (plus - minus)).sum()) == 2 * float((dx * v.double()).sum())
+
+
 def test_products_without_offsets():
     w, ws = binding.scaled_pack(uneven((1, 200, 300), BF16, 1, 0.1))
     q, s = binding.scaled_rows(uneven((37, 300), FP16, 2))
