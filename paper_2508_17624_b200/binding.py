@@ -324,7 +324,7 @@ class _Torch:
         cls.int32, cls.float32, cls.uint8, cls.bfloat16 = torch.int32, torch.float32, torch.uint8, torch.bfloat16
         cls.e4m3, cls.e5m2, cls.exponent = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
         cls.eights = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
-        cls.recording, cls.empty_like = torch.is_grad_enabled, torch.empty_like
+        cls.recording, cls.empty_like, cls.empty = torch.is_grad_enabled, torch.empty_like, torch.empty_strided      # (half a microsecond less than new_empty)
         cls.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         cls.ready = True
         return cls
@@ -618,8 +618,8 @@ def _row_blocks(out, rows, width, dtype, T, like):
     if out is None:
         wide, blocks = (width + 15) // 16 * 16, (width + 127) // 128
         room = (blocks + 3) // 4 * 4
-        scales = like.new_empty((rows, room), dtype=T.exponent)
-        q = T.empty_like(like, dtype=dtype) if like.shape == (rows, wide) else like.new_empty((rows, wide), dtype=dtype)
+        at = like.device
+        q, scales = T.empty((rows, wide), (wide, 1), dtype=dtype, device=at), T.empty((rows, room), (room, 1), dtype=T.exponent, device=at)
         return q if wide == width else q[:, :width], scales if room == blocks else scales[:, :blocks], wide, room
     q, scales = out
     q, scales = _result(q, (rows, width), dtype, like, "q"), _result(scales, (rows, (width + 127) // 128), T.exponent, like, "scales")
@@ -706,7 +706,7 @@ def _scaled_product(where, a, a_scales, w, w_scales, offsets, out, out_dtype, gr
         out_dtype = T.bfloat16 if out is None else out.dtype
     code = _code(T, out_dtype)
     if out is None:
-        out, ldo = a.new_empty((rows, wide), dtype=out_dtype), wide
+        out, ldo = T.empty((rows, wide), (wide, 1), dtype=out_dtype, device=a.device), wide
     else:
         _result(out, (rows, wide), out_dtype, a)
         ldo = out.stride(0) if rows > 1 else wide
@@ -829,9 +829,9 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     out, ldo = _like(out, rows, width, "out", t)
     fn = lib()
     parts, room, room_at = fn.ew_rms_norm_grad_parts(rows, width), None, None
-    dw = t.new_empty((width,), dtype=T.float32)
+    dw = T.empty((width,), (1,), dtype=T.float32, device=t.device)
     if parts:
-        room = t.new_empty((parts, width), dtype=T.float32)
+        room = T.empty((parts, width), (width, 1), dtype=T.float32, device=t.device)
         room_at = room.data_ptr()
     rc = fn.ew_rms_norm_grad(dev, code, dy_at, lddy, t.data_ptr(), ldt, weight.data_ptr(), dt_at, lddt, eps, rows, width, out.data_ptr(), ldo, dw.data_ptr(), room_at,
                              T.stream(dev))
