@@ -7,7 +7,7 @@
 // Bound by HBM: 3, 5 and 3 bytes a value, each read or written once.  A block's values stay in the registers of half a warp
 // (rows) or a CTA (weights) between the search for the largest and the rounding.  Measured: rows 24582 x 2048 25 us = 6.1 TB/s
 // (93 % of the measured copy bandwidth), SwiGLU 49152 x 1408 57 us = 6.1 TB/s, 63 to 67 in long runs at the power limit, weights
-// 64 x 2816 x 2048 176 us = 6.3 TB/s (96 %).
+// 64 x 2816 x 2048 166 us = 6.7 TB/s, 174 to 180 in long runs.
 #include "ew_blocks.cuh"
 #include "ew_ops.h"
 #include "ew_tc.cuh"
@@ -85,8 +85,8 @@ struct WeightArgs {
     int n, k, nb, kb;
 };
 
-// A CTA a block of 128 x 128.  VEC: sixteen lanes a row of the block; otherwise 128.  (Three CTAs an SM 176 us, four, with spills, 186; the values
-// kept in 32 bits, two CTAs, 191.)
+// A CTA a block of 128 x 128.  VEC: sixteen lanes a row of the block; otherwise 128.  (Three CTAs an SM 166 us, 179 in long
+// runs at the power limit; four 160 and 185; two 201.)
 template <class T, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? 3 : 2) weights_kernel(const WeightArgs a) {
     tc::pdl_launch_dependents();
@@ -108,14 +108,8 @@ __global__ void __launch_bounds__(kThreads, VEC ? 3 : 2) weights_kernel(const We
             for (int j = 0; j < 8; ++j) raw[i].v[j] = w[min(row_of(i, j), a.n - 1) * a.ldw + min(col_of(j), a.k - 1)];
         }
     }
-    float most;
-    auto find = [&](bool finite) {
-        most = 0.f;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-            const float v = fabsf(to_f(raw[i >> 3].v[i & 7]));
-            most = fmaxf(most, finite && not_finite(v) ? 0.f : v);
-        }
+    float most = 0.f;
+    auto of_all = [&] {                                // the CTA's largest, in every thread
 #pragma unroll
         for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, d));
         if ((t & 31) == 0) part[t >> 5] = most;
@@ -123,26 +117,37 @@ __global__ void __launch_bounds__(kThreads, VEC ? 3 : 2) weights_kernel(const We
 #pragma unroll
         for (int i = 0; i < kThreads / 32; ++i) most = fmaxf(most, part[i]);
     };
-    find(false);
-    const bool bad = not_finite(most);                 // the same in every thread
-    if (bad) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        Two v[4];
+        to_pairs(v, raw[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = max_abs(most, v[j]);
+    }
+    of_all();
+    if (not_finite(most)) {                            // the same in every thread
+        most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            T &x = raw[i >> 3].v[i & 7];
+            if (not_finite(to_f(x))) x = from_f<T>(__int_as_float(0x7fffffff));
+            else most = fmaxf(most, fabsf(to_f(x)));
+        }
         __syncthreads();
-        find(true);
+        of_all();
     }
     const uint32_t code = scale_code(most, kTop<false>);
-    const float f = inverse_scale(code);
+    const Two f = two(inverse_scale(code), inverse_scale(code));
     if (t == 0) a.scales[((long long)blockIdx.y * a.nb + bn) * a.kb + bk] = (uint8_t)code;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        Two v[4];
+        to_pairs(v, raw[i]);
         uint32_t pair[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float lo = to_f(raw[i].v[2 * j]), hi = to_f(raw[i].v[2 * j + 1]);
-            if (bad) {
-                if (not_finite(lo)) lo = __int_as_float(0x7fffffff);
-                if (not_finite(hi)) hi = __int_as_float(0x7fffffff);
-            }
-            pair[j] = two_values<false>(lo * f, hi * f);
+            const float2 x = parts_of(mul2(v[j], f));
+            pair[j] = two_values<false>(x.x, x.y);
         }
         if constexpr (VEC) {
             if (col_of(0) < a.k && row_of(i, 0) < a.n)

@@ -66,6 +66,11 @@ __device__ __forceinline__ Two mul2(Two a, Two b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
 // max(m, |a.lo|, |a.hi|); a NaN is passed over
 __device__ __forceinline__ float max_abs(float m, Two a) {
     const float2 v = parts_of(a);
@@ -76,6 +81,14 @@ template <class T>
 __device__ __forceinline__ void to_pairs(Two (&p)[4], const Eight<T> &o) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j] = two(to_f(o.v[2 * j]), to_f(o.v[2 * j + 1]));
+}
+
+__device__ __forceinline__ void round_pair(__nv_bfloat16 *to, float2 f) { *reinterpret_cast<__nv_bfloat162 *>(to) = __floats2bfloat162_rn(f.x, f.y); }
+__device__ __forceinline__ void round_pair(__half *to, float2 f) { *reinterpret_cast<__half2 *>(to) = __floats2half2_rn(f.x, f.y); }
+template <class T>
+__device__ __forceinline__ void from_pairs(Eight<T> &o, const Two (&p)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) round_pair(o.v + 2 * j, parts_of(p[j]));
 }
 
 // Where a lane's eight values of a span lie.  VEC: side by side, so that they move in one access (rows on 16-byte boundaries, of a

@@ -74,8 +74,12 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
                 T *sum = reinterpret_cast<T *>(a.sum) + r * a.ldsum;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
+                    Two xv[4], rv[4];
+                    to_pairs(xv, t[i]);
+                    to_pairs(rv, more[i]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) t[i].v[j] = from_f<T>(to_f(t[i].v[j]) + to_f(more[i].v[j]));
+                    for (int j = 0; j < 4; ++j) xv[j] = add2(xv[j], rv[j]);
+                    from_pairs(t[i], xv);
                     store_span<T, VEC>(t[i], sum, (i * W + w) * kSpan, lane, a.width);
                 }
             }
@@ -101,12 +105,8 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
             to_pairs(tv, t[i]);
             to_pairs(wv, weight);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                tv[j] = mul2(mul2(tv[j], two(norm, norm)), wv[j]);
-                const float2 f = parts_of(tv[j]);
-                y.v[2 * j] = from_f<T>(f.x);
-                y.v[2 * j + 1] = from_f<T>(f.y);
-            }
+            for (int j = 0; j < 4; ++j) tv[j] = mul2(mul2(tv[j], two(norm, norm)), wv[j]);
+            from_pairs(y, tv);
             if (a.y) store_span<T, VEC>(y, reinterpret_cast<T *>(a.y) + r * a.ldy, at, lane, a.width);
             if (a.q && at < a.width) put_span<VEC, false>(tv, a.q + r * a.ldq, a.scales + r * a.lds, at, lane, a.width);
         }
@@ -221,12 +221,10 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const Two scaled = mul2(dv[j], norm2);
-                Two v = a.more ? fma2(tv[j], back, mv[j]) : mul2(tv[j], back);
-                v = fma2(scaled, weight[i][j], v);
                 dw[i][j] = fma2(scaled, tv[j], dw[i][j]);
-                dt.v[2 * j] = from_f<T>(parts_of(v).x);
-                dt.v[2 * j + 1] = from_f<T>(parts_of(v).y);
+                tv[j] = fma2(scaled, weight[i][j], a.more ? fma2(tv[j], back, mv[j]) : mul2(tv[j], back));
             }
+            from_pairs(dt, tv);
             store_span<T, BULK>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
         }
     }
@@ -338,8 +336,7 @@ __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(c
                 Two v = a.more ? fma2(tv[i][j], back, mv[i][j]) : mul2(tv[i][j], back);
                 v = fma2(scaled, weight[i][j], v);
                 dw[i][j] = fma2(scaled, tv[i][j], dw[i][j]);
-                dt.v[2 * j] = from_f<T>(parts_of(v).x);
-                dt.v[2 * j + 1] = from_f<T>(parts_of(v).y);
+                round_pair(dt.v + 2 * j, parts_of(v));
             }
             store_span<T, VEC>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
         }
