@@ -173,6 +173,7 @@ def every_operator(seed=0):
     """One call of each, and their results as bits."""
     x, r, w = uneven((300, 512), BF16, seed + 1), uneven((300, 512), BF16, seed + 2), randn((512,), BF16, seed + 3)
     weights = randn((8, 384, 512), BF16, seed + 4, 0.05)
+    many = uneven((700, 512), BF16, seed + 5)           # beyond the rows that the norm's gradient takes in one launch
     offsets = torch.tensor([0, 10, 10, 90, 130, 200, 201, 280, 300], dtype=torch.int32, device="cuda")
     torch.cuda.synchronize()
 
@@ -183,7 +184,7 @@ def every_operator(seed=0):
         act = binding.swiglu_scaled(h, torch.ones(300, device="cuda"))
         back = binding.scaled_mm_dx(*binding.scaled_rows(h, E5M2), *packed, offsets, out_dtype=FP32)
         dense = binding.scaled_mm(q[:7], s[:7], packed[0][:1], packed[1][:1])
-        return [q, s, y, t, *packed, h, *act, back, dense, binding.rms_norm(x, w), *binding.rms_norm_grad(y, t, w, r)]
+        return [q, s, y, t, *packed, h, *act, back, dense, binding.rms_norm(x, w), *binding.rms_norm_grad(y, t, w, r), *binding.rms_norm_grad(many, many, w)]
     return call
 
 
