@@ -173,7 +173,9 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
         Eight<T> dy[NV], t[NV], more[NV];
         const T *t_row, *dy_row, *more_row;
         if (BULK) {
-            tc::wait_warp(bar + 8 * stage, phase, abort_flag, a.err);        // (where it gives up, the rest is wrong and reported, but ends)
+            // Every lane waits for itself: what the copy wrote is visible to the threads that saw its phase end, and to no others.  (Where it
+            // gives up, the rest is wrong and reported, but ends.)
+            tc::wait_all<false>(bar + 8 * stage, phase, abort_flag, a.err);
             t_row = reinterpret_cast<const T *>(ring + stage * stage_bytes);
             dy_row = t_row + a.width;
             more_row = dy_row + a.width;
@@ -205,8 +207,8 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
         }
         float sums[2] = {parts_of(square).x + parts_of(square).y, parts_of(along2).x + parts_of(along2).y};
         add_up<W, 2>(sums, turn++);
-        if (BULK) {                                    // every thread has its part of the stage: the next row may come
-            if (threadIdx.x == 0 && r + (long long)a.stages * gridDim.x < a.rows) fetch(r + (long long)a.stages * gridDim.x, stage);
+        if (BULK) {                                    // every thread has its part of the stage: the next row may come, unless a wait gave up with a copy still on its way
+            if (threadIdx.x == 0 && r + (long long)a.stages * gridDim.x < a.rows && !*abort_flag) fetch(r + (long long)a.stages * gridDim.x, stage);
             if (++stage == a.stages) { stage = 0; phase ^= 1; }
         }
         const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);      // mean(g u) = norm mean(g t)

@@ -363,6 +363,23 @@ def test_norm_grad(rows, width, pad, with_dt, dtype):
     assert torch.equal(again[0], got) and torch.equal(again[1], dw)
 
 
+@pytest.mark.parametrize("with_dt", [True, False])
+@pytest.mark.parametrize("rows,width", [(4000, 256), (2500, 512), (3000, 1000), (9000, 1024), (2500, 2048), (700, 8192), (3000, 300)])
+def test_norm_grad_reads_no_earlier_row(rows, width, with_dt):
+    """Two sets of inputs in turn: what a call finds in shared memory is of the other set, and must not show."""
+    sets = [(randn((rows, width), BF16, s, 0.1), randn((rows, width), BF16, s + 1, 0.5), 1 + randn((width,), BF16, s + 2, 0.2),
+             randn((rows, width), BF16, s + 3, 0.1) if with_dt else None) for s in (10, 20)]
+    first = [binding.rms_norm_grad(dy, t, w, dt) for dy, t, w, dt in sets]
+    for (dy, t, w, dt), (got, dw) in zip(sets, first):
+        ref, mag, ref_dw, mag_dw = grad_ref(dy, t, w, dt, 1e-6)
+        assert ((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 4 * NORM * mag + 2.0 ** -134).all()
+        assert ((dw.double() - ref_dw).abs() <= (NORM + (rows / 592 + 40) * 2.0 ** -24) * mag_dw + 1e-40).all()
+    for _ in range(20):
+        for (dy, t, w, dt), (got, dw) in zip(sets, first):
+            again = binding.rms_norm_grad(dy, t, w, dt)
+            assert torch.equal(again[0], got) and torch.equal(again[1], dw)
+
+
 def test_norm_grad_by_differences():
     """Along a random direction against (f(t + e v) - f(t - e v)) / 2 e of the formula in 64 bits."""
     t, dy, w = randn((5, 48), FP16, 4), randn((5, 48), FP16, 5), (1 + 0.2 * randn((48,), FP32, 6)).to(FP16)
