@@ -163,7 +163,8 @@ __global__ void __launch_bounds__(kThreads, VEC ? 3 : 2) weights_kernel(const We
 template <class T, bool ACT, bool E5M2, bool VEC>
 ew_status_t launch_rows(const Device &d, const RowArgs &a, cudaStream_t st) {
     constexpr int kWarps = kThreads / 32;
-    // a CTA a row where warps would not fill half of the GPU (1536 rows of 1408: 3.8 us)
+    // a CTA a row where warps would not fill half of the GPU (SwiGLU of 1408 columns: 2368 rows 4.9 us against 6.7 with a warp a row, 4736
+    // rows 10.6 against 9.7; rows of 2048: 3.9 and 4.8, 7.3 and 5.9; of 512, either way in the launch's noise up to 2368 rows: 3.9 and 3.4)
     const bool wide = a.rows < (long long)d.sm_count * kWarps * 2;
     const long long ctas = wide ? a.rows : (a.rows + kWarps - 1) / kWarps, most = 0x7fffffff;
     const dim3 grid((unsigned)(ctas < most ? ctas : most));

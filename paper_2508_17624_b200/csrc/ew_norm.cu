@@ -128,20 +128,26 @@ struct GradArgs {
     float inv_width, eps;
 };
 
-// A row a CTA of W warps at a time, its columns' sums in the registers of the threads that own them.  BULK: rows come to shared memory by bulk
-// copies, up to kMostStages of them ahead of the one that is worked on; without them a CTA's loads wait for the row before.  Needs rows on
-// 16-byte boundaries of a multiple of eight values.
+// Teams of W warps (eight teams of one, or one team a CTA), a row a team at a time, its columns' sums in the registers of the threads that own
+// them.  BULK: rows come to shared memory by bulk copies, up to kMostStages of them ahead of the one that is worked on; without them a
+// team's loads wait for the row before.  Needs rows on 16-byte boundaries of a multiple of eight values.
 template <class T, bool BULK, int W, int NV>
-__global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 && NV <= 2 ? 2 : 1) grad_kernel(const GradArgs a) {
     tc::pdl_launch_dependents();
-    extern __shared__ __align__(128) uint8_t ring[];   // [stages][t, dy, dt_in][width]
-    __shared__ uint64_t bars[kMostStages];
+    constexpr int kRows = kThreadsOf<W> / 32 / W;
+    extern __shared__ __align__(128) uint8_t ring[];   // [teams][stages][t, dy, dt_in][width]; at the end, with several teams, their sums
+    __shared__ uint64_t bars[kRows * kMostStages];
     __shared__ int abort_word;
     volatile int *abort_flag = &abort_word;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const uint32_t row_bytes = (uint32_t)a.width * 2, stage_bytes = row_bytes * (a.more ? 3 : 2), bar = tc::smem_u32(bars), ring_at = tc::smem_u32(ring);
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W, team = (threadIdx.x >> 5) / W;
+    const bool fetcher = threadIdx.x % (W * 32) == 0;
+    const uint32_t row_bytes = (uint32_t)a.width * 2, stage_bytes = row_bytes * (a.more ? 3 : 2);
+    const uint32_t bar = tc::smem_u32(bars + team * kMostStages);
+    const uint8_t *stages = ring + team * a.stages * stage_bytes;
+    const uint32_t stages_at = tc::smem_u32(stages);
+    const long long first = (long long)blockIdx.x * kRows + team, step = (long long)gridDim.x * kRows;
     auto fetch = [&](long long r, int stage) {         // by one thread
-        const uint32_t to = ring_at + stage * stage_bytes, full = bar + 8 * stage;
+        const uint32_t to = stages_at + stage * stage_bytes, full = bar + 8 * stage;
         tc::mbar_expect_tx(full, stage_bytes);
         tc::bulk_load(to, reinterpret_cast<const T *>(a.t) + r * a.ldt, row_bytes, full);
         tc::bulk_load(to + row_bytes, reinterpret_cast<const T *>(a.dy) + r * a.lddy, row_bytes, full);
@@ -149,16 +155,16 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
     };
     if (BULK) {
         if (threadIdx.x == 0) {
-            for (int i = 0; i < a.stages; ++i) tc::mbar_init(bar + 8 * i, 1);
+            for (int i = 0; i < kRows * kMostStages; ++i) tc::mbar_init(tc::smem_u32(bars + i), 1);
             abort_word = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
     }
     tc::pdl_wait();
-    if (BULK && threadIdx.x == 0)
+    if (BULK && fetcher)
         for (int i = 0; i < a.stages; ++i)
-            if (blockIdx.x + (long long)i * gridDim.x < a.rows) fetch(blockIdx.x + (long long)i * gridDim.x, i);
+            if (first + i * step < a.rows) fetch(first + i * step, i);
     Two weight[NV][4], dw[NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -169,14 +175,14 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
         for (int j = 0; j < 4; ++j) dw[i][j] = two(0.f, 0.f);
     }
     int turn = 0, stage = 0, phase = 0;
-    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    for (long long r = first; r < a.rows; r += step) {
         Eight<T> dy[NV], t[NV], more[NV];
         const T *t_row, *dy_row, *more_row;
         if (BULK) {
             // Every lane waits for itself: what the copy wrote is visible to the threads that saw its phase end, and to no others.  (Where it
             // gives up, the rest is wrong and reported, but ends.)
             tc::wait_all<false>(bar + 8 * stage, phase, abort_flag, a.err);
-            t_row = reinterpret_cast<const T *>(ring + stage * stage_bytes);
+            t_row = reinterpret_cast<const T *>(stages + stage * stage_bytes);
             dy_row = t_row + a.width;
             more_row = dy_row + a.width;
         } else {
@@ -207,8 +213,12 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
         }
         float sums[2] = {parts_of(square).x + parts_of(square).y, parts_of(along2).x + parts_of(along2).y};
         add_up<W, 2>(sums, turn++);
-        if (BULK) {                                    // every thread has its part of the stage: the next row may come, unless a wait gave up with a copy still on its way
-            if (threadIdx.x == 0 && r + (long long)a.stages * gridDim.x < a.rows && !*abort_flag) fetch(r + (long long)a.stages * gridDim.x, stage);
+        if (BULK) {                                    // every thread of the team has its part of the stage: the next row may come, unless a wait gave up with a copy still on its way
+            if (W == 1) {                              // (several warps have met at a barrier)
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            if (fetcher && r + a.stages * step < a.rows && !*abort_flag) fetch(r + a.stages * step, stage);
             if (++stage == a.stages) { stage = 0; phase ^= 1; }
         }
         const float norm = rsqrtf(sums[0] * a.inv_width + a.eps), along = norm * norm * (sums[1] * a.inv_width);      // mean(g u) = norm mean(g t)
@@ -230,15 +240,25 @@ __global__ void __launch_bounds__(W * 32, W == 4 && NV <= 2 ? 3 : 1) grad_kernel
             store_span<T, BULK>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
         }
     }
-    float *part = a.parts + (long long)blockIdx.x * a.width;
+    float *part = a.parts + (long long)blockIdx.x * a.width, *mine = kRows > 1 ? reinterpret_cast<float *>(ring) + team * a.width : part;
+    if (kRows > 1) __syncthreads();                    // all rows have been read
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int c = (i * W + w) * kSpan + place<BULK>(lane, j);
             const float2 f = parts_of(dw[i][j >> 1]);
-            if (c < a.width) part[c] = j & 1 ? f.y : f.x;
+            if (c < a.width) mine[c] = j & 1 ? f.y : f.x;
         }
+    if (kRows > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.width; c += kThreadsOf<W>) {
+            float v = 0.f;
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) v += reinterpret_cast<const float *>(ring)[k * a.width + c];
+            part[c] = v;
+        }
+    }
     if (BULK) {
         __syncthreads();
         if (*abort_flag) {                             // let copies in flight land before the CTA's memory is reused
@@ -400,15 +420,24 @@ ew_status_t launch(const Args &a, cudaStream_t st) {
 // (8192 x 2048: four warps a row 25.7 us, two 28.3, eight 28.8, one 33; one row: 2.0, 2.9, 1.8 us)
 template <class T, bool VEC>
 ew_status_t pick(const Args &a, cudaStream_t st) {
+    if (a.width <= 256) return launch<T, VEC, 1, 1>(a, st);
     if (a.width <= 512) return launch<T, VEC, 1, 2>(a, st);
-    if (a.width <= 1024) return launch<T, VEC, 4, 1>(a, st);
+    if (a.width <= 1024) return launch<T, VEC, 2, 2>(a, st);
     if (a.width <= 2048) return launch<T, VEC, 4, 2>(a, st);
-    if (a.width <= 4096) return launch<T, VEC, 4, 4>(a, st);
+    if (a.width <= 4096) return launch<T, VEC, 8, 2>(a, st);
     if (a.width <= 8192) return launch<T, VEC, 8, 4>(a, st);
     return launch<T, VEC, 16, 4>(a, st);
 }
 
-int grad_ctas(long long rows) { return (int)(rows < kMostCtas ? rows : kMostCtas); }
+// Up to here a warp a row, eight rows a CTA, then a CTA a row: with short rows a CTA a row has too few bytes on their way and meets at a
+// barrier a row (65536 x 256: 25.8 us against 157; 32768 x 512: 26.8, 81; 16384 x 1024: 26.1, 38; 600 x 1024: 5.3, 6.0; 400 x 512: 5.3, 5.0).
+// As many CTAs as stay on the SMs at once (65536 x 256: 444 of them 25.8 us, 296 34.6, 148 58; 32768 x 512: 296 26.8, 148 34.9,
+// 444 30.1; 16384 x 1024: 148 26.2, 296 28.9).
+constexpr int kNarrow = 1024;
+int grad_ctas(long long rows, int width) {
+    const long long wanted = width <= kNarrow ? (rows + 7) / 8 : rows, most = width <= 256 ? kMostCtas : width <= 512 ? 296 : width <= kNarrow ? 148 : kMostCtas;
+    return (int)(wanted < most ? wanted : most);
+}
 bool few_rows(long long rows, int width) { return rows <= kFewRows && width <= kFewWidth; }
 
 template <class T, bool VEC, int NV>
@@ -432,9 +461,11 @@ ew_status_t launch_few(GradArgs a, float *dw, cudaStream_t st) {
 
 template <class T, bool BULK, int W, int NV>
 ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
-    const int ctas = grad_ctas(a.rows), stage_bytes = a.width * 2 * (a.more ? 3 : 2), fit = kRingBytes / stage_bytes;
+    constexpr int kRows = kThreadsOf<W> / 32 / W;
+    const int ctas = grad_ctas(a.rows, a.width), stage_bytes = a.width * 2 * (a.more ? 3 : 2) * kRows, fit = kRingBytes / stage_bytes;
     a.stages = fit < 1 ? 1 : fit < kMostStages ? fit : kMostStages;
-    const ew_status_t s = launched(launch_pdl(grad_kernel<T, BULK, W, NV>, dim3((unsigned)ctas), dim3(W * 32), BULK ? a.stages * stage_bytes : 0, st, a), "RMS norm gradient");
+    const int sums = kRows > 1 ? kRows * a.width * 4 : 0, ring = BULK ? a.stages * stage_bytes : 0;
+    const ew_status_t s = launched(launch_pdl(grad_kernel<T, BULK, W, NV>, dim3((unsigned)ctas), dim3(kThreadsOf<W>), ring > sums ? ring : sums, st, a), "RMS norm gradient");
     if (s != EW_OK) return s;
     return launched(launch_pdl(parts_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(1024), 0, st, (const float *)a.parts, dw, ctas, a.width), "RMS norm gradient");
 }
@@ -442,7 +473,9 @@ ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
 template <class T, bool BULK>
 ew_status_t pick_grad(const GradArgs &a, float *dw, cudaStream_t st) {
     if (few_rows(a.rows, a.width)) return a.width <= 1024 ? launch_few<T, BULK, 1>(a, dw, st) : launch_few<T, BULK, 2>(a, dw, st);
-    if (a.width <= 1024) return launch_grad<T, BULK, 4, 1>(a, dw, st);
+    if (a.width <= 256) return launch_grad<T, BULK, 1, 1>(a, dw, st);
+    if (a.width <= 512) return launch_grad<T, BULK, 1, 2>(a, dw, st);
+    if (a.width <= kNarrow) return launch_grad<T, BULK, 1, 4>(a, dw, st);
     if (a.width <= 2048) return launch_grad<T, BULK, 4, 2>(a, dw, st);
     if (a.width <= 4096) return launch_grad<T, BULK, 8, 2>(a, dw, st);
     if (a.width <= 8192) return launch_grad<T, BULK, 16, 2>(a, dw, st);
@@ -457,10 +490,10 @@ int load_grad() {
 template <class T, bool VEC>
 int load_one() {
     cudaFuncAttributes fa;
-    return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 1>) |
-           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 4>) |
+    return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 1>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) |
+           (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 2, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 2>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) |
-           load_grad<T, VEC, 4, 1>() | load_grad<T, VEC, 4, 2>() | load_grad<T, VEC, 8, 2>() | load_grad<T, VEC, 16, 2>() | load_grad<T, VEC, 16, 4>() |
+           load_grad<T, VEC, 1, 1>() | load_grad<T, VEC, 1, 2>() | load_grad<T, VEC, 1, 4>() | load_grad<T, VEC, 4, 2>() | load_grad<T, VEC, 8, 2>() | load_grad<T, VEC, 16, 2>() | load_grad<T, VEC, 16, 4>() |
            (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
            (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 2>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
            (int)cudaFuncGetAttributes(&fa, parts_kernel);
@@ -507,7 +540,7 @@ extern "C" ew_status_t ew_rms_norm(int32_t device, int32_t dtype, const void *x,
 }
 
 extern "C" int32_t ew_rms_norm_grad_parts(int32_t rows, int32_t width) {
-    return rows < 1 || few_rows(rows, width) ? 0 : grad_ctas(rows);
+    return rows < 1 || few_rows(rows, width) ? 0 : grad_ctas(rows, width);
 }
 
 extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const void *dy, int64_t lddy, const void *t, int64_t ldt, const void *weight, const void *dt_in,
