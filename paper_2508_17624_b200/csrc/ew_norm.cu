@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
 
 constexpr int kMostCtas = 444;                         // of the gradient, three an SM, whose sums are the workspace (8192 x 2048: 27 us; two 34, four 31)
 constexpr int kMostStages = 3;
-constexpr int kRingBytes = 98304;                      // a CTA's rows on their way: at least one of the widest, of three operands
-static_assert(kMostWidth * 6 <= kRingBytes, "room for a row");
+// A CTA's rows on their way, at least one of the widest, of three operands; where one CTA has the SM, two (1024 x 16384: 45 us, with one 47.5)
+template <int W> constexpr int kRingBytes = W == 16 ? 196608 : 98304;
+static_assert(kMostWidth * 6 * 2 <= kRingBytes<16>, "room for two rows");
 
 struct GradArgs {
     const void *dy, *t, *weight, *more;
@@ -165,12 +166,16 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
     if (BULK && fetcher)
         for (int i = 0; i < a.stages; ++i)
             if (first + i * step < a.rows) fetch(first + i * step, i);
-    Two weight[NV][4], dw[NV][4];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    constexpr bool kHold = W * NV < 64;                // the weights in registers; those of the widest rows are read again (4096 x 16384: 106 us, held 123, for what spills)
+    Two weight[kHold ? NV : 1][4], dw[NV][4];
+    auto weight_of = [&](Two (&v)[4], int i) {
         Eight<T> x;
         load_span<T, BULK>(x, reinterpret_cast<const T *>(a.weight), (i * W + w) * kSpan, lane, a.width);
-        to_pairs(weight[i], x);
+        to_pairs(v, x);
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (kHold) weight_of(weight[i], i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) dw[i][j] = two(0.f, 0.f);
     }
@@ -205,10 +210,12 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
             clear_span<T, BULK>(t[i], (i * W + w) * kSpan, lane, a.width);
             to_pairs(tv, t[i]);
             to_pairs(dv, dy[i]);
+            if (!kHold) weight_of(weight[0], i);
+            Two (&wv)[4] = weight[kHold ? i : 0];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 square = fma2(tv[j], tv[j], square);
-                along2 = fma2(mul2(dv[j], weight[i][j]), tv[j], along2);
+                along2 = fma2(mul2(dv[j], wv[j]), tv[j], along2);
             }
         }
         float sums[2] = {parts_of(square).x + parts_of(square).y, parts_of(along2).x + parts_of(along2).y};
@@ -229,12 +236,14 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
             Two tv[4], dv[4], mv[4];
             to_pairs(tv, t[i]);
             to_pairs(dv, dy[i]);
+            if (!kHold) weight_of(weight[0], i);
+            Two (&wv)[4] = weight[kHold ? i : 0];
             if (a.more) to_pairs(mv, more[i]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const Two scaled = mul2(dv[j], norm2);
                 dw[i][j] = fma2(scaled, tv[j], dw[i][j]);
-                tv[j] = fma2(scaled, weight[i][j], a.more ? fma2(tv[j], back, mv[j]) : mul2(tv[j], back));
+                tv[j] = fma2(scaled, wv[j], a.more ? fma2(tv[j], back, mv[j]) : mul2(tv[j], back));
             }
             from_pairs(dt, tv);
             store_span<T, BULK>(dt, reinterpret_cast<T *>(a.dt) + r * a.lddt, (i * W + w) * kSpan, lane, a.width);
@@ -417,7 +426,9 @@ ew_status_t launch(const Args &a, cudaStream_t st) {
     return launched(launch_pdl(norm_kernel<T, VEC, W, NV>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kThreadsOf<W>), 0, st, a), "RMS norm");
 }
 
-// (8192 x 2048: four warps a row 25.7 us, two 28.3, eight 28.8, one 33; one row: 2.0, 2.9, 1.8 us)
+// (8192 x 2048: four warps a row 25.7 us, two 28.3, eight 28.8, one 33; one row: 2.0, 2.9, 1.8 us.  65536 x 256: one span a lane 26.1, two
+// 33.4; 32768 x 512: one warp 25.3, two 35, four 44; 16384 x 1024: two 25.5, four 27.3; 4096 x 4096: eight 26.3, four 27.2; 2048 x 8192: eight
+// 30.4, sixteen 41)
 template <class T, bool VEC>
 ew_status_t pick(const Args &a, cudaStream_t st) {
     if (a.width <= 256) return launch<T, VEC, 1, 1>(a, st);
@@ -432,10 +443,11 @@ ew_status_t pick(const Args &a, cudaStream_t st) {
 // Up to here a warp a row, eight rows a CTA, then a CTA a row: with short rows a CTA a row has too few bytes on their way and meets at a
 // barrier a row (65536 x 256: 25.8 us against 157; 32768 x 512: 26.8, 81; 16384 x 1024: 26.1, 38; 600 x 1024: 5.3, 6.0; 400 x 512: 5.3, 5.0).
 // As many CTAs as stay on the SMs at once (65536 x 256: 444 of them 25.8 us, 296 34.6, 148 58; 32768 x 512: 296 26.8, 148 34.9,
-// 444 30.1; 16384 x 1024: 148 26.2, 296 28.9).
+// 444 30.1; 16384 x 1024: 148 26.2, 296 28.9; 4096 x 4096: 296 29.8, 444 33.9; 2048 x 8192: 148 30.1, 296 35, 444 42; 1024 x 16384: 148 47, 444 69).
 constexpr int kNarrow = 1024;
 int grad_ctas(long long rows, int width) {
-    const long long wanted = width <= kNarrow ? (rows + 7) / 8 : rows, most = width <= 256 ? kMostCtas : width <= 512 ? 296 : width <= kNarrow ? 148 : kMostCtas;
+    const long long wanted = width <= kNarrow ? (rows + 7) / 8 : rows,
+                    most = width <= 256 ? kMostCtas : width <= 512 ? 296 : width <= kNarrow ? 148 : width <= 2048 ? kMostCtas : width <= 4096 ? 296 : 148;
     return (int)(wanted < most ? wanted : most);
 }
 bool few_rows(long long rows, int width) { return rows <= kFewRows && width <= kFewWidth; }
@@ -462,7 +474,7 @@ ew_status_t launch_few(GradArgs a, float *dw, cudaStream_t st) {
 template <class T, bool BULK, int W, int NV>
 ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
     constexpr int kRows = kThreadsOf<W> / 32 / W;
-    const int ctas = grad_ctas(a.rows, a.width), stage_bytes = a.width * 2 * (a.more ? 3 : 2) * kRows, fit = kRingBytes / stage_bytes;
+    const int ctas = grad_ctas(a.rows, a.width), stage_bytes = a.width * 2 * (a.more ? 3 : 2) * kRows, fit = kRingBytes<W> / stage_bytes;
     a.stages = fit < 1 ? 1 : fit < kMostStages ? fit : kMostStages;
     const int sums = kRows > 1 ? kRows * a.width * 4 : 0, ring = BULK ? a.stages * stage_bytes : 0;
     const ew_status_t s = launched(launch_pdl(grad_kernel<T, BULK, W, NV>, dim3((unsigned)ctas), dim3(kThreadsOf<W>), ring > sums ? ring : sums, st, a), "RMS norm gradient");
@@ -484,7 +496,7 @@ ew_status_t pick_grad(const GradArgs &a, float *dw, cudaStream_t st) {
 
 template <class T, bool BULK, int W, int NV>
 int load_grad() {
-    return (int)cudaFuncSetAttribute(grad_kernel<T, BULK, W, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+    return (int)cudaFuncSetAttribute(grad_kernel<T, BULK, W, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<W>);
 }
 
 template <class T, bool VEC>

@@ -364,7 +364,7 @@ def test_norm_grad(rows, width, pad, with_dt, dtype):
 
 
 @pytest.mark.parametrize("with_dt", [True, False])
-@pytest.mark.parametrize("rows,width", [(4000, 256), (2500, 512), (3000, 1000), (9000, 1024), (2500, 2048), (700, 8192), (3000, 300)])
+@pytest.mark.parametrize("rows,width", [(4000, 256), (2500, 512), (3000, 1000), (9000, 1024), (2500, 2048), (1500, 4096), (700, 8192), (900, 16384), (3000, 300)])
 def test_norm_grad_reads_no_earlier_row(rows, width, with_dt):
     """Two sets of inputs in turn: what a call finds in shared memory is of the other set, and must not show."""
     sets = [(randn((rows, width), BF16, s, 0.1), randn((rows, width), BF16, s + 1, 0.5), 1 + randn((width,), BF16, s + 2, 0.2),
