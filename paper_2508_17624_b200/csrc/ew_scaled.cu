@@ -486,7 +486,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             };
             gather(0);
             for (int kb = 0; kb < it.kb; kb += 4) {
-                if (!(ok = wait_warp(bar_sempty + 8 * slot, phase ^ 1, abort_flag, a.err))) break;
+                if (!(ok = wait_all<false>(bar_sempty + 8 * slot, phase ^ 1, abort_flag, a.err))) break;
                 uint4 *to = reinterpret_cast<uint4 *>(scales + slot * C::kSlotBytes) + lane;
                 to[0] = make_uint4(w_word, w_word, w_word, w_word);
 #pragma unroll
@@ -511,7 +511,7 @@ scaled_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             const size_t at = (size_t)it.row0 * a.ldo + f;
             for (int kb = 0; kb < it.kb; kb += it.chunk) {
                 // (the two warps of a pair meet at barriers below, so they go on or give up together)
-                if (!(ok = both_of_pair(wait_warp(bar_tfull + 8 * acc, acc_phases >> acc & 1, abort_flag, a.err)))) break;
+                if (!(ok = both_of_pair(wait_all<false>(bar_tfull + 8 * acc, acc_phases >> acc & 1, abort_flag, a.err)))) break;
                 tc_fence_after();
                 const uint32_t lanes = tmem_base + ((uint32_t)(lg * 32) << 16), t0 = lanes + acc * NT;
                 const bool here = sums_here(it);
