@@ -54,8 +54,9 @@ constexpr int kMaps = 8;                               // row boxes of 16, 32 ..
 constexpr int kTiles = 2;                              // 16-bit results on their way out: tiles of 64 f x 32 rows of each pair of epilogue warps
 // Long sums are made in parts that the epilogue adds up in fp32, as in the 16-bit products and for the same reason: 2048 terms for
 // fp32 results, 8192 for fp16, 65536 for bf16.  (Products of 8-bit values have few digits: over terms of one sign and size 1.1e-7 of the result is cut
-// off in 1024 of them; but with a first block 2^12 times the others up to 7e-6, 1.4e-5 in 2048, 5.5e-5 in 8192: two steps of 2^-23 an
-// instruction.)
+// off in 1024 of them; with a first block 2^12 times the others up to 7e-6, 1.4e-5 in 2048, 5.5e-5 in 8192.  At most it is what lies below 2^-25 of
+// the largest addend's power of two, of 33 addends an instruction, and the sum's 24th bit: 9.25 steps of 2^-23 an instruction, 7.1e-5 in 2048 terms
+// (a first term 2^26 times all others: 5.4e-5 measured), 2.8e-4 in 8192, 2.3e-3 in 65536, where the worst order of fp32 additions loses 1.2e-4, 4.9e-4, 3.9e-3.)
 constexpr int sum_blocks(int out_dtype) { return (out_dtype == EW_FP32 ? 2048 : out_dtype == EW_FP16 ? 8192 : 65536) / kBlock; }
 
 struct Args {
