@@ -330,10 +330,11 @@ typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2, EW_E4M3 = 3, EW_E5M2 = 4 }
 /* Matrix product grouped by expert (Section 2.1's grouped matrix multiplication, on its own): for every group g and
  * its rows offsets[g] <= r < offsets[g+1]
  *     y[r, :] = x[r, :] w[g]^T        x [rows, k], w [groups, n, k] (group_stride elements between groups), y [rows, n]
- * summed in fp32 and rounded once.  The tensor core cuts the running sum off instead of rounding it; sums are made in parts
- * (1024 terms for fp32 results, 8192 for fp16, 65536 for bf16) that are added up rounded, so that the result is off by at most
- * 1e-5 (fp32 results) or an eighth of half a step of its type (16-bit ones) of sum |x w| besides its own rounding and half a step
- * of fp32 a part.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
+ * summed in fp32 and rounded once.  An instruction of the tensor core adds 16 products to the running sum and cuts off, instead of
+ * rounding, what lies below 2^-25 of the largest or behind the sum's 24th bit; sums are made in parts (1024 terms for fp32 results,
+ * 8192 for fp16, 65536 for bf16) that are added up rounded.  A result is off by at most 4.1e-5 (fp32), 3.3e-4 (fp16) or 2.6e-3 (bf16; 0.66 of half a
+ * step of either) of sum |x w| besides its own rounding and half a step of fp32 a part: that much only if one term is 2^25 times nearly all of the others.
+ * Terms of like sizes: 1e-5 (fp32) or an eighth of half a step.  offsets: int32 [groups + 1], ascending, as ew_moe_forward_debug gives them;
  * they need not start at 0 nor end at `rows`, and rows outside them are left as they were.  An offset below the one
  * before it or outside [0, rows] is clamped and reported as EW_ERR_INVALID_ARG.
  * dtype: EW_BF16 or EW_FP16; out_dtype: the same or EW_FP32.  x and w are 16-byte aligned with ldx, ldw and

@@ -41,3 +41,25 @@ def test_sums_next_to_the_last_bit(out_dtype, k):
             ref = values(q, s).sum(1)[:, None]
             off = (binding.scaled_mm(q, s, w, ws, out_dtype=out_dtype).double() - ref).abs() / ref
             assert (off <= loss(k, out_dtype, TERMS, 32)).all(), (first, m, float(off.max()))
+
+
+@pytest.mark.parametrize("dtype,out_dtype,k", [(BF16, FP32, 1024), (BF16, FP32, 5000), (FP16, FP16, 8192), (BF16, BF16, 70000)], ids=str)
+def test_sums_of_16_bit_products_next_to_the_last_bit(dtype, out_dtype, k):
+    """The same for the grouped products and their gradients."""
+    parts_of, most = {FP32: 1024, FP16: 8192, BF16: 65536}, 31 if dtype == BF16 else 14       # (fp16 ends at 2^-14)
+    offsets = torch.tensor([0, most], dtype=torch.int32, device="cuda")
+    for first in (1, 64):
+        for m in (1.0, 1.9921875):
+            x = torch.exp2(-torch.arange(most, device="cuda").double())[:, None] * torch.full((1, k), m, dtype=torch.float64, device="cuda")
+            x[:, :64] = 0
+            x[:, :first] = 1
+            x = x.to(dtype)
+            ref = x.double().sum(1)
+            for call, w in ((binding.grouped_mm, torch.ones((1, 16, k), dtype=dtype, device="cuda")), (binding.grouped_mm_dx, torch.ones((1, k, 16), dtype=dtype, device="cuda"))):
+                off = (call(x, w, offsets, out_dtype=out_dtype).double() - ref[:, None]).abs() / ref[:, None]
+                assert (off <= loss(k, out_dtype, parts_of, 16)).all(), (call.__name__, first, m, float(off.max()))
+            rows = torch.ones((k, 16), dtype=dtype, device="cuda")
+            wide = torch.zeros((k, 32), dtype=dtype, device="cuda")[:, :most].copy_(x.t())
+            got = binding.grouped_mm_dw(wide, rows, torch.tensor([0, k], dtype=torch.int32, device="cuda"), out_dtype=out_dtype)[0].double()
+            off = (got - ref[:, None]).abs() / ref[:, None]
+            assert (off <= loss(k, out_dtype, parts_of, 16)).all(), ("dw", first, m, float(off.max()))
