@@ -311,8 +311,9 @@ class Pool:
 # ---------------------------------------------------------------------------------------------------------------------
 # Stand-alone operators (no pool): argument checks, output allocation, one library call on the current stream.  A small
 # call takes the GPU less time than the host, so the checks of a good call are a handful of comparisons; only when one of
-# them fails does `_on` find out which and say so.  autograd does not see the calls: an operand that it is recording is
-# refused, since a result without a gradient would go unnoticed (torch.autograd.Function runs its two halves unrecorded).
+# them fails does `_on` find out which and say so.  autograd does not see the calls: an operand that it is recording, or that carries
+# a tangent of forward-mode differentiation, is refused, since a result without one would go unnoticed (torch.autograd.Function runs
+# its halves unrecorded and without tangents).
 class _Torch:
     """What the operators need of torch, resolved on first use (the package imports without it)."""
     ready = False
@@ -320,6 +321,8 @@ class _Torch:
     @classmethod
     def load(cls):
         import torch
+        from torch.autograd import forward_ad
+        cls.forward = forward_ad
         cls.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         cls.int32, cls.float32, cls.uint8, cls.bfloat16 = torch.int32, torch.float32, torch.uint8, torch.bfloat16
         cls.e4m3, cls.e5m2, cls.exponent = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
@@ -350,6 +353,14 @@ def _on(t, like=None, ndim=2, name="operand", dtype=None):
 def _recorded(where):
     raise ValueError(f"{where}: autograd is recording an operand and would lose its gradient here; call it under torch.no_grad() or inside "
                      "a torch.autograd.Function, and the gradient's operators in its backward")
+
+
+def _without_tangents(where, *operands):
+    """For calls while forward-mode differentiation is on (torch.no_grad() leaves it on)."""
+    for t in operands:
+        if t is not None and _Torch.forward.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{where}: forward-mode autograd's tangent of a tensor would be lost here; pass what torch.autograd.forward_ad.unpack_dual "
+                             "gives, or call it inside a torch.autograd.Function that has a jvp")
 
 
 def _code(T, dtype) -> int:
@@ -411,6 +422,8 @@ def _result(out, shape, dtype, like, name="out"):
         return like.new_empty(shape, dtype=dtype)
     if out.requires_grad and _torch().recording():
         raise ValueError(f"{name}: autograd is recording it and would not see it overwritten; pass it under torch.no_grad(), or a tensor of its own")
+    if _torch().forward._current_level >= 0:
+        _without_tangents(name, out)
     _on(out, like, len(shape), name)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise ValueError(f"{name}: {tuple(shape)} of {dtype} is wanted, got {tuple(out.shape)} of {out.dtype}")
@@ -421,6 +434,8 @@ def _rows_product(fn, where, a, w, offsets, out, out_dtype, grad):
     T, dev, dtype = _torch(), a.get_device(), a.dtype
     if (a.requires_grad or w.requires_grad) and T.recording():
         _recorded(where)
+    if T.forward._current_level >= 0:
+        _without_tangents(where, a, w)
     code = _code(T, dtype)
     rows, width, lda = _matrix(a, dev, dtype, "the rows' operand", None)
     groups, n, k, ldw, stride = _matrices(w, dev, dtype, "w", a)
@@ -462,6 +477,8 @@ def grouped_mm_dw(dy, x, offsets, out=None, out_dtype=None, accumulate=False):
     T, dev, dtype = _torch(), dy.get_device(), dy.dtype
     if (dy.requires_grad or x.requires_grad) and T.recording():
         _recorded("ew_grouped_mm_dw")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_grouped_mm_dw", dy, x)
     code = _code(T, dtype)
     rows, n, lddy = _matrix(dy, dev, dtype, "dy", None)
     x_rows, k, ldx = _matrix(x, dev, dtype, "x", dy)
@@ -509,6 +526,8 @@ def quant_mv(x, q, scales, slots=None, out=None, out_dtype=None):
     T, dev, dtype = _torch(), x.get_device(), x.dtype
     if (x.requires_grad or scales.requires_grad) and T.recording():
         _recorded("ew_quant_mv")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_quant_mv", x, scales)
     code = _code(T, dtype)
     rows, k, ldx = _matrix(x, dev, dtype, "x", None)
     if not _good(q, dev, T.uint8, 3):
@@ -558,6 +577,8 @@ def swiglu(h, row_weights=None, out=None):
     T, dev, dtype = _torch(), h.get_device(), h.dtype
     if (h.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
         _recorded("ew_swiglu")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_swiglu", h, row_weights)
     code = _code(T, dtype)
     rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     if two < 2 or two % 2:
@@ -580,6 +601,8 @@ def swiglu_grad(dact, h, row_weights=None, out=None):
     T, dev, dtype = _torch(), h.get_device(), h.dtype
     if (h.requires_grad or dact.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
         _recorded("ew_swiglu_grad")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_swiglu_grad", dact, h, row_weights)
     code = _code(T, dtype)
     rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     d_rows, inter, ldd = _matrix(dact, dev, dtype, "dact", h)
@@ -632,6 +655,8 @@ def scaled_rows(x, dtype=None, out=None):
     T, dev = _torch(), x.get_device()
     if x.requires_grad and T.recording():
         _recorded("ew_scaled_rows")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_scaled_rows", x)
     code = _code(T, x.dtype)
     if dtype is None:
         dtype = T.e4m3
@@ -671,6 +696,8 @@ def _scaled_product(where, a, a_scales, w, w_scales, offsets, out, out_dtype, gr
     T, dev = _torch(), a.get_device()
     if (a.requires_grad or w.requires_grad) and T.recording():
         _recorded(where)
+    if T.forward._current_level >= 0:
+        _without_tangents(where, a, w)
     row_type = _eight(T, a.dtype, "the rows' operand")
     rows, width, lda = _matrix(a, dev, a.dtype, "the rows' operand", None)
     groups, n, k, ldw, stride = _matrices(w, dev, T.e4m3, "w", a)
@@ -736,6 +763,8 @@ def swiglu_scaled(h, row_weights=None, out=None):
     T, dev, dtype = _torch(), h.get_device(), h.dtype
     if (h.requires_grad or (row_weights is not None and row_weights.requires_grad)) and T.recording():
         _recorded("ew_swiglu_scaled")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_swiglu_scaled", h, row_weights)
     code = _code(T, dtype)
     rows, two, ldh = _matrix(h, dev, dtype, "h", None)
     if two < 2 or two % 2:
@@ -780,6 +809,8 @@ def _norm(x, weight, residual, eps, y, with_y, blocks, with_blocks, total):
     T, dev = _torch(), x.get_device()
     if (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)) and T.recording():
         _recorded("ew_rms_norm")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_rms_norm", x, weight, residual)
     code, rows, width, ldx = _norm_operands(x, weight, T, dev)
     res = total_at = y_at = q_at = scales_at = None
     ldr = ldt = ldy = ldq = lds = 0
@@ -823,6 +854,8 @@ def rms_norm_grad(dy, t, weight, dt=None, eps=1e-6, out=None):
     T, dev = _torch(), t.get_device()
     if (dy.requires_grad or t.requires_grad or weight.requires_grad or (dt is not None and dt.requires_grad)) and T.recording():
         _recorded("ew_rms_norm_grad")
+    if T.forward._current_level >= 0:
+        _without_tangents("ew_rms_norm_grad", dy, t, weight, dt)
     code, rows, width, ldt = _norm_operands(t, weight, T, dev)
     dy_at, lddy = _beside(dy, rows, width, "dy", t, dev)
     dt_at, lddt = (None, 0) if dt is None else _beside(dt, rows, width, "dt", t, dev)
