@@ -437,6 +437,10 @@ ew_status_t ew_scaled_mm_dx(int32_t device, int32_t row_type, int32_t out_dtype,
                             const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k, void *dx, int64_t lddx,
                             void *cuda_stream);
 
+/* The kernel's form that ew_scaled_mm (input_gradient: ew_scaled_mm_dx) takes for these sizes on a device with so many SMs, for profiles and
+ * tests: 0 = one CTA a tile, 1 = a CTA pair whose results leave by eight warps, 2 = by four.  Its results are the same to rounding. */
+int32_t ew_scaled_mm_form(int32_t input_gradient, int32_t rows, int32_t groups, int32_t n, int32_t k, int32_t sm_count);
+
 /* ew_swiglu with its result as blocks of rows in EW_E4M3 (rounded once, from fp32). */
 ew_status_t ew_swiglu_scaled(int32_t device, int32_t dtype, const void *h, int64_t ldh, const float *row_weights, int32_t rows,
                              int32_t inter, void *q, int64_t ldq, void *scales, int64_t ldscales, void *cuda_stream);

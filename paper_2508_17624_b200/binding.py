@@ -24,7 +24,7 @@ EXPORTS = ["ew_pool_create", "ew_pool_destroy", "ew_load_base", "ew_load_adapter
            "ew_pool_trim", "ew_moe_forward", "ew_moe_forward_debug", "ew_moe_forward_host", "ew_profile_enable",
            "ew_profile_read", "ew_reroute", "ew_reroute_unfused", "ew_route_logits", "ew_route_noalloc", "ew_selftest_bounded_wait", "ew_get_expert_map",
            "ew_moe_forward_partial", "ew_ep_finish", "ew_moe_forward_scatter", "ew_ep_finish_gathered", "ew_pool_stats", "ew_last_device_error", "ew_slot_address", "ew_grouped_mm", "ew_grouped_mm_dx", "ew_grouped_mm_dw",
-           "ew_quant_mv", "ew_quant_pack", "ew_swiglu", "ew_swiglu_grad", "ew_scaled_rows", "ew_scaled_pack", "ew_scaled_mm", "ew_scaled_mm_dx",
+           "ew_quant_mv", "ew_quant_pack", "ew_swiglu", "ew_swiglu_grad", "ew_scaled_rows", "ew_scaled_pack", "ew_scaled_mm", "ew_scaled_mm_dx", "ew_scaled_mm_form",
            "ew_swiglu_scaled", "ew_rms_norm", "ew_rms_norm_grad", "ew_rms_norm_grad_parts", "ew_last_operator_error", "ew_status_str", "ew_last_error_string"]
 
 

@@ -641,6 +641,20 @@ bool bad_matrix(const void *p, long long ld, long long width) {
     return !p || ((uintptr_t)p & 15) || ld < width || (ld & 15) || ld >= (1ll << 39);
 }
 
+// The form that a product takes: ew_scaled_mm_form's numbers.
+// One CTA with 128 columns against the pair: 64 groups of 2816 x 2048 with 96 rows each 69.4 and 69.8 us, 128 rows 73.0 and 72.7, 144 rows 95.7
+// and 75.7; where the pairs' tiles would not fill the GPU (8 groups of 1024 x 512, 160 rows each) 6.7 and 7.5.  (The host
+// knows only how many groups there are, not which have rows: over many empty ones the one-CTA form may be taken where the pair would
+// be faster.)
+// Short sums: the results' way out is what counts, and eight warps walk it (20000 rows, 16 groups, n = 1408; k = 256: 19.6 us
+// against 23.8, 512: 22.4 and 25.8, 1024: 31.5 and 32.3); long ones: at the power limit four cost less (2048, 49152 rows: 285 and 289).
+enum Form { kOneCta = 0, kPairEight = 1, kPairFour = 2 };
+Form form_of(long long rows, long long groups, long long f, long long t, int sm_count) {
+    const long long live = groups < rows ? groups : rows, pair_tiles = (live + rows / 224) * ((f + 255) / 256);
+    if (rows <= 128 * groups || pair_tiles <= sm_count / 2) return kOneCta;
+    return t <= 1024 ? kPairEight : kPairFour;
+}
+
 ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dtype, const void *x, int64_t ldx, const void *x_scales, int64_t lds, const void *w,
                     int64_t ldw, int64_t group_stride, const void *w_scales, const int32_t *offsets, int32_t rows, int32_t groups, int32_t n, int32_t k, void *out,
                     int64_t ldo, void *stream) {
@@ -696,15 +710,11 @@ ew_status_t product(bool grad, int32_t device, int32_t row_type, int32_t out_dty
     }
     cudaStream_t st = (cudaStream_t)stream;
 #define EW_LAUNCH(CG, NT, EW) (grad ? launch<CG, NT, EW, kInputGrad>(*d, ma, mb, mo, a, st) : launch<CG, NT, EW, kProduct>(*d, ma, mb, mo, a, st))
-    // One CTA with 128 columns against the pair: 64 groups of 2816 x 2048 with 96 rows each 69.4 and 69.8 us, 128 rows 73.0 and 72.7, 144 rows 95.7
-    // and 75.7; where the pairs' tiles would not fill the GPU (8 groups of 1024 x 512, 160 rows each) 6.7 and 7.5.  (The host
-    // knows only how many groups there are, not which have rows: over many empty ones the one-CTA form may be taken where the pair would
-    // be faster.)
-    const long long live = groups < rows ? groups : rows, pair_tiles = (live + rows / 224) * ((f + 255) / 256);
-    if (rows <= 128ll * groups || pair_tiles <= d->sm_count / 2) return EW_LAUNCH(1, 128, 4);
-    // Short sums: the results' way out is what counts, and eight warps walk it (20000 rows, 16 groups, n = 1408; k = 256: 19.6 us
-    // against 23.8, 512: 22.4 and 25.8, 1024: 31.5 and 32.3); long ones: at the power limit four cost less (2048, 49152 rows: 285 and 289).
-    return t <= 1024 ? EW_LAUNCH(2, 224, 8) : EW_LAUNCH(2, 224, 4);
+    switch (form_of(rows, groups, f, t, d->sm_count)) {
+        case kOneCta: return EW_LAUNCH(1, 128, 4);
+        case kPairEight: return EW_LAUNCH(2, 224, 8);
+        default: return EW_LAUNCH(2, 224, 4);
+    }
 #undef EW_LAUNCH
 }
 
@@ -728,4 +738,8 @@ extern "C" ew_status_t ew_scaled_mm_dx(int32_t device, int32_t row_type, int32_t
                                        const void *w, int64_t ldw, int64_t group_stride, const void *w_scales, const int32_t *offsets, int32_t rows, int32_t groups,
                                        int32_t n, int32_t k, void *dx, int64_t lddx, void *cuda_stream) {
     return ew::ops::product(true, device, row_type, out_dtype, dy, lddy, dy_scales, lddys, w, ldw, group_stride, w_scales, offsets, rows, groups, n, k, dx, lddx, cuda_stream);
+}
+
+extern "C" int32_t ew_scaled_mm_form(int32_t input_gradient, int32_t rows, int32_t groups, int32_t n, int32_t k, int32_t sm_count) {
+    return ew::ops::form_of(rows, groups, input_gradient ? k : n, input_gradient ? n : k, sm_count);
 }

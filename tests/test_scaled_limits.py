@@ -3,7 +3,9 @@ import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
 
-from paper_2508_17624_b200 import binding
+from paper_2508_17624_b200 import binding, build
+
+from test_gpu_scaled_limits import FORMS, form
 
 BF16, E4M3, E8M0 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
 
@@ -50,3 +52,13 @@ def test_operators_inside_a_function_with_a_jvp():
     with forward_ad.dual_level():
         out = Norm.apply(forward_ad.make_dual(x, 2 * x), weight)
         assert torch.equal(forward_ad.unpack_dual(out).tangent, 2 * x)
+
+
+def test_the_listed_sizes_reach_every_form():
+    """A rule that changes must not leave a form of the product's kernel without its tests."""
+    build.build()
+    assert [form(grad, counts, n, k, 21, 148) for _, grad, counts, n, k, *_ in FORMS] == [case[0] for case in FORMS]
+    for want in range(3):
+        assert {case[1] for case in FORMS if case[0] == want} == {False, True}
+        assert {case[6] for case in FORMS if case[0] == want} == {BF16, torch.float16, torch.float32}
+    assert form(False, (768,) * 64, 2816, 2048, 0, 148) == form(True, (384,) * 64, 2048, 1408, 0, 148) == 2 and form(False, (16,) * 96, 2816, 2048, 0, 148) == 0
