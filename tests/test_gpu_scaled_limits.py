@@ -162,3 +162,16 @@ def test_a_pair_clamps_and_reports_bad_offsets(ends):
     fixed = np.maximum.accumulate(np.clip(ends, 0, 1500)).tolist()
     binding.scaled_mm(*rows, *weights, torch.tensor(fixed, dtype=torch.int32, device="cuda"), out=want)
     assert torch.equal(got, want) and binding.last_operator_error() == 0
+
+
+def test_rows_gathered_by_index():
+    """As the README does: a token's rows, once for each of its experts, by indexing both parts of the blocks."""
+    tokens, hidden, inter, experts = 50, 512, 128, 4
+    q, s, x, t = binding.rms_norm_scaled(uneven((tokens, hidden), BF16, 1), torch.ones(hidden, dtype=BF16, device="cuda"), uneven((tokens, hidden), BF16, 2), with_y=True)
+    w = binding.scaled_pack(uneven((experts, 2 * inter, hidden), BF16, 3, 0.05))
+    token = torch.arange(2 * tokens, device="cuda") % tokens
+    offsets = torch.tensor([0, 30, 30, 31, 100], dtype=torch.int32, device="cuda")
+    y = binding.scaled_mm(q[token], s[token], *w, offsets)
+    for g, (i, j) in enumerate(zip(offsets.tolist()[:-1], offsets.tolist()[1:])):
+        xd, wd = values(q, s)[token[i:j]], values(w[0][g:g + 1], w[1][g:g + 1])[0].t()
+        near(y[i:j], xd @ wd, xd.abs() @ wd.abs(), hidden, g)
