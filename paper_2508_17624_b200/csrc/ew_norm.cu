@@ -387,6 +387,7 @@ __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(c
         for (int k = 1; k < kTeams; ++k) v += columns[k * a.width + c];
         columns[c] = v;
     }
+    __syncwarp();                                      // (the cluster's barrier is one of whole warps, and the last turn of such a loop may have had a part of one)
     tc::cluster_sync_all();
     const int share = (a.width + kCluster - 1) / kCluster, from = rank * share, to = min(from + share, a.width);
     for (int c = from + threadIdx.x; c < to; c += kTeams * W * 32) {
@@ -397,6 +398,7 @@ __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(c
         for (int k = 0; k < kCluster; ++k) v += x[k];
         a.parts[c] = v;
     }
+    __syncwarp();
     tc::cluster_sync_all();                            // until then the others read this CTA's sums
 }
 
