@@ -14,6 +14,8 @@
 #include "ew_ops.h"
 #include "ew_tc.cuh"
 
+#include <cstdlib>
+
 namespace ew {
 namespace ops {
 namespace {
@@ -282,7 +284,8 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
 // order.  One launch and no workspace take the host 4 us less, which is what a call of few rows waits for: 2048 columns, alone and called from
 // Python, 128 rows 6.7 and 11.9 us, with the two kernels above 7.7 and 16; 333 rows 10.5 and 12 against 9.3 and 16; 512 rows 13.5 and 13.9 against
 // 9.0 and 16.  (Clusters of eight, the portable size: 333 rows 16 us.)
-constexpr int kCluster = 16, kTeams = 4, kTeamWarps = 4;
+// (A device whose GPCs, or what this process has of them, hold no cluster of sixteen takes one of eight, which all hold.)
+constexpr int kMostCluster = 16, kPortableCluster = 8, kTeams = 4, kTeamWarps = 4;
 constexpr int kFewRows = 384, kFewWidth = 2048;
 
 __device__ __forceinline__ float peer_value(const float *p, uint32_t rank) {
@@ -291,14 +294,14 @@ __device__ __forceinline__ float peer_value(const float *p, uint32_t rank) {
     return v;
 }
 
-template <class T, bool VEC, int NV>
+template <class T, bool VEC, int NV, int CLUSTER>
 __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(const GradArgs a) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     constexpr int W = kTeamWarps;
     extern __shared__ float columns[];                 // [kTeams][width]
     __shared__ __align__(16) float part[kTeams][2][2][W];
-    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W, team = (threadIdx.x >> 5) / W, step = kCluster * kTeams;
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % W, team = (threadIdx.x >> 5) / W, step = CLUSTER * kTeams;
     const int rank = (int)tc::cluster_ctarank();
     Eight<T> dy[NV], t[NV], more[NV];
     auto load = [&](int r) {
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(c
             load_span<T, VEC>(more[i], more_row, (i * W + w) * kSpan, lane, a.width);
         }
     };
-    const int first = rank + kCluster * team;          // (one row a CTA before two)
+    const int first = rank + CLUSTER * team;          // (one row a CTA before two)
     load(first);
     Two weight[NV][4], dw[NV][4];
 #pragma unroll
@@ -389,13 +392,13 @@ __global__ void __launch_bounds__(kTeams * kTeamWarps * 32, 1) few_rows_kernel(c
     }
     __syncwarp();                                      // (the cluster's barrier is one of whole warps, and the last turn of such a loop may have had a part of one)
     tc::cluster_sync_all();
-    const int share = (a.width + kCluster - 1) / kCluster, from = rank * share, to = min(from + share, a.width);
+    const int share = (a.width + CLUSTER - 1) / CLUSTER, from = rank * share, to = min(from + share, a.width);
     for (int c = from + threadIdx.x; c < to; c += kTeams * W * 32) {
-        float x[kCluster], v = 0.f;
+        float x[CLUSTER], v = 0.f;
 #pragma unroll
-        for (int k = 0; k < kCluster; ++k) x[k] = peer_value(columns + c, k);
+        for (int k = 0; k < CLUSTER; ++k) x[k] = peer_value(columns + c, k);
 #pragma unroll
-        for (int k = 0; k < kCluster; ++k) v += x[k];
+        for (int k = 0; k < CLUSTER; ++k) v += x[k];
         a.parts[c] = v;
     }
     __syncwarp();
@@ -454,23 +457,30 @@ int grad_ctas(long long rows, int width) {
 }
 bool few_rows(long long rows, int width) { return rows <= kFewRows && width <= kFewWidth; }
 
+// One cluster of so many CTAs
+void few_config(cudaLaunchConfig_t *cfg, cudaLaunchAttribute *attr, int cluster, int width) {
+    cfg->gridDim = dim3(cluster);
+    cfg->blockDim = dim3(kTeams * kTeamWarps * 32);
+    cfg->dynamicSmemBytes = (size_t)kTeams * width * 4;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = cluster;
+    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+    cfg->attrs = attr;
+    cfg->numAttrs = 1;
+}
+
 template <class T, bool VEC, int NV>
-ew_status_t launch_few(GradArgs a, float *dw, cudaStream_t st) {
+ew_status_t launch_few(const Device &d, GradArgs a, float *dw, cudaStream_t st) {
     a.parts = dw;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kCluster);
-    cfg.blockDim = dim3(kTeams * kTeamWarps * 32);
-    cfg.dynamicSmemBytes = (size_t)kTeams * a.width * 4;
-    cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    few_config(&cfg, attr, d.few_rows_cluster, a.width);
+    cfg.stream = st;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return launched((int)cudaLaunchKernelEx(&cfg, few_rows_kernel<T, VEC, NV>, a), "RMS norm gradient");
+    if (pdl_enabled()) cfg.numAttrs = 2;
+    return launched((int)(d.few_rows_cluster == kMostCluster ? cudaLaunchKernelEx(&cfg, few_rows_kernel<T, VEC, NV, kMostCluster>, a)
+                                                             : cudaLaunchKernelEx(&cfg, few_rows_kernel<T, VEC, NV, kPortableCluster>, a)), "RMS norm gradient");
 }
 
 template <class T, bool BULK, int W, int NV>
@@ -485,8 +495,8 @@ ew_status_t launch_grad(GradArgs a, float *dw, cudaStream_t st) {
 }
 
 template <class T, bool BULK>
-ew_status_t pick_grad(const GradArgs &a, float *dw, cudaStream_t st) {
-    if (few_rows(a.rows, a.width)) return a.width <= 1024 ? launch_few<T, BULK, 1>(a, dw, st) : launch_few<T, BULK, 2>(a, dw, st);
+ew_status_t pick_grad(const Device &d, const GradArgs &a, float *dw, cudaStream_t st) {
+    if (few_rows(a.rows, a.width)) return a.width <= 1024 ? launch_few<T, BULK, 1>(d, a, dw, st) : launch_few<T, BULK, 2>(d, a, dw, st);
     if (a.width <= 256) return launch_grad<T, BULK, 1, 1>(a, dw, st);
     if (a.width <= 512) return launch_grad<T, BULK, 1, 2>(a, dw, st);
     if (a.width <= kNarrow) return launch_grad<T, BULK, 1, 4>(a, dw, st);
@@ -501,25 +511,44 @@ int load_grad() {
     return (int)cudaFuncSetAttribute(grad_kernel<T, BULK, W, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<W>);
 }
 
+template <class T, bool VEC, int NV>
+int load_few(int *cluster) {
+    const auto kernel = few_rows_kernel<T, VEC, NV, kMostCluster>;
+    cudaFuncAttributes fa;
+    int rc = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) | (int)cudaFuncGetAttributes(&fa, few_rows_kernel<T, VEC, NV, kPortableCluster>), fit = 0;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    few_config(&cfg, &attr, kMostCluster, kFewWidth);
+    if (rc == 0) rc = (int)cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg);
+    if (rc == (int)cudaErrorInvalidClusterSize) {      // no room for any, either
+        cudaGetLastError();
+        rc = 0;
+    }
+    if (fit < 1) *cluster = kPortableCluster;
+    return rc;
+}
+
 template <class T, bool VEC>
-int load_one() {
+int load_one(int *cluster) {
     cudaFuncAttributes fa;
     return (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 1>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 1, 2>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 2, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 4, 2>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 2>) |
            (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 8, 4>) | (int)cudaFuncGetAttributes(&fa, norm_kernel<T, VEC, 16, 4>) |
            load_grad<T, VEC, 1, 1>() | load_grad<T, VEC, 1, 2>() | load_grad<T, VEC, 1, 4>() | load_grad<T, VEC, 4, 2>() | load_grad<T, VEC, 8, 2>() | load_grad<T, VEC, 16, 2>() | load_grad<T, VEC, 16, 4>() |
-           (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
-           (int)cudaFuncSetAttribute(few_rows_kernel<T, VEC, 2>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) |
-           (int)cudaFuncGetAttributes(&fa, parts_kernel);
+           load_few<T, VEC, 1>(cluster) | load_few<T, VEC, 2>(cluster) | (int)cudaFuncGetAttributes(&fa, parts_kernel);
 }
 
 bool bad_eps(float eps) { return !(eps >= 0.f && eps <= 3.402823466e38f); }
 
 }  // namespace
 
-// Loads the kernels (a first launch inside a graph capture would have to).
-int norm_setup() {
-    return load_one<__nv_bfloat16, false>() | load_one<__nv_bfloat16, true>() | load_one<__half, false>() | load_one<__half, true>();
+// Loads the kernels (a first launch inside a graph capture would have to) and finds out which cluster the gradient of few rows can have
+// (EW_DISABLE_CLUSTER16=1: the portable one).
+int norm_setup(Device *d) {
+    const char *e = getenv("EW_DISABLE_CLUSTER16");
+    int *c = &d->few_rows_cluster;
+    *c = e && e[0] == '1' ? kPortableCluster : kMostCluster;
+    return load_one<__nv_bfloat16, false>(c) | load_one<__nv_bfloat16, true>(c) | load_one<__half, false>(c) | load_one<__half, true>(c);
 }
 
 }  // namespace ops
@@ -575,6 +604,6 @@ extern "C" ew_status_t ew_rms_norm_grad(int32_t device, int32_t dtype, const voi
     if (rows == 0) return launched((int)cudaMemsetAsync(dweight, 0, (size_t)width * 4, st), "cudaMemsetAsync");
     const GradArgs a = {dy, t, weight, dt_in, dt, workspace, lddy, ldt, dt_in ? lddt_in : 0, lddt, rows, d->err, width, 0, (float)(1.0 / width), eps};
     const bool vec = !((((uintptr_t)dy | (uintptr_t)t | (uintptr_t)weight | (uintptr_t)dt_in | (uintptr_t)dt) & 15) | ((a.lddy | a.ldt | a.ldmore | a.lddt | width) & 7));
-    if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(a, dweight, st) : pick_grad<__nv_bfloat16, false>(a, dweight, st);
-    return vec ? pick_grad<__half, true>(a, dweight, st) : pick_grad<__half, false>(a, dweight, st);
+    if (dtype == EW_BF16) return vec ? pick_grad<__nv_bfloat16, true>(*d, a, dweight, st) : pick_grad<__nv_bfloat16, false>(*d, a, dweight, st);
+    return vec ? pick_grad<__half, true>(*d, a, dweight, st) : pick_grad<__half, false>(*d, a, dweight, st);
 }

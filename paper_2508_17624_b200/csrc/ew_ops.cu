@@ -34,7 +34,7 @@ ew_status_t resolve(Device *d, int device) {
     d->err = static_cast<int *>(err);
     cudaFuncAttributes fa;
     return launched((int)cudaFuncGetAttributes(&fa, take_error_kernel) | grouped_setup() | quant_setup() | swiglu_setup() | blocks_setup() |
-                    norm_setup() | scaled_setup(), "operator set-up");
+                    norm_setup(d) | scaled_setup(), "operator set-up");
 }
 
 }  // namespace

@@ -27,6 +27,7 @@ struct Device {
     int sm_count = 0;
     int *err = nullptr;              // device address of the error word
     EncodeTiled encode = nullptr;
+    int few_rows_cluster = 0;        // CTAs of the norm gradient of few rows
 };
 
 // The device's constants, resolved on first use (thread-safe).  The caller has made the device current.
@@ -40,7 +41,7 @@ int grouped_setup();
 int quant_setup();
 int swiglu_setup();
 int blocks_setup();
-int norm_setup();
+int norm_setup(Device *d);
 int scaled_setup();
 
 inline bool is_16bit(int dtype) { return dtype == EW_BF16 || dtype == EW_FP16; }

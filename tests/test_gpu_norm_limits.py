@@ -2,6 +2,10 @@
 
 Tolerances as in the tests of the formula: sums of squares off by at most 2^-18, results by half a step of their type.
 """
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -11,6 +15,7 @@ from test_gpu_scaled import NORM, grad_ref, randn, uneven
 
 pytestmark = pytest.mark.gpu
 BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 # one launch up to 384 rows of 2048, of which a team of warps takes every 64th
 SIZES = [(64, 2048), (65, 2048), (128, 2048), (129, 1024), (200, 999), (333, 2048), (384, 2048), (385, 2048), (384, 2049), (384, 2056), (65, 1333), (333, 1333), (384, 1025), (130, 1), (384, 7)]
 
@@ -74,3 +79,21 @@ def test_norm_grad_beyond_two_to_the_31_elements():
     dt, dw = binding.rms_norm_grad(t, t, w, t)
     assert not dt[:-64].any()
     check(dt[-64:], dw, t[-64:], t[-64:], w, t[-64:], 1e-6)
+
+
+def test_norm_grad_of_few_rows_in_the_portable_cluster():
+    """Where no cluster of sixteen CTAs fits: the same tests in a process that takes the one of eight, and its sums are of another order."""
+    code = ("import sys, torch; sys.path.insert(0, 'tests'); import test_gpu_norm_limits as t\n"
+            "for rows, width in t.SIZES:\n"
+            "    for pad in (0, 3):\n"
+            "        for with_dt in (True, False):\n"
+            "            t.test_norm_grad_of_few_rows(rows, width, pad, with_dt, torch.bfloat16)\n"
+            "dw = t.binding.rms_norm_grad(*t.inputs(384, 2048, torch.bfloat16, True, 0))[1]\n"
+            "print('sum', dw.view(torch.int32).long().sum().item())\n")
+
+    def run(**env):
+        r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT, env={**os.environ, "PYTHONPATH": ROOT, **env})
+        assert r.returncode == 0, r.stderr[-2000:]
+        return r.stdout.split()[-1]
+
+    assert run(EW_DISABLE_CLUSTER16="1") != run()
