@@ -115,7 +115,9 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
     }
 }
 
-constexpr int kMostCtas = 444;                         // of the gradient, three an SM, whose sums are the workspace (8192 x 2048: 27 us; two 34, four 31)
+// The gradient's CTAs are counted in SMs of a B200, whatever the device: their sums are the workspace, whose size a caller learns without naming one.
+constexpr int kSms = 148;
+constexpr int kMostCtas = 3 * kSms;                    // (8192 x 2048: 27 us; two an SM 34, four 31)
 constexpr int kMostStages = 3;
 // A CTA's rows on their way, at least one of the widest, of three operands; where one CTA has the SM, two (1024 x 16384: 45 us, with one 47.5)
 template <int W> constexpr int kRingBytes = W == 16 ? 196608 : 98304;
@@ -452,7 +454,7 @@ ew_status_t pick(const Args &a, cudaStream_t st) {
 constexpr int kNarrow = 1024;
 int grad_ctas(long long rows, int width) {
     const long long wanted = width <= kNarrow ? (rows + 7) / 8 : rows,
-                    most = width <= 256 ? kMostCtas : width <= 512 ? 296 : width <= kNarrow ? 148 : width <= 2048 ? kMostCtas : width <= 4096 ? 296 : 148;
+                    most = kSms * (width <= 256 ? 3 : width <= 512 ? 2 : width <= kNarrow ? 1 : width <= 2048 ? 3 : width <= 4096 ? 2 : 1);
     return (int)(wanted < most ? wanted : most);
 }
 bool few_rows(long long rows, int width) { return rows <= kFewRows && width <= kFewWidth; }
