@@ -8,8 +8,8 @@
 // stays in the registers of a warp (or of 8 or 16, for wide rows and few) between the sum and its use.  The weight's gradient
 // is summed in the registers of the threads that own its columns, over all rows that a CTA meets; a second kernel adds the
 // CTAs' sums up, in the same order every time (few rows: one cluster of CTAs, one kernel).  Measured: 8192 x 2048 with a
-// residual and both results 25.6 us = 5.9 TB/s (90 % of the measured copy bandwidth); its gradient 27 us = 4.9 TB/s, 23 of them the first
-// kernel's stream.
+// residual and both results 25.6 us = 5.9 TB/s (90 % of the measured copy bandwidth); its gradient 27.2 us = 4.9 TB/s, 23 of them the
+// first kernel's stream.
 #include "ew_blocks.cuh"
 #include "ew_ops.h"
 #include "ew_tc.cuh"
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreadsOf<W>) norm_kernel(const Args a) {
 constexpr int kSms = 148;
 constexpr int kMostCtas = 3 * kSms;                    // (8192 x 2048: 27 us; two an SM 34, four 31)
 constexpr int kMostStages = 3;
-// A CTA's rows on their way, at least one of the widest, of three operands; where one CTA has the SM, two (1024 x 16384: 45 us, with one 47.5)
+// A CTA's rows on their way, at least one of the widest, of three operands; where one CTA has the SM, two (1024 x 16384: 46.8 us, with one 47.8)
 template <int W> constexpr int kRingBytes = W == 16 ? 196608 : 98304;
 static_assert(kMostWidth * 6 * 2 <= kRingBytes<16>, "room for two rows");
 
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
     if (BULK && fetcher)
         for (int i = 0; i < a.stages; ++i)
             if (first + i * step < a.rows) fetch(first + i * step, i);
-    constexpr bool kHold = W * NV < 64;                // the weights in registers; those of the widest rows are read again (4096 x 16384: 106 us, held 123, for what spills)
+    constexpr bool kHold = W * NV < 64;                // the weights in registers; those of the widest rows are read again (4096 x 16384: 123 us, held 128, for what spills; without a third operand 110 and 120)
     Two weight[kHold ? NV : 1][4], dw[NV][4];
     auto weight_of = [&](Two (&v)[4], int i) {
         Eight<T> x;
@@ -283,9 +283,12 @@ __global__ void __launch_bounds__(kThreadsOf<W>, W == 4 && NV <= 2 ? 3 : W == 1 
 
 // The gradient of few rows in one launch: a cluster of sixteen CTAs, four teams of four warps in each, a row a team at a time, the next one
 // asked for before this one is worked on.  The teams' and then the CTAs' sums for dw are added up through shared memory, in their
-// order.  One launch and no workspace take the host 4 us less, which is what a call of few rows waits for: 2048 columns, alone and called from
-// Python, 128 rows 6.7 and 11.9 us, with the two kernels above 7.7 and 16; 333 rows 10.5 and 12 against 9.3 and 16; 512 rows 13.5 and 13.9 against
-// 9.0 and 16.  (Clusters of eight, the portable size: 333 rows 16 us.)
+// order.  One launch and no workspace take the host 4 us less, which is what a call of few rows waits for; a replayed graph does not wait for
+// it, and there the two kernels above are faster from 130 to 220 rows on.  Replayed and called from Python, us, with the two kernels behind the stroke:
+//   2048 columns: 64 rows 5.4, 11.3 / 6.3, 15.0; 220: 8.6, 11.3 / 8.4, 15.1; 333: 10.7, 11.3 / 8.9, 15.1; 384: 11.5, 11.9 / 8.7, 15.1; 512: 13.7, 14.2 / 8.9, 15.1
+//   1024 columns: 64 rows 3.8, 11.2 / 6.0, 15.0; 220: 5.6, 11.2 / 5.6, 15.1; 384: 7.3, 11.2 / 6.1, 15.1; 512: 8.6, 11.2 / 5.8, 15.1
+//    300 columns: 64 rows 3.8, 11.2 / 4.6, 15.1; 128: 4.8, 11.1 / 4.7, 15.1; 384: 8.6, 11.2 / 5.1, 15.2; 512: 10.4, 11.2 / 5.1, 15.2
+// The limit is where a call from Python gains what a replayed one loses, 3 us.  (Clusters of eight: 333 rows of 2048 17.4 us replayed.)
 // (A device whose GPCs, or what this process has of them, hold no cluster of sixteen takes one of eight, which all hold.)
 constexpr int kMostCluster = 16, kPortableCluster = 8, kTeams = 4, kTeamWarps = 4;
 constexpr int kFewRows = 384, kFewWidth = 2048;
