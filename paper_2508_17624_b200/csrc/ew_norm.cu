@@ -520,17 +520,15 @@ template <class T, bool VEC, int NV>
 int load_few(int *cluster) {
     const auto kernel = few_rows_kernel<T, VEC, NV, kMostCluster>;
     cudaFuncAttributes fa;
-    int rc = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) | (int)cudaFuncGetAttributes(&fa, few_rows_kernel<T, VEC, NV, kPortableCluster>), fit = 0;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
     few_config(&cfg, &attr, kMostCluster, kFewWidth);
-    if (rc == 0) rc = (int)cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg);
-    if (rc == (int)cudaErrorInvalidClusterSize) {      // no room for any, either
-        cudaGetLastError();
-        rc = 0;
+    int fit = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess || cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess || fit < 1) {
+        cudaGetLastError();                            // (an answer, not an error)
+        *cluster = kPortableCluster;
     }
-    if (fit < 1) *cluster = kPortableCluster;
-    return rc;
+    return (int)cudaFuncGetAttributes(&fa, kernel) | (int)cudaFuncGetAttributes(&fa, few_rows_kernel<T, VEC, NV, kPortableCluster>);
 }
 
 template <class T, bool VEC>
