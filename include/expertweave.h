@@ -330,7 +330,7 @@ typedef enum { EW_BF16 = 0, EW_FP16 = 1, EW_FP32 = 2, EW_E4M3 = 3, EW_E5M2 = 4 }
 /* Matrix product grouped by expert (Section 2.1's grouped matrix multiplication, on its own): for every group g and
  * its rows offsets[g] <= r < offsets[g+1]
  *     y[r, :] = x[r, :] w[g]^T        x [rows, k], w [groups, n, k] (group_stride elements between groups), y [rows, n]
- * summed in fp32 and rounded once.  An instruction of the tensor core adds 16 products to the running sum and cuts off, instead of
+ * summed in fp32 and rounded once.  An instruction of the tensor core adds 16 products to the running sum and cuts off (as measured), instead of
  * rounding, what lies below 2^-25 of the largest or behind the sum's 24th bit; sums are made in parts (1024 terms for fp32 results,
  * 8192 for fp16, 65536 for bf16) that are added up rounded.  A result is off by at most 4.1e-5 (fp32), 3.3e-4 (fp16) or 2.6e-3 (bf16; 0.66 of half a
  * step of either) of sum |x w| besides its own rounding and half a step of fp32 a part: that much only if one term is 2^25 times nearly all of the others.
@@ -421,7 +421,7 @@ ew_status_t ew_scaled_pack(int32_t device, int32_t dtype, const void *w, int64_t
  *     y[r, :] = x[r, :] w[g]^T  for  offsets[g] <= r < offsets[g+1]     of the values that the blocks stand for
  * x: blocks of rows, row_type EW_E4M3 or EW_E5M2; w: blocks of weights in EW_E4M3 (group_stride elements between matrices).  Every product
  * is exact; sums are fp32, made in parts (2048 terms for fp32 results, 8192 for fp16, 65536 for bf16) that are added up rounded.  An instruction of the tensor core adds
- * 32 products to the running sum and cuts off what lies below 2^-25 of the largest or behind the sum's 24th bit.  So a result is off by at most 7.1e-5 of
+ * 32 products to the running sum and cuts off (as measured) what lies below 2^-25 of the largest or behind the sum's 24th bit.  So a result is off by at most 7.1e-5 of
  * sum |x w| for fp32, 2.9e-4 for fp16 and 2.3e-3 for bf16 (0.58 of half a step of either) besides its own rounding and half a step of fp32 a part; that much only if one term is
  * 2^25 times nearly all of the others, 1e-7 as a rule.  out_dtype: EW_BF16, EW_FP16 or EW_FP32.
  * offsets: as there, and what is said there of rows outside them and of bad offsets; null: one group (groups = 1) of all rows.
